@@ -68,9 +68,12 @@ extern "C" {
 
 #define CFGZIP_DTYPE_F32 0
 #define CFGZIP_DTYPE_BF16 1
+#define CFGZIP_DTYPE_F16 2 /* the vocabulary projection's calls only, and MX4 */
+#define CFGZIP_DTYPE_MX4 3 /* hidden states of cfgzip_mx4_logits in blocks of 4-bit values */
 
 #define CFGZIP_BITS_TOKEN 0 /* `bits` is a token-level mask  [B][W(V)] */
 #define CFGZIP_BITS_CLASS 1 /* `bits` is a class-level mask  [B][W(C)], gathered through class_of_token */
+#define CFGZIP_BITS_NONE 2  /* no mask: every token is admitted (the vocabulary projection's calls only) */
 
 /* hipError_t (as int) of the last failing HIP call made by this host thread; 0 if none. */
 int cfgzip_last_hip_error(void);
@@ -434,6 +437,79 @@ int cfgzip_nfa_class_masks(const int32_t *state_mask, int32_t S, int32_t C,
 int cfgzip_nfa_advance_states(const int32_t *rel_rep, int32_t C, int32_t S,
                               const int32_t *class_of_token, int32_t V, const int32_t *tok, int32_t B,
                               int32_t *state_sets, void *stream);
+
+/*
+ * The vocabulary projection at the end of a model, under the grammar's masks.  The masked logits that the calls above take are
+ *     z[i][v] = sum_d hidden[i][d] * weight[v][d],
+ * with -infinity where row i does not admit token v (paper Section 2.2).  The calls below train that projection without the
+ * logits in memory, keep its weights in 4 bits, and make the masked logits from those.
+ *
+ * Masks of all of them: bits_kind CFGZIP_BITS_TOKEN (int32 [rows][W(V)]), CFGZIP_BITS_CLASS (int32 [rows][W(C)], gathered through
+ * class_of_token) or CFGZIP_BITS_NONE (bits, class_of_token NULL: every token is admitted).
+ */
+/*
+ * cfgzip_head_loss: cross entropy of every row against its target over the tokens that the row admits,
+ *     lse[i]  = log sum over admitted v of exp z[i][v]          (-inf if the row admits none)
+ *     loss[i] = lse[i] - z[i][target[i]]
+ * A target outside [0, V) is none: loss 0.  A target that the row does not admit: loss +inf.
+ *   hidden, weight   [N] and [V] rows of D elements, BF16 or F16 alike, hidden_stride and weight_stride ELEMENTS apart (>= D);
+ *                    any alignment to whole elements, fastest at multiples of 16 bytes and D, strides multiples of 8
+ *   target   int32 [N]
+ *   loss, lse   out, float [N]
+ *   ws       cfgzip_head_loss_workspace_bytes(N, V, D, bits_kind) bytes, 256-byte aligned
+ * cfgzip_head_loss_grad: with grad_loss float [N] and the lse of the call above,
+ *     dz[i][v] = grad_loss[i] * (exp(z[i][v] - lse[i]) - [v = target[i]])   for admitted v, else 0
+ *     grad_hidden[i] = sum_v dz[i][v] * weight[v],     grad_weight[v] = sum_i dz[i][v] * hidden[i]
+ * Rows whose target is none or not admitted (no step lowers an infinite loss), and rows whose grad_loss is 0, have dz = 0
+ * whatever their hidden states hold.  The weights have to be finite, those of masked tokens too.
+ *   grad_hidden, grad_weight   out, [N] and [V] rows of D elements of the inputs' type; either may be NULL
+ * dz is kept in the inputs' type for a piece of the vocabulary at a time; all sums are fp32, and nothing is added in an order that
+ * changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
+ */
+size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);
+int cfgzip_head_loss(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                     int32_t dtype, int32_t N, int32_t V, int32_t D, const int32_t *target,
+                     const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token, int32_t C,
+                     float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
+size_t cfgzip_head_loss_grad_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);
+int cfgzip_head_loss_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                          int32_t dtype, int32_t N, int32_t V, int32_t D, const int32_t *target,
+                          const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token, int32_t C,
+                          const float *lse, const float *grad_loss,
+                          void *grad_hidden, int64_t grad_hidden_stride,
+                          void *grad_weight, int64_t grad_weight_stride,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Values in 4 bits.  A row of K values is cut into nb = ceil(K / 32) blocks (the last one filled up with 0).  A block has the scale
+ * 2^e, e = max(floor(log2 max|x|) - 2, -127) (-127 for a block of zeros); a value is the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ * to x / 2^e, ties to the even code, at most 6.  A block with an infinity or a NaN in it is NaN as a whole.
+ *   codes    uint8 [R][16 * nb], 16-byte aligned: code = sign * 8 + index of the value above, the earlier value of two in the low half
+ *   scales   uint8 [R][nb]: e + 127, 255 for a NaN block
+ *   x        [R] rows of K elements, x_stride ELEMENTS apart; F32, BF16 or F16
+ * cfgzip_mx4_values writes what codes and scales stand for, rounded to `dtype` (exact in F32 and, down to 2^-133, in BF16).
+ * R = 0 enqueues nothing.
+ */
+int cfgzip_mx4_quantize(const void *x, int32_t dtype, int64_t R, int32_t K, int64_t x_stride,
+                        uint8_t *codes, uint8_t *scales, void *stream);
+int cfgzip_mx4_values(const uint8_t *codes, const uint8_t *scales, int64_t R, int32_t K,
+                      void *x, int32_t dtype, int64_t x_stride, void *stream);
+/*
+ * cfgzip_mx4_logits: logits[b][v] = sum_k hidden[b][k] * weight[v][k] where row b admits token v, else -inf, of weights in 4 bits.
+ * What masked places would hold does not matter: weights of tokens that no row admits may not even be read.
+ *   hidden         [B] rows of K values, hidden_stride elements apart, BF16 or F16 (hidden_scales NULL); or MX4: codes
+ *                  uint8 [B][16 * nb] (hidden_stride = 16 * nb, 16-byte aligned) with hidden_scales uint8 [B][nb]
+ *   codes, scales  of the V rows of weights
+ *   logits         out, [B] rows of V elements, row_stride ELEMENTS apart (>= V), F32 or BF16: what cfgzip_apply_mask takes
+ *   ws             cfgzip_mx4_logits_workspace_bytes(..) bytes, 256-byte aligned; NULL where that is 0
+ * Weights and hidden states go into the products without a further rounding; sums are fp32.  B = 0 enqueues nothing.
+ */
+size_t cfgzip_mx4_logits_workspace_bytes(int32_t hidden_dtype, int32_t B, int32_t V, int32_t K, int32_t bits_kind);
+int cfgzip_mx4_logits(const void *hidden, int32_t hidden_dtype, int64_t hidden_stride, const uint8_t *hidden_scales,
+                      const uint8_t *codes, const uint8_t *scales, int32_t B, int32_t V, int32_t K,
+                      const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token, int32_t C,
+                      void *logits, int32_t dtype, int64_t row_stride,
+                      void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,12 @@ from .binding import (  # noqa: F401
     cfgzip_displacements,
     cfgzip_engine_step,
     cfgzip_expand_mask,
+    cfgzip_head_loss,
+    cfgzip_head_loss_grad,
     cfgzip_map_to_rep,
+    cfgzip_mx4_logits,
+    cfgzip_mx4_quantize,
+    cfgzip_mx4_values,
     cfgzip_nfa_advance_states,
     cfgzip_nfa_class_masks,
     cfgzip_nfa_signatures,

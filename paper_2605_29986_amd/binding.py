@@ -35,8 +35,11 @@ DEFAULT_HASH_SEED = 0x5EED_CF62_1234_ABCD
 
 CFGZIP_DTYPE_F32 = 0
 CFGZIP_DTYPE_BF16 = 1
+CFGZIP_DTYPE_F16 = 2
+CFGZIP_DTYPE_MX4 = 3
 CFGZIP_BITS_TOKEN = 0
 CFGZIP_BITS_CLASS = 1
+CFGZIP_BITS_NONE = 2
 
 _ERRORS = {
     -1: "CFGZIP_E_INVALID (bad argument)",
@@ -147,6 +150,23 @@ def load_library() -> ctypes.CDLL:
     lib.cfgzip_displacements.restype = ctypes.c_int
     lib.cfgzip_displacements.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, u64,
                                          vp, sz, vp]
+    lib.cfgzip_head_loss_workspace_bytes.restype = sz
+    lib.cfgzip_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.cfgzip_head_loss.restype = ctypes.c_int
+    lib.cfgzip_head_loss.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+    lib.cfgzip_head_loss_grad_workspace_bytes.restype = sz
+    lib.cfgzip_head_loss_grad_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.cfgzip_head_loss_grad.restype = ctypes.c_int
+    lib.cfgzip_head_loss_grad.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp, i64,
+                                          vp, i64, vp, sz, vp]
+    lib.cfgzip_mx4_quantize.restype = ctypes.c_int
+    lib.cfgzip_mx4_quantize.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
+    lib.cfgzip_mx4_values.restype = ctypes.c_int
+    lib.cfgzip_mx4_values.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+    lib.cfgzip_mx4_logits_workspace_bytes.restype = sz
+    lib.cfgzip_mx4_logits_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.cfgzip_mx4_logits.restype = ctypes.c_int
+    lib.cfgzip_mx4_logits.argtypes = [vp, i32, i64, vp, vp, vp, i32, i32, i32, vp, i32, vp, i32, vp, i32, i64, vp, sz, vp]
     _decode_step, _engine_step, _signatures, _build_classes, _displacements, _nfa_signatures = _load_stepcall(lib)
     _lib = lib
     return lib
@@ -660,3 +680,210 @@ def cfgzip_engine_step(logits: torch.Tensor, state_mask: torch.Tensor, C: int,
         _stream(stream))
     _check("cfgzip_engine_step", rc)
     return states_out
+
+
+# ---------------------------------------------------------------- the vocabulary projection
+
+_DTYPE = {torch.float32: CFGZIP_DTYPE_F32, torch.bfloat16: CFGZIP_DTYPE_BF16, torch.float16: CFGZIP_DTYPE_F16}
+
+
+def _rows(t: torch.Tensor, name: str, dtypes, columns: Optional[int] = None) -> Tuple[int, int]:
+    """(address, row stride in elements) of a 2-D GPU tensor of one of `dtypes` with unit column stride"""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a tensor in GPU memory")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must have dtype {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if t.dim() != 2 or (columns is not None and t.shape[1] != columns):
+        raise ValueError(f"{name} must be 2-D" + (f" with {columns} columns" if columns is not None else ""))
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    stride = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if rows > 1 and stride < cols:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return t.data_ptr(), stride
+
+
+def _vector(t: torch.Tensor, dtype, n: int, name: str) -> int:
+    p = _dev(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return p
+
+
+def _masks(bits, class_of_token, C, rows: int, V: int):
+    """(bits, bits_kind, class_of_token, C) of a call with `rows` rows"""
+    if bits is None:
+        if class_of_token is not None or C:
+            raise ValueError("class_of_token and C go with bits")
+        return None, CFGZIP_BITS_NONE, None, 0
+    words = words_for(V if class_of_token is None else C)
+    if bits.dim() != 2 or bits.shape[0] != rows or bits.shape[1] != words:
+        raise ValueError("bits must be [rows, ceil(C/32)] with class_of_token, [rows, ceil(V/32)] without")
+    if class_of_token is None:
+        return _dev(bits, torch.int32, "bits"), CFGZIP_BITS_TOKEN, None, 0
+    return (_dev(bits, torch.int32, "bits"), CFGZIP_BITS_CLASS, _vector(class_of_token, torch.int32, V, "class_of_token"),
+            int(C))
+
+
+def _same_device(device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} must be on {device}")
+
+
+def _head(hidden, weight, target, bits, class_of_token, C):
+    """The arguments that cfgzip_head_loss and cfgzip_head_loss_grad share"""
+    w, w_stride = _rows(weight, "weight", (torch.bfloat16, torch.float16))
+    V, D = weight.shape
+    h, h_stride = _rows(hidden, "hidden", (weight.dtype,), D)
+    _same_device(weight.device, hidden=hidden, target=target, bits=bits, class_of_token=class_of_token)
+    N = hidden.shape[0]
+    t = _vector(target, torch.int32, N, "target")
+    return (h, h_stride, w, w_stride, _DTYPE[weight.dtype], N, V, D, t, *_masks(bits, class_of_token, C, N, V))
+
+
+def cfgzip_head_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, *,
+                     bits: Optional[torch.Tensor] = None, class_of_token: Optional[torch.Tensor] = None, C: int = 0,
+                     loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, lse) float32 [N]: cross entropy of hidden [N, D] (bfloat16 or float16, rows any stride apart) through weight
+    [V, D] against target int32 [N], over the tokens that `bits` admits (masks over classes with `class_of_token` and `C`, over
+    tokens without, every token without `bits`).  A target outside [0, V) has loss 0, one that is not admitted +inf."""
+    lib = _lib or load_library()
+    args = _head(hidden, weight, target, bits, class_of_token, C)
+    N, V, D, kind = args[5], args[6], args[7], args[10]
+    dev = weight.device
+    loss = torch.empty((N,), dtype=torch.float32, device=dev) if loss is None else loss
+    lse = torch.empty((N,), dtype=torch.float32, device=dev) if lse is None else lse
+    if workspace is None:
+        workspace = _workspace(lib.cfgzip_head_loss_workspace_bytes(N, V, D, kind), dev)
+    _same_device(dev, loss=loss, lse=lse, workspace=workspace)
+    rc = lib.cfgzip_head_loss(*args, _vector(loss, torch.float32, N, "loss"), _vector(lse, torch.float32, N, "lse"),
+                              _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("cfgzip_head_loss", rc)
+    return loss, lse
+
+
+def cfgzip_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
+                          grad_loss: torch.Tensor, *, bits: Optional[torch.Tensor] = None,
+                          class_of_token: Optional[torch.Tensor] = None, C: int = 0, want_hidden: bool = True,
+                          want_weight: bool = True, grad_hidden: Optional[torch.Tensor] = None,
+                          grad_weight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                          ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(grad_hidden [N, D], grad_weight [V, D]) in the inputs' type for grad_loss float32 [N], with the lse of cfgzip_head_loss
+    on the same inputs.  Rows without a target, or with one that is not admitted, have no gradient."""
+    lib = _lib or load_library()
+    args = _head(hidden, weight, target, bits, class_of_token, C)
+    N, V, D, kind = args[5], args[6], args[7], args[10]
+    dev = weight.device
+    if want_hidden and grad_hidden is None:
+        grad_hidden = torch.empty((N, D), dtype=weight.dtype, device=dev)
+    if want_weight and grad_weight is None:
+        grad_weight = torch.empty((V, D), dtype=weight.dtype, device=dev)
+    outs = []
+    for t, rows, name in ((grad_hidden if want_hidden else None, N, "grad_hidden"),
+                          (grad_weight if want_weight else None, V, "grad_weight")):
+        if t is None:
+            outs += [None, 0]
+            continue
+        outs += _rows(t, name, (weight.dtype,), D)
+        if t.shape[0] != rows:
+            raise ValueError(f"{name} must have {rows} rows")
+    if outs[0] is None and outs[2] is None:
+        raise ValueError("one of the gradients must be wanted")
+    if workspace is None:
+        workspace = _workspace(lib.cfgzip_head_loss_grad_workspace_bytes(N, V, D, kind), dev)
+    _same_device(dev, lse=lse, grad_loss=grad_loss, grad_hidden=grad_hidden, grad_weight=grad_weight, workspace=workspace)
+    rc = lib.cfgzip_head_loss_grad(*args, _vector(lse, torch.float32, N, "lse"),
+                                   _vector(grad_loss, torch.float32, N, "grad_loss"), *outs,
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("cfgzip_head_loss_grad", rc)
+    return grad_hidden if want_hidden else None, grad_weight if want_weight else None
+
+
+def _blocks(K: int) -> int:
+    return (int(K) + 31) // 32
+
+
+def _mx4(codes, scales, name: str) -> Tuple[int, int, int, int]:
+    """(codes, scales, rows, blocks of a row)"""
+    c, s = _dev(codes, torch.uint8, f"{name}codes"), _dev(scales, torch.uint8, f"{name}scales")
+    if scales.dim() != 2 or tuple(codes.shape) != (scales.shape[0], 16 * scales.shape[1]):
+        raise ValueError(f"{name}codes must be [rows, 16 * blocks] and {name}scales [rows, blocks]")
+    return c, s, scales.shape[0], scales.shape[1]
+
+
+def cfgzip_mx4_quantize(x: torch.Tensor, *, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                        stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes uint8 [R, 16 * nb], scales uint8 [R, nb]), nb = ceil(K / 32), of x [R, K] (float32, bfloat16 or float16, rows any
+    stride apart): blocks of 32 values in 4 bits with a shared power of two."""
+    lib = _lib or load_library()
+    p, stride = _rows(x, "x", tuple(_DTYPE))
+    R, K = x.shape
+    nb = _blocks(K)
+    if codes is None:
+        codes = torch.empty((R, 16 * nb), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((R, nb), dtype=torch.uint8, device=x.device)
+    c, s, rows, blocks = _mx4(codes, scales, "")
+    if (rows, blocks) != (R, nb):
+        raise ValueError("codes and scales must be those of x")
+    _same_device(x.device, codes=codes, scales=scales)
+    _check("cfgzip_mx4_quantize", lib.cfgzip_mx4_quantize(p, _DTYPE[x.dtype], R, K, stride, c, s, _stream(stream)))
+    return codes, scales
+
+
+def cfgzip_mx4_values(codes: torch.Tensor, scales: torch.Tensor, K: int, *, dtype=torch.float32,
+                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """What codes and scales of rows of K values stand for, [R, K] in `dtype`."""
+    lib = _lib or load_library()
+    c, s, R, nb = _mx4(codes, scales, "")
+    if _blocks(K) != nb:
+        raise ValueError("scales must have ceil(K / 32) columns")
+    if out is None:
+        out = torch.empty((R, K), dtype=dtype, device=codes.device)
+    p, stride = _rows(out, "out", tuple(_DTYPE), K)
+    if out.shape[0] != R:
+        raise ValueError(f"out must have {R} rows")
+    _same_device(codes.device, scales=scales, out=out)
+    _check("cfgzip_mx4_values", lib.cfgzip_mx4_values(c, s, R, K, p, _DTYPE[out.dtype], stride, _stream(stream)))
+    return out
+
+
+def cfgzip_mx4_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *,
+                      hidden_scales: Optional[torch.Tensor] = None, dtype=torch.float32, bits: Optional[torch.Tensor] = None,
+                      class_of_token: Optional[torch.Tensor] = None, C: int = 0, logits: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Logits [B, V] (float32 or bfloat16) of hidden [B, K] (bfloat16 or float16; or codes uint8 [B, 16 * nb] with hidden_scales
+    uint8 [B, nb]) and weights in 4 bits (codes, scales of V rows of K values), -inf where `bits` does not admit the token."""
+    lib = _lib or load_library()
+    c, s, V, nb = _mx4(codes, scales, "")
+    dev = codes.device
+    if hidden_scales is None:
+        h, h_stride = _rows(hidden, "hidden", (torch.bfloat16, torch.float16))
+        hs, (B, K), kind = None, hidden.shape, _DTYPE[hidden.dtype]
+        if _blocks(K) != nb:
+            raise ValueError("hidden and weights must have rows of as many blocks")
+    else:
+        h, hs, B, blocks = _mx4(hidden, hidden_scales, "hidden ")
+        if blocks != nb:
+            raise ValueError("hidden and weights must have rows of as many blocks")
+        h_stride, K, kind = 16 * nb, 32 * nb, CFGZIP_DTYPE_MX4
+    masks = _masks(bits, class_of_token, C, B, V)
+    if logits is None:
+        logits = torch.empty((B, V), dtype=dtype, device=dev)
+    p, stride = _rows(logits, "logits", (torch.float32, torch.bfloat16), V)
+    if logits.shape[0] != B:
+        raise ValueError(f"logits must have {B} rows")
+    if workspace is None:
+        need = lib.cfgzip_mx4_logits_workspace_bytes(kind, B, V, K, masks[1])
+        workspace = _workspace(need, dev) if need else None
+    _same_device(dev, hidden=hidden, scales=scales, hidden_scales=hidden_scales, bits=bits, class_of_token=class_of_token,
+                 logits=logits, workspace=workspace)
+    rc = lib.cfgzip_mx4_logits(
+        h, kind, h_stride, hs, c, s, B, V, K, *masks, p, _DTYPE[logits.dtype], stride,
+        _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
+        workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("cfgzip_mx4_logits", rc)
+    return logits
