@@ -15,27 +15,33 @@
 namespace cfgzip {
 namespace {
 
-using Shape16 = Shape<64, 16, 4, 1>;     // few rows: reading the weights is what counts, many small workgroups
-using Shape64 = Shape<128, 64, 4, 1>;
-using Shape128 = Shape<256, 128, 4, 2>;
-using Shape256 = Shape<256, 256, 2, 4>;
-using ShapeFlat = Shape<128, 256, 2, 4>;  // weight gradients of small hidden sizes
+using Shape16 = Shape<64, 16, 4, 1, 4>;  // few rows: reading the weights is what counts, many small workgroups
+using Shape64 = Shape<128, 64, 4, 1, 3>;
+using Shape128 = Shape<256, 128, 4, 2, 3>;
+using Shape256 = Shape<256, 256, 2, 2, 2>;
+using ShapeFlat = Shape<128, 256, 2, 4, 3>;  // weight gradients of small hidden sizes
+
+// workgroups that are at work at a time: as many to a compute unit as its LDS holds
+template <typename S>
+constexpr int64_t slots() {
+    return 256 * (160 * 1024 / (S::kStages * S::kLds));
+}
 
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time: the size of the last-level cache
+// Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum instead of lse, which
+// large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
+// than the products, which are twice as many.
+constexpr int32_t kFewRows = 128;
 constexpr int32_t kPieceLeast = 2048;              // columns
+constexpr int32_t kSplitLeast = 256;               // of the sum over the vocabulary: the steps that a workgroup takes at the least
+constexpr int32_t kMaxRows = 1 << 22;               // offsets in a tile of dz stay below 2^32
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kInf = __builtin_inff();
 
 struct Masks {
     const int32_t *bits;  // [N][words], over tokens; null: every token is admitted
     int64_t words;
 };
-
-// bit r: whether token v + r is admitted, for the four tokens from v on (v a multiple of 4)
-__device__ __forceinline__ uint32_t admitted4(const Masks &m, uint32_t word, int32_t v, int32_t V) {
-    const int32_t left = V - v;
-    const uint32_t there = left >= 4 ? 15u : left <= 0 ? 0u : (1u << left) - 1u;
-    return m.bits ? (word >> (v & 31)) & there : there;
-}
 
 struct LogitsArgs {
     Operand W, H;  // [V][D], [N][D]
@@ -50,103 +56,159 @@ struct LogitsArgs {
     // backward
     const float *lse;
     const float *scaled_grad;  // 0: the row has no gradient
-    uint16_t *dz;              // [rows][ld]
-    int64_t dz_ld;
+    uint16_t *dz;              // [piece / 64][dz_rows][64]
+    int64_t dz_rows;
+    float *z;                  // [tokens / 64][N][64], -inf where not admitted
 };
 
-enum : int { STATISTICS = 0, GRADIENT = 1 };
+// what becomes of a tile of logits: maxima and sums; those and the logits themselves, of few rows; dz
+enum : int { STATISTICS = 0, KEPT = 1, GRADIENT = 2 };
 
 template <typename T, typename S, bool DIRECT, int WHAT>
 __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
     using TileA = Tile<S::BM, S::kThreads, false, DIRECT>;
     using TileB = Tile<S::BN, S::kThreads, false, true>;
-    __shared__ __attribute__((aligned(16))) char lds0[S::kLds], lds1[S::kLds];
-    int32_t tm, tn;
-    tile_of(blockIdx.x, gridDim.x, a.tiles_m, a.tiles_n, tm, tn);
-    f32x4 acc[S::FM][S::FN];
-    multiply<T, S, TileA, TileB>(a.W, a.H, tm * S::BM, tn * S::BN, 0, a.D, lds0, lds1, acc);
-
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int wm = wave / S::WN, wn = wave % S::WN, g = lane >> 4;
-    const int32_t first = tm * S::BM + wm * S::TM;  // in the piece
-    const int32_t v_first = a.v0 + first;
-#pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int32_t row = tn * S::BN + wn * S::TN + 16 * j + (lane & 15);
-        const bool in = row < a.N;
-        const int32_t at = in ? row : a.N - 1;
-        const int32_t target = a.target[at];
-        uint32_t words[(S::TM + 31) / 32] = {};
-        if (a.masks.bits) {
-#pragma unroll
-            for (int w = 0; w < (S::TM + 31) / 32; ++w) {
-                const int64_t k = (v_first >> 5) + w;
-                words[w] = k < a.masks.words ? (uint32_t)a.masks.bits[at * a.masks.words + k] : 0u;
+    CFGZIP_STAGES(S, lds);
+    auto work = [&](int32_t i, Work &w) CFGZIP_INLINE {
+        const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n, t = blockIdx.x + i * gridDim.x;
+        if (t >= total) return false;
+        int32_t tm, tn;
+        tile_of(t, total, a.tiles_m, a.tiles_n, tm, tn);
+        w = Work{tm * S::BM, tn * S::BN, 0, a.D};
+        return true;
+    };
+    auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
+        int32_t tm, tn;
+        tile_of(blockIdx.x + i * gridDim.x, (uint32_t)a.tiles_m * a.tiles_n, a.tiles_m, a.tiles_n, tm, tn);
+        const int g = lane >> 4;
+        const int32_t first = tm * S::BM + wm * S::TM;  // in the piece
+        const int32_t v_first = a.v0 + first;
+        const bool masked = a.masks.bits || v_first + S::TM > a.V;
+        each<S::FN>([&](auto jj) CFGZIP_INLINE {
+            constexpr int j = jj.value;
+            const int32_t row = tn * S::BN + wn * S::TN + 16 * j + (lane & 15);
+            const bool in = row < a.N;
+            const int32_t at = in ? row : a.N - 1;
+            if (masked) {  // what a row does not admit becomes -inf, whatever it was
+                each<(S::TM + 31) / 32>([&](auto ww) CFGZIP_INLINE {
+                    const int64_t k = (v_first >> 5) + ww.value;
+                    uint32_t word = 0;
+                    if (k < a.masks.words) word = a.masks.bits ? (uint32_t)a.masks.bits[at * a.masks.words + k] : ~0u;
+                    const int32_t left = a.V - (int32_t)k * 32;  // tokens from the word's first on
+                    if (left < 32) word &= left > 0 ? (1u << left) - 1u : 0u;
+                    each<(S::TM < 32 ? S::FM : 2)>([&](auto ii) CFGZIP_INLINE {
+                        constexpr int i = ww.value * 2 + ii.value;
+                        const int32_t four = (int32_t)(word >> (((v_first & 31) + 16 * ii.value + 4 * g) & 31));
+                        each<4>([&](auto r) CFGZIP_INLINE {
+                            const uint32_t keep = (uint32_t)((int32_t)((uint32_t)four << (31 - r.value)) >> 31);
+                            const float z = acc[i][j][r.value];  // (a cast of the element itself takes the first one's bits)
+                            acc[i][j][r.value] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, z) & keep) | (0xFF800000u & ~keep));
+                        });
+                    });
+                });
             }
-        }
-        if constexpr (WHAT == STATISTICS) {
-            float most = -kInf;
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i) {
-                const int32_t v = v_first + 16 * i + 4 * g;
-                const uint32_t ok = admitted4(a.masks, words[i / 2], v, a.V);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (ok >> r & 1) most = fmaxf(most, acc[i][j][r]);
-                    if (in && v + r == target) a.z_target[row] = acc[i][j][r];
+            const int32_t mark = a.target[at] - v_first - 4 * g;  // the target is element mark % 16 of fragment mark / 16
+            const bool marked = __builtin_amdgcn_ballot_w64(in && mark >= 0 && mark < S::TM) != 0;  // seldom
+            if constexpr (WHAT != GRADIENT) {
+                float most = -kInf;
+                each<S::FM>([&](auto i) CFGZIP_INLINE {
+                    most = fmaxf(fmaxf(most, acc[i.value][j][0]), acc[i.value][j][1]);
+                    most = fmaxf(fmaxf(most, acc[i.value][j][2]), acc[i.value][j][3]);
+                });
+                if (WHAT == STATISTICS && marked) {
+                    float z = 0.0f;
+                    bool mine = false;
+                    each<S::FM * 4>([&](auto e) CFGZIP_INLINE {
+                        const bool here = mark == e.value / 4 * 16 + e.value % 4;
+                        z = here ? acc[e.value / 4][j][e.value % 4] : z;
+                        mine |= here;
+                    });
+                    if (in && mine) a.z_target[row] = z;
                 }
-            }
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            const float shift = most == -kInf ? 0.0f : most;
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i) {
-                const uint32_t ok = admitted4(a.masks, words[i / 2], v_first + 16 * i + 4 * g, a.V);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum += ok >> r & 1 ? __expf(acc[i][j][r] - shift) : 0.0f;
-            }
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
-            if (g == 0 && in) a.parts[(int64_t)(tm * S::WM + wm) * a.N + row] = f32x2{most, sum};
-        } else {
-            const float lse = a.lse[at], grad = in ? a.scaled_grad[at] : 0.0f;
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i) {
-                const int32_t v = v_first + 16 * i + 4 * g;
-                const uint32_t ok = grad != 0.0f ? admitted4(a.masks, words[i / 2], v, a.V) : 0u;
-                f32x4 d;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __expf(acc[i][j][r] - lse) - (v + r == target ? 1.0f : 0.0f);
-                    d[r] = ok >> r & 1 ? p * grad : 0.0f;
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float shift = most == -kInf ? 0.0f : most;
+                float sum = 0.0f;
+                each<S::FM * 4>([&](auto e) CFGZIP_INLINE {
+                    sum += __builtin_amdgcn_exp2f((acc[e.value / 4][j][e.value % 4] - shift) * kLog2e);
+                });
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (g == 0 && in) a.parts[(int64_t)(tm * S::WM + wm) * a.N + row] = f32x2{most, sum};
+                if (WHAT == KEPT && in) {
+                    float *const out = a.z + ((int64_t)(first >> 6) * a.N + row) * 64 + (first & 63) + 4 * g;
+                    each<S::FM>([&](auto i) CFGZIP_INLINE {
+                        *reinterpret_cast<f32x4 *>(out + (int64_t)(i.value / 4) * a.N * 64 + i.value % 4 * 16) = acc[i.value][j];
+                    });
                 }
-                *reinterpret_cast<u32x2 *>(a.dz + row * a.dz_ld + first + 16 * i + 4 * g) = round4<T>(d);
+            } else {
+                const float grad = in ? a.scaled_grad[at] : 0.0f;
+                // rows without a gradient have hidden states of 0 here, so logits of 0 or -inf, and exp(-inf) * 0
+                const float shift = grad != 0.0f ? a.lse[at] : kInf;
+                uint16_t *const out = a.dz + row * 64 + (first >> 6) * (a.dz_rows * 64) + (first & 63) + 4 * g;
+                each<S::FM>([&](auto i) CFGZIP_INLINE {
+                    f32x4 d;
+                    each<4>([&](auto r) CFGZIP_INLINE {
+                        d[r.value] = __builtin_amdgcn_exp2f((acc[i.value][j][r.value] - shift) * kLog2e) * grad;
+                    });
+                    if (marked) {
+                        each<4>([&](auto r) CFGZIP_INLINE {
+                            if (mark == 16 * i.value + r.value && acc[i.value][j][r.value] > -kInf) d[r.value] -= grad;
+                        });
+                    }
+                    *reinterpret_cast<u32x2 *>(out + (i.value / 4) * (a.dz_rows * 64) + i.value % 4 * 16) = round4<T>(d);
+                });
             }
-        }
-    }
+        });
+    };
+    multiply<T, S, TileA, TileB>(a.W, a.H, lds, work, store);
 }
 
-// Joins the parts of 16 rows: lse and loss.
-__global__ __launch_bounds__(256) void join_kernel(const f32x2 *parts, int32_t count, int32_t N, int32_t V, Masks masks,
-                                                   const int32_t *target, const float *z_target, float *loss, float *lse) {
-    __shared__ f32x2 shared[16][17];
-    const int r = threadIdx.x & 15, s = threadIdx.x >> 4;
-    const int32_t row = blockIdx.x * 16 + r;
-    float most = -kInf, sum = 0.0f;
-    auto take = [&](f32x2 p) {
-        const float m = fmaxf(most, p[0]);
-        // a part without admitted tokens has the maximum -inf and the sum 0 (or NaN, of logits that are)
-        sum = (most == -kInf ? sum : sum * __expf(most - m)) + (p[0] == -kInf ? p[1] : p[1] * __expf(p[0] - m));
-        most = m;
+// Joins the parts of a row: lse and loss, or (`whole` given) its maximum and sum.  A workgroup has ROWS rows and splits the parts over the other lanes; a lane asks for
+// eight parts before it uses the first.
+template <int ROWS>
+__global__ __launch_bounds__(1024) void join_kernel(const f32x2 *parts, int32_t count, int32_t N, int32_t V, Masks masks,
+                                                    const int32_t *target, const float *z_target, float *loss, float *lse,
+                                                    f32x2 *whole) {
+    constexpr int kShares = 1024 / ROWS;
+    struct Part {
+        float most;
+        double sum;  // the sum of a row that is certain is 1 and very little, and that little is its gradient
     };
-    if (row < N)
-        for (int32_t p = s; p < count; p += 16) take(parts[(int64_t)p * N + row]);
-    shared[s][r] = f32x2{most, sum};
-    __syncthreads();
+    __shared__ Part shared[kShares][ROWS + 1];
+    const int r = threadIdx.x % ROWS, s = threadIdx.x / ROWS;
+    const int32_t row = blockIdx.x * ROWS + r;
+    float most = -kInf;
+    double sum = 0.0;
+    auto take = [&](float m, double x) {
+        const float top = fmaxf(most, m);
+        // a part without admitted tokens has the maximum -inf and the sum 0 (or NaN, of logits that are)
+        sum = (most == -kInf ? sum : sum * __expf(most - top)) + (m == -kInf ? x : x * __expf(m - top));
+        most = top;
+    };
+    if (row < N) {
+        for (int32_t p = s; p < count; p += 8 * kShares) {
+            f32x2 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p + i * kShares < count ? parts[(int64_t)(p + i * kShares) * N + row] : f32x2{-kInf, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) take(x[i][0], x[i][1]);
+        }
+    }
+    shared[s][r] = Part{most, sum};
+    for (int half = kShares / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (s < half) {
+            take(shared[s + half][r].most, shared[s + half][r].sum);
+            shared[s][r] = Part{most, sum};
+        }
+    }
     if (s != 0 || row >= N) return;
-    for (int p = 1; p < 16; ++p) take(shared[p][r]);
-    const float l = (most == -kInf ? 0.0f : most) + logf(sum);
+    if (whole) {
+        whole[row] = f32x2{most, (float)sum};
+        return;
+    }
+    const float l = (most == -kInf ? 0.0f : most) + logf((float)sum);
     const int32_t t = target[row];
     float out = 0.0f;
     if (t >= 0 && t < V) {
@@ -157,45 +219,90 @@ __global__ __launch_bounds__(256) void join_kernel(const f32x2 *parts, int32_t c
     loss[row] = out;
 }
 
-// The rows' gradients times a power of two that brings the largest to at most 2^14, so that dz fills the range of fp16 (bf16
-// would not need it), and 2 to minus that; 0 for rows whose target is none or not admitted.  One workgroup.
-__global__ __launch_bounds__(1024) void rows_kernel(const float *grad_loss, const int32_t *target, int32_t N, int32_t V, Masks masks,
-                                                    float *scaled, float *unscale) {
-    __shared__ float shared[16];
-    auto grad_of = [&](int32_t i) {
+// Row i's gradient; 0 if its target is none or not admitted.
+struct Rows {
+    const float *grad_loss;
+    const int32_t *target;
+    int32_t N, V;
+    Masks masks;
+    __device__ __forceinline__ float grad(int32_t i) const {
         const int32_t t = target[i];
         if (t < 0 || t >= V) return 0.0f;
         if (masks.bits && !(masks.bits[i * masks.words + (t >> 5)] >> (t & 31) & 1)) return 0.0f;
         return grad_loss[i];
-    };
-    float most = 0.0f;
-    for (int32_t i = threadIdx.x; i < N; i += 1024) {
-        const float x = fabsf(grad_of(i));
-        if (x < kInf) most = fmaxf(most, x);
     }
-    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
-    __syncthreads();
-    for (int i = 0; i < 16; ++i) most = fmaxf(most, shared[i]);
-    int e = 0;
-    if (most > 0.0f) {
-        frexpf(most, &e);  // most < 2^e
-        e = 14 - e;
-        e = e > 100 ? 100 : e < -100 ? -100 : e;
+    // The factor that makes the largest finite gradient 2^14, so that dz fills the range of fp16 (bf16 would not need it), and where all
+    // are the same, as those of a mean, a row that is certain and wrong has dz without a rounding.  For all threads of a workgroup,
+    // whose waves leave their maxima in `shared`.
+    __device__ float scale(float *shared) const {
+        float most = 0.0f;
+        for (int32_t i = threadIdx.x; i < N; i += blockDim.x) {
+            const float x = fabsf(grad(i));
+            if (x < kInf) most = fmaxf(most, x);
+        }
+        for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
+        __syncthreads();
+        for (int i = 0; i < (int)blockDim.x / kWave; ++i) most = fmaxf(most, shared[i]);
+        return 0x1p14f / fminf(fmaxf(most, 0x1p-86f), 0x1p114f);
     }
-    for (int32_t i = threadIdx.x; i < N; i += 1024) scaled[i] = ldexpf(grad_of(i), e);
-    if (threadIdx.x == 0) *unscale = ldexpf(1.0f, -e);
+};
+
+__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale) {
+    __shared__ float shared[16];
+    const float factor = rows.scale(shared);
+    for (int32_t i = threadIdx.x; i < rows.N; i += 1024) scaled[i] = rows.grad(i) * factor;
+    if (threadIdx.x == 0) *unscale = 1.0f / factor;
 }
 
-// hidden states in rows of whole units of 8 elements; zeros in rows that have no gradient (`scaled`, or null), whatever they hold
-__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, const float *scaled,
-                                                        uint16_t *y, int32_t y_ld) {
+// dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
+// leave, the rest 0.  A thread has four tokens.
+template <typename T>
+__global__ __launch_bounds__(256) void few_rows_dz_kernel(Rows rows, const float *z, int32_t blocks, const f32x2 *whole, uint16_t *dz,
+                                                          int32_t dz_rows, float *unscale) {
+    __shared__ float shared[4];
+    const float factor = rows.scale(shared);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = 1.0f / factor;
+    const int32_t N = rows.N, span = dz_rows - N;
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int32_t q = (int32_t)(k & 15), r = (int32_t)((k >> 4) % span);
+    const int64_t block = (k >> 4) / span;
+    if (block >= blocks) return;
+    uint16_t *const out = dz + block * dz_rows * 64 + q * 4;
+    u32x2 hi = {0, 0}, lo = {0, 0};
+    if (r < N) {
+        const float grad = rows.grad(r) * factor;
+        if (grad != 0.0f) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(z + (block * N + r) * 64 + q * 4);
+            const f32x2 w = whole[r];
+            const int32_t mark = rows.target[r] - (int32_t)(block * 64 + q * 4);
+            f32x4 d, rest;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = x[j] == -kInf ? 0.0f : __expf(x[j] - w[0]) / w[1];
+                d[j] = (p - (j == mark ? 1.0f : 0.0f)) * grad;
+                rest[j] = d[j] - T::value(T::round(d[j]));
+            }
+            hi = round4<T>(d);
+            lo = round4<T>(rest);
+        }
+        *reinterpret_cast<u32x2 *>(out + (int64_t)(N + r) * 64) = lo;
+        *reinterpret_cast<u32x2 *>(out + (int64_t)r * 64) = hi;
+    } else {
+        *reinterpret_cast<u32x2 *>(out + (int64_t)(N + r) * 64) = hi;
+    }
+}
+
+// Hidden states in rows of whole units of 8 elements, `times` times over; but for `whole`, zeros in those that have no gradient, whatever they
+// hold.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, int32_t times, bool whole,
+                                                        Rows rows, uint16_t *y, int32_t y_ld) {
     const int32_t units = y_ld / 8;
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (k >= (int64_t)N * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
     u32x4 v = {0, 0, 0, 0};
-    if (!scaled || scaled[row] != 0.0f) {
+    if (whole || rows.grad(row) != 0.0f) {
         const uint16_t *p = x + row * x_ld + c;
         if (c + 8 <= D) {
             v = *reinterpret_cast<const u32x4_any *>(p);
@@ -203,7 +310,7 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64
             for (int j = 0; c + j < D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
         }
     }
-    *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = v;
+    for (int32_t i = 0; i < times; ++i) *reinterpret_cast<u32x4 *>(y + ((int64_t)i * N + row) * y_ld + c) = v;
 }
 
 // four results next to each other at any element alignment, the last of a row one by one
@@ -221,7 +328,7 @@ __device__ __forceinline__ void store4(uint16_t *row, int32_t c, int32_t n, f32x
 struct GradArgs {
     Operand A, B;  // A: m = hidden size; B: n = rows (grad_hidden) or tokens (grad_weight)
     int32_t n, D;  // extents of the result
-    int32_t k, k_split;
+    int32_t k, k_split, splits;
     int32_t tiles_m, tiles_n;
     const float *unscale;
     uint16_t *out;  // [n][out_ld]
@@ -236,43 +343,53 @@ template <typename T, typename S, bool DIRECT, bool B_COLUMNS>
 __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     using TileA = Tile<S::BM, S::kThreads, true, DIRECT>;
     using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true>;
-    __shared__ __attribute__((aligned(16))) char lds0[S::kLds], lds1[S::kLds];
-    int32_t tm, tn;
-    tile_of(blockIdx.x, gridDim.x, a.tiles_m, a.tiles_n, tm, tn);
-    const int32_t k0 = blockIdx.y * a.k_split, k1 = k0 + a.k_split < a.k ? k0 + a.k_split : a.k;
-    f32x4 acc[S::FM][S::FN];
-    multiply<T, S, TileA, TileB>(a.A, a.B, tm * S::BM, tn * S::BN, k0, k1, lds0, lds1, acc);
-
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int wm = wave / S::WN, wn = wave % S::WN;
-    const float unscale = *a.unscale;
-#pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int32_t n = tn * S::BN + wn * S::TN + 16 * j + (lane & 15);
-        if (n >= a.n) continue;
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int32_t c = tm * S::BM + wm * S::TM + 16 * i + 4 * (lane >> 4);
-            if (c >= a.D) continue;
-            if (a.sums) {
-                f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)blockIdx.y * a.n + n) * a.sums_ld + c);
-                *p = a.add ? *p + acc[i][j] : acc[i][j];
-            } else {
-                store4<T>(a.out + n * a.out_ld, c, a.D, acc[i][j] * unscale);
-            }
-        }
-    }
+    CFGZIP_STAGES(S, lds);
+    auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
+        const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = blockIdx.x + i * gridDim.x;
+        if (t >= total) return false;
+        tile_of(t, total, a.tiles_m, a.tiles_n * a.splits, tm, tn);
+        split = tn / a.tiles_n;
+        tn -= split * a.tiles_n;
+        return true;
+    };
+    auto work = [&](int32_t i, Work &w) CFGZIP_INLINE {
+        int32_t tm, tn, split;
+        if (!place(i, tm, tn, split)) return false;
+        const int32_t k0 = split * a.k_split;
+        w = Work{tm * S::BM, tn * S::BN, k0 / kStepK, a.k - k0 < a.k_split ? a.k - k0 : a.k_split};
+        return true;
+    };
+    auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
+        int32_t tm = 0, tn = 0, split = 0;
+        place(i, tm, tn, split);
+        const float unscale = *a.unscale;
+        each<S::FN>([&](auto j) CFGZIP_INLINE {
+            const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
+            if (n >= a.n) return;
+            each<S::FM>([&](auto i) CFGZIP_INLINE {
+                const int32_t c = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
+                if (c >= a.D) return;
+                if (a.sums) {
+                    f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
+                    *p = a.add ? *p + acc[i.value][j.value] : acc[i.value][j.value];
+                } else {
+                    store4<T>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale);
+                }
+            });
+        });
+    };
+    multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store);
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void finish_kernel(const float *sums, int32_t splits, int32_t n, int32_t D, int32_t sums_ld,
+__global__ __launch_bounds__(256) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
                                                      const float *unscale, uint16_t *out, int64_t out_ld) {
     const int32_t units = sums_ld / 4;
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (k >= (int64_t)n * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 4;
     f32x4 x = {0, 0, 0, 0};
-    for (int32_t s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4 *>(sums + ((int64_t)s * n + row) * sums_ld + c);
+    for (int32_t s = 0; s < count; ++s) x += *reinterpret_cast<const f32x4 *>(sums + ((int64_t)s * n + row) * sums_ld + c);
     store4<T>(out + row * out_ld, c, D, x * *unscale);
 }
 
@@ -294,8 +411,10 @@ int rows_of_tile(int32_t N) {
 int32_t columns_of_tile(int rows) { return rows == 16 ? 64 : rows == 64 ? 128 : 256; }
 
 struct Plan {
-    int rows;           // of a tile
-    int32_t rows_pad;   // N in whole tiles
+    int logits_rows;    // of a tile of logits
+    int32_t parts;      // 16-bit numbers that make up a value of dz
+    int rows;           // of a tile of dz
+    int32_t rows_pad;   // rows of dz in whole tiles
     int32_t d_pad;      // hidden size in units of 8
     int32_t piece;      // tokens of a piece of dz
     int32_t splits, k_split;
@@ -305,31 +424,32 @@ struct Plan {
 
 Plan plan_of(int32_t N, int32_t V, int32_t D) {
     Plan p{};
-    p.rows = rows_of_tile(N);
-    p.rows_pad = (int32_t)pad(N, p.rows);
+    p.logits_rows = rows_of_tile(N);
+    p.parts = N <= kFewRows ? 2 : 1;
+    p.rows = rows_of_tile(N * p.parts);
+    p.rows_pad = (int32_t)pad(N * p.parts, p.rows);
     p.d_pad = (int32_t)pad(D, 8);
     int64_t most = (int64_t)(kPieceBytes / 2 / p.rows_pad) / 256 * 256;
     if (most < kPieceLeast) most = kPieceLeast;
-    const int64_t pieces = ceil_div(V, most);
+    const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, most);
     p.piece = (int32_t)pad(ceil_div(V, pieces), 256);
     // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip
-    const int64_t tiles = ceil_div(D, columns_of_tile(p.rows)) * ceil_div(N, p.rows);
-    const int64_t at_a_time = p.rows == 256 ? 256 : p.rows == 128 ? 256 : p.rows == 64 ? 768 : 1024;
+    const int64_t tiles = ceil_div(D, columns_of_tile(p.rows)) * (p.rows_pad / p.rows);
+    const int64_t at_a_time = p.rows == 16 ? slots<Shape16>() : p.rows == 64 ? slots<Shape64>() : p.rows == 128 ? slots<Shape128>() : slots<Shape256>();
     int64_t best = 1;
     double best_use = 0;
-    for (int64_t s = 1; s <= 1024 && s * 256 <= p.piece; ++s) {
+    for (int64_t s = 1; s * kSplitLeast <= p.piece && tiles * s <= at_a_time * 2; ++s) {
         const int64_t rounds = ceil_div(tiles * s, at_a_time);
         const double use = (double)(tiles * s) / (double)(rounds * at_a_time);
-        if (use > best_use + 0.05) {
+        if (use > best_use * 1.05) {  // a further share of the sums costs a pass over them
             best_use = use;
             best = s;
         }
-        if (tiles * s >= at_a_time * 2) break;
     }
     p.k_split = (int32_t)pad(ceil_div(p.piece, best), kStepK);
-    p.splits = (int32_t)ceil_div(p.piece, p.k_split);
+    p.splits = (int32_t)ceil_div(V < p.piece ? V : p.piece, p.k_split);  // of the first piece; later ones add to them
     p.sums_ld = (int32_t)pad(D, 4);
-    p.direct_out = pieces == 1 && p.splits == 1;
+    p.direct_out = pieces == 1 && p.splits == 1 && p.parts == 1;
     return p;
 }
 
@@ -361,7 +481,7 @@ int check_call(const LossCall &c) {
         if (c.bits_kind == CFGZIP_BITS_CLASS && (!c.class_of_token || c.C <= 0 || !aligned_to(c.class_of_token, 4)))
             return CFGZIP_E_INVALID;
     }
-    if (c.V > 0x7FFFFC00 || c.N > 0x7FFFFC00) return CFGZIP_E_TOO_LARGE;
+    if (c.V > 0x7FFFFC00 || c.N > kMaxRows) return CFGZIP_E_TOO_LARGE;
     if (c.weight_stride >= kMaxStride || c.D >= kMaxStride - 8) return CFGZIP_E_TOO_LARGE;
     return CFGZIP_OK;
 }
@@ -382,8 +502,8 @@ int masks_of(const LossCall &c, Carver &ws, hipStream_t stream, Masks &m, bool l
 
 template <typename T, typename S, int WHAT>
 int launch_logits_of(const LogitsArgs &a, bool direct, hipStream_t stream) {
-    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n;
-    if (grid > 0x7FFFFFFF) return CFGZIP_E_TOO_LARGE;
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n, grid = work < slots<S>() ? work : slots<S>();
+    if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
     if (direct) hipLaunchKernelGGL((logits_kernel<T, S, true, WHAT>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
     else hipLaunchKernelGGL((logits_kernel<T, S, false, WHAT>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
     return check_launch();
@@ -397,35 +517,47 @@ int launch_logits(int rows, LogitsArgs a, int32_t tokens, bool direct, hipStream
         case 16: return launch_logits_of<T, Shape16, WHAT>(a, direct, stream);
         case 64: return launch_logits_of<T, Shape64, WHAT>(a, direct, stream);
         case 128: return launch_logits_of<T, Shape128, WHAT>(a, direct, stream);
-        default: return launch_logits_of<T, Shape256, WHAT>(a, direct, stream);
+        default:
+            if constexpr (WHAT == KEPT) return CFGZIP_E_INVALID;  // (not that few rows)
+            else return launch_logits_of<T, Shape256, WHAT>(a, direct, stream);
     }
 }
 
 template <typename T, typename S, bool DIRECT, bool B_COLUMNS>
-int launch_grad_of(GradArgs a, int32_t splits, hipStream_t stream) {
+int launch_grad_of(GradArgs a, hipStream_t stream) {
     a.tiles_m = (int32_t)ceil_div(a.D, S::BM);
     a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
-    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n;
-    if (grid > 0x7FFFFFFF) return CFGZIP_E_TOO_LARGE;
-    hipLaunchKernelGGL((grad_kernel<T, S, DIRECT, B_COLUMNS>), dim3((uint32_t)grid, splits), dim3(S::kThreads), 0, stream, a);
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = work < slots<S>() ? work : slots<S>();
+    if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
+    hipLaunchKernelGGL((grad_kernel<T, S, DIRECT, B_COLUMNS>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
     return check_launch();
 }
 
 template <typename T, bool DIRECT>
-int launch_grad_hidden(int rows, const GradArgs &a, int32_t splits, hipStream_t stream) {
+int launch_grad_hidden(int rows, const GradArgs &a, hipStream_t stream) {
     switch (rows) {
-        case 16: return launch_grad_of<T, Shape16, DIRECT, false>(a, splits, stream);
-        case 64: return launch_grad_of<T, Shape64, DIRECT, false>(a, splits, stream);
-        case 128: return launch_grad_of<T, Shape128, DIRECT, false>(a, splits, stream);
-        default: return launch_grad_of<T, Shape256, DIRECT, false>(a, splits, stream);
+        case 16: return launch_grad_of<T, Shape16, DIRECT, false>(a, stream);
+        case 64: return launch_grad_of<T, Shape64, DIRECT, false>(a, stream);
+        case 128: return launch_grad_of<T, Shape128, DIRECT, false>(a, stream);
+        default: return launch_grad_of<T, Shape256, DIRECT, false>(a, stream);
     }
 }
 
-template <typename T>
-int copy_rows(const LossCall &c, const float *scaled, uint16_t *y, int32_t y_ld, hipStream_t stream) {
+int copy_rows(const LossCall &c, int32_t times, bool whole, const Rows &rows, uint16_t *y, int32_t y_ld, hipStream_t stream) {
     const int64_t units = (int64_t)c.N * (y_ld / 8);
     hipLaunchKernelGGL(copy_rows_kernel, dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream,
-                       static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N, c.D, scaled, y, y_ld);
+                       static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N, c.D, times, whole, rows, y, y_ld);
+    return check_launch();
+}
+
+int join(const f32x2 *parts, int32_t count, const LossCall &c, const Masks &masks, const float *z_target, float *loss, float *lse,
+         f32x2 *whole, hipStream_t stream) {
+    if (c.N <= 64)
+        hipLaunchKernelGGL(join_kernel<1>, dim3(c.N), dim3(1024), 0, stream, parts, count, c.N, c.V, masks, c.target, z_target, loss, lse,
+                           whole);
+    else
+        hipLaunchKernelGGL(join_kernel<16>, dim3((uint32_t)ceil_div(c.N, 16)), dim3(1024), 0, stream, parts, count, c.N, c.V, masks,
+                           c.target, z_target, loss, lse, whole);
     return check_launch();
 }
 
@@ -445,18 +577,15 @@ int forward(const LossCall &c, float *loss, float *lse, Carver &ws, hipStream_t 
     uint16_t *copy = ws.take<uint16_t>((size_t)c.N * d_pad);
     if (!launch) return CFGZIP_OK;
     const bool as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.hidden_stride < kMaxStride;
-    if (!as_it_is) CFGZIP_TRY(copy_rows<T>(c, nullptr, copy, d_pad, stream));
-    a.W = Operand{static_cast<const uint16_t *>(c.weight), c.weight_stride, c.V, c.D};
-    a.H = as_it_is ? Operand{static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N, c.D}
-                   : Operand{copy, d_pad, c.N, d_pad};
+    if (!as_it_is) CFGZIP_TRY(copy_rows(c, 1, true, Rows{}, copy, d_pad, stream));
+    a.W = by_rows(static_cast<const uint16_t *>(c.weight), c.weight_stride, c.V);
+    a.H = as_it_is ? by_rows(static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N) : by_rows(copy, d_pad, c.N);
     a.V = c.V;
     a.N = c.N;
     a.D = c.D;
     a.target = c.target;
     CFGZIP_TRY((launch_logits<T, STATISTICS>(rows, a, c.V, whole_units(c.weight, c.weight_stride, c.D), stream)));
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)ceil_div(c.N, 16)), dim3(256), 0, stream, a.parts, parts, c.N, c.V, a.masks,
-                       c.target, a.z_target, loss, lse);
-    return check_launch();
+    return join(a.parts, parts, c, a.masks, a.z_target, loss, lse, nullptr, stream);
 }
 
 template <typename T>
@@ -465,23 +594,30 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     const Plan p = plan_of(c.N, c.V, c.D);
     Masks masks;
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
+    const bool few = p.parts == 2;
+    const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
     float *unscale = ws.take<float>(1);
-    float *scaled = ws.take<float>(c.N);
-    uint16_t *copy = ws.take<uint16_t>((size_t)c.N * p.d_pad);
+    float *scaled = few ? nullptr : ws.take<float>(c.N);
+    uint16_t *copy = ws.take<uint16_t>((size_t)rows_dz * p.d_pad);
     uint16_t *dz = ws.take<uint16_t>((size_t)p.rows_pad * p.piece);
-    float *sums = ws.take<float>((size_t)p.splits * c.N * p.sums_ld);
+    float *sums = ws.take<float>((size_t)p.splits * rows_dz * p.sums_ld);
+    float *z = few ? ws.take<float>((size_t)c.N * p.piece) : nullptr;
+    f32x2 *parts = few ? ws.take<f32x2>((size_t)count * c.N) : nullptr, *whole = few ? ws.take<f32x2>(c.N) : nullptr;
     if (!launch) return CFGZIP_OK;
-    hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, grad_loss, c.target, c.N, c.V, masks, scaled, unscale);
-    CFGZIP_TRY(check_launch());
-    CFGZIP_TRY(copy_rows<T>(c, scaled, copy, p.d_pad, stream));
+    const Rows rows{grad_loss, c.target, c.N, c.V, masks};
+    if (!few) {
+        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale);
+        CFGZIP_TRY(check_launch());
+    }
+    CFGZIP_TRY(copy_rows(c, p.parts, false, rows, copy, p.d_pad, stream));
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
     for (int64_t v0 = 0; v0 < c.V; v0 += p.piece) {
         const int32_t tokens = (int32_t)(c.V - v0 < p.piece ? c.V - v0 : p.piece);
-        const Operand W{weight + v0 * c.weight_stride, c.weight_stride, tokens, c.D};
+        const uint16_t *const first = weight + v0 * c.weight_stride;
         LogitsArgs a{};
-        a.W = W;
-        a.H = Operand{copy, p.d_pad, c.N, p.d_pad};
+        a.W = by_rows(first, c.weight_stride, tokens);
+        a.H = by_rows(copy, p.d_pad, c.N);
         a.V = c.V;
         a.N = c.N;
         a.D = c.D;
@@ -491,13 +627,25 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         a.lse = lse;
         a.scaled_grad = scaled;
         a.dz = dz;
-        a.dz_ld = p.piece;
-        CFGZIP_TRY((launch_logits<T, GRADIENT>(p.rows, a, tokens, direct, stream)));
+        a.dz_rows = p.rows_pad;
+        a.parts = parts;
+        a.z = z;
+        if (few) {
+            CFGZIP_TRY((launch_logits<T, KEPT>(p.logits_rows, a, tokens, direct, stream)));
+            CFGZIP_TRY(join(parts, count, c, masks, nullptr, nullptr, nullptr, whole, stream));
+            const int32_t blocks = (int32_t)(pad(tokens, 64) / 64);
+            const int64_t threads = (int64_t)blocks * (p.rows_pad - c.N) * 16;
+            hipLaunchKernelGGL((few_rows_dz_kernel<T>), dim3((uint32_t)ceil_div(threads, 256)), dim3(256), 0, stream, rows, z, blocks, whole,
+                               dz, p.rows_pad, unscale);
+            CFGZIP_TRY(check_launch());
+        } else {
+            CFGZIP_TRY((launch_logits<T, GRADIENT>(p.logits_rows, a, tokens, direct, stream)));
+        }
         if (grad_hidden) {
             GradArgs g{};
-            g.A = Operand{W.p, W.ld, c.D, tokens};  // by columns
-            g.B = Operand{dz, p.piece, p.rows_pad, (int32_t)pad(tokens, 8)};
-            g.n = c.N;
+            g.A = by_columns(first, c.weight_stride, c.D);
+            g.B = Operand{dz, 64, 64, (int64_t)p.rows_pad * 64, p.rows_pad};
+            g.n = rows_dz;
             g.D = c.D;
             g.k = tokens;
             g.k_split = p.k_split;
@@ -507,29 +655,30 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.sums = p.direct_out ? nullptr : sums;
             g.sums_ld = p.sums_ld;
             g.add = v0 > 0;
-            const int32_t splits = (int32_t)ceil_div(tokens, p.k_split);
-            CFGZIP_TRY(direct ? (launch_grad_hidden<T, true>(p.rows, g, splits, stream))
-                              : (launch_grad_hidden<T, false>(p.rows, g, splits, stream)));
+            g.splits = (int32_t)ceil_div(tokens, p.k_split);
+            CFGZIP_TRY(direct ? (launch_grad_hidden<T, true>(p.rows, g, stream))
+                              : (launch_grad_hidden<T, false>(p.rows, g, stream)));
         }
         if (grad_weight) {
             GradArgs g{};
-            g.A = Operand{copy, p.d_pad, p.d_pad, c.N};
-            g.B = Operand{dz, p.piece, p.piece, c.N};
+            g.A = by_columns(copy, p.d_pad, p.d_pad);
+            g.B = Operand{dz, 64, (int64_t)p.rows_pad * 64, kStepK * 64, p.piece};
             g.n = tokens;
             g.D = c.D;
-            g.k = c.N;
-            g.k_split = (int32_t)pad(c.N, kStepK);
+            g.k = rows_dz;
+            g.k_split = (int32_t)pad(rows_dz, kStepK);
+            g.splits = 1;
             g.unscale = unscale;
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
-            CFGZIP_TRY(c.D > 128 ? (launch_grad_of<T, Shape256, true, true>(g, 1, stream))
-                                 : (launch_grad_of<T, ShapeFlat, true, true>(g, 1, stream)));
+            CFGZIP_TRY(c.D > 128 ? (launch_grad_of<T, Shape256, true, true>(g, stream))
+                                 : (launch_grad_of<T, ShapeFlat, true, true>(g, stream)));
         }
     }
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
-        hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream, sums, p.splits, c.N, c.D,
-                           p.sums_ld, unscale, grad_hidden, gh_stride);
+        hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream, sums, p.splits * p.parts, c.N,
+                           c.D, p.sums_ld, unscale, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }
     return CFGZIP_OK;
@@ -541,7 +690,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
 using namespace cfgzip;
 
 extern "C" size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind) {
-    if (N <= 0 || V <= 0 || D <= 0 || N > 0x7FFFFC00 || V > 0x7FFFFC00 || D >= kMaxStride - 8 || !kind_ok(bits_kind)) return 0;
+    if (N <= 0 || V <= 0 || D <= 0 || N > kMaxRows || V > 0x7FFFFC00 || D >= kMaxStride - 8 || !kind_ok(bits_kind)) return 0;
     LossCall c{};
     c.N = N, c.V = V, c.D = D, c.bits_kind = bits_kind;
     Carver ws(nullptr);
@@ -550,7 +699,7 @@ extern "C" size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t
 }
 
 extern "C" size_t cfgzip_head_loss_grad_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind) {
-    if (N <= 0 || V <= 0 || D <= 0 || N > 0x7FFFFC00 || V > 0x7FFFFC00 || D >= kMaxStride - 8 || !kind_ok(bits_kind)) return 0;
+    if (N <= 0 || V <= 0 || D <= 0 || N > kMaxRows || V > 0x7FFFFC00 || D >= kMaxStride - 8 || !kind_ok(bits_kind)) return 0;
     LossCall c{};
     c.N = N, c.V = V, c.D = D, c.bits_kind = bits_kind;
     Carver ws(nullptr);

@@ -16,8 +16,6 @@ namespace cfgzip {
 namespace {
 
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_bytes __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint16_t u16_bytes __attribute__((aligned(1)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
@@ -430,6 +428,8 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a) {
 }
 
 // ---------------------------------------------------------------- many rows
+
+static __device__ const u32x4 kZeros = {0, 0, 0, 0};  // what lanes behind the end of a row load
 
 // Rows of UNITS units of 16 bytes of a step, to LDS directly; unit c of row r lies where the 16 lanes of a read spread over all banks
 template <int R, int THREADS, int UNITS>

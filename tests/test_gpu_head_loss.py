@@ -91,7 +91,7 @@ def _check(lib, N, V, D, dtype, mask, seed, pad=0, offset=0, w_pad=0):
 
 
 SIZES = [(1, 1, 1), (1, 5, 8), (2, 31, 7), (3, 33, 40), (16, 100, 64), (17, 257, 72), (40, 130, 128), (64, 300, 136), (65, 1000, 200),
-         (130, 515, 96), (257, 700, 264), (300, 2048, 65), (20, 3000, 1001), (500, 40, 520), (6, 9000, 328)]
+         (130, 515, 96), (257, 700, 264), (300, 2048, 65), (20, 3000, 1001), (500, 40, 520), (6, 9000, 328), (129, 5678, 72), (128, 2100, 80)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
