@@ -109,13 +109,18 @@ struct Operand {
 constexpr int kStepK = 64;
 constexpr int64_t kMaxStride = 1 << 22;
 
-inline Operand by_rows(const uint16_t *p, int64_t ld, int32_t rows) { return Operand{p, ld, 64, kStepK, rows}; }
-inline Operand by_columns(const uint16_t *p, int64_t ld, int32_t columns) { return Operand{p, ld, 64, kStepK * ld, columns}; }
+__host__ __device__ inline Operand by_rows(const uint16_t *p, int64_t ld, int32_t rows) { return Operand{p, ld, 64, kStepK, rows}; }
+__host__ __device__ inline Operand by_columns(const uint16_t *p, int64_t ld, int32_t columns) { return Operand{p, ld, 64, kStepK * ld, columns}; }
 
 // R: the tile's extent in m or n.  COLUMNS: m (n) next to m in memory.  DIRECT: the base and the rows of memory lie at multiples
 // of 16 bytes and hold whole units of 8 elements; then lanes load to LDS directly, else through registers, the units at the end
 // of a row element by element.
-template <int R, int THREADS, bool COLUMNS, bool DIRECT>
+// END: what a tile holds where k has ended within a step.  ZERO: zeros.  ANY: something that is there and finite if the operand is, for
+// the other operand holds zeros there.  PADDED: memory itself goes on with zeros to the end of the step.  (Zeros are put in place
+// behind the loads to LDS, which costs two waits for memory a tile: 5 us of 42 for 777 x 50,003 x 1,000.)
+enum : int { ZERO = 0, ANY = 1, PADDED = 2 };
+
+template <int R, int THREADS, bool COLUMNS, bool DIRECT, int END>
 struct Tile {
     static constexpr bool kDirect = DIRECT;
     static constexpr int kUnits = R * kStepK / 8;
@@ -146,9 +151,9 @@ struct Tile {
         // rows (units of a column-major row) behind the end load the last one; what comes of them is not stored
         if (COLUMNS) {
             if (DIRECT && c * 8 >= rows_left) c = rows_left / 8 - 1;
-            return (uint32_t)(r * ld + (c >> 3) * block + (c & 7) * 8) * 2u;
+            return ((uint32_t)r * (uint32_t)ld + (uint32_t)(c >> 3) * (uint32_t)block + (c & 7) * 8) * 2u;
         }
-        return (uint32_t)((r < rows_left ? r : rows_left - 1) * ld + c * 8) * 2u;
+        return ((uint32_t)(r < rows_left ? r : rows_left - 1) * (uint32_t)ld + c * 8) * 2u;
     }
 
     // the tile from row0 (unit-aligned column row0) on, k from step0 steps on
@@ -181,17 +186,24 @@ struct Tile {
     }
 
     // Loads to LDS are not conditional, so that nothing branches among the products: where not all of a step's k are there (`whole`
-    // of them) they fetch the tile's first unit, and commit() puts what belongs there in its place.
-    __device__ __forceinline__ void not_whole() {
+    // of them) they fetch units that are, and commit() puts what belongs there in its place.
+    __device__ __forceinline__ void not_whole(int whole) {
         if constexpr (DIRECT) {
+            if (END == PADDED && whole > 0) return;
+            const int thread = afresh(threadIdx.x);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) at[i] = 0;
+            for (int i = 0; i < kPer; ++i) {
+                int r, c;
+                place(i * THREADS + thread, r, c);
+                at[i] = END != ANY ? 0 : COLUMNS ? offset(r < whole ? r : 0, c) : offset(r, c * 8 < whole ? c : 0);
+            }
         }
     }
     template <int I>
     __device__ __forceinline__ void load_one(lds_char *lds, int whole) {
         if constexpr (DIRECT) {
-            __builtin_amdgcn_global_load_lds((global_void *)(reinterpret_cast<const char *>(base) + at[I]),
+            const uint32_t from = COLUMNS ? at[I] : (uint32_t)afresh((int)at[I]);  // (else some are kept in 64 bits)
+            __builtin_amdgcn_global_load_lds((global_void *)(reinterpret_cast<const char *>(base) + from),
                                              (lds_void *)(lds + (I * THREADS * 16 + wave_at)), 16, 0, 0);
         } else {
             int r, c;
@@ -202,7 +214,7 @@ struct Tile {
     __device__ __forceinline__ void commit(lds_char *lds, int whole) {
         typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
         if constexpr (DIRECT) {
-            if (whole == kStepK) return;
+            if (END == ANY || whole == kStepK || (END == PADDED && whole > 0)) return;
             __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): what the loads to LDS left is replaced
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -277,10 +289,13 @@ struct Fragments {
         else a[Q - S::FN] = TileA::fragment(lds.a, wm * S::TM, Q - S::FN, kk, lane);
     }
     // acc[i][j][r]: lane l has m = 16 i + 4 (l >> 4) + r, n = 16 j + (l & 15) of its wave's part; group P of the FM * FN products
-    template <int P>
-    __device__ __forceinline__ void multiply_some(f32x4 (&acc)[S::FM][S::FN]) const {
+    template <int P, int BYTE, typename X>
+    __device__ __forceinline__ void multiply_some(f32x4 (&acc)[S::FM][S::FN], const X &scales) const {
         constexpr int i = P * S::kGroup / S::FN, j = P * S::kGroup % S::FN;
-        if constexpr (S::kGroup == 4)
+        if constexpr (X::kScaled)
+            T::template mma4<BYTE>(a[i], b[j], b[j + 1], b[j + 2], b[j + 3], acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3],
+                                   scales.a[i], scales.b[j], scales.b[j + 1], scales.b[j + 2], scales.b[j + 3]);
+        else if constexpr (S::kGroup == 4)
             T::mma4(a[i], b[j], b[j + 1], b[j + 2], b[j + 3], acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]);
         else acc[i][j] = T::mma(a[i], b[j], acc[i][j]);
     }
@@ -303,12 +318,12 @@ constexpr int from(int p, int count, int groups) { return p >= groups ? count : 
 
 // The products of `now`; the fragments `next` are read in three quarters of their time, and LOADS loads begun and then `last`, evenly
 // among them.  The order is the one written here: the compiler's own gathers the reads, and the matrix cores wait.
-template <typename S, int LOADS, typename F, typename L, typename M>
+template <typename S, int LOADS, int BYTE, typename F, typename L, typename M, typename X>
 __device__ __forceinline__ void multiply_and_read(const F &now, F &next, const Stage &lds, int wm, int wn, int kk, int lane,
-                                                  f32x4 (&acc)[S::FM][S::FN], L &&load_one, M &&last) {
+                                                  f32x4 (&acc)[S::FM][S::FN], L &&load_one, M &&last, const X &scales) {
     constexpr int kGroups = S::FM * S::FN / S::kGroup, kFragments = S::FM + S::FN, kLast = kGroups * 3 / 4 ? kGroups * 3 / 4 : 1;
     each<kGroups>([&](auto p) CFGZIP_INLINE {
-        now.template multiply_some<p.value>(acc);
+        now.template multiply_some<p.value, BYTE>(acc, scales);
         constexpr int q0 = from(p.value, kFragments, kLast), q1 = from(p.value + 1, kFragments, kLast);
         each<q1 - q0>([&](auto q) CFGZIP_INLINE { next.template read_one<q0 + q.value>(lds, wm, wn, kk, lane); });
         constexpr int l0 = from(p.value, LOADS + 1, kGroups), l1 = from(p.value + 1, LOADS + 1, kGroups);
@@ -336,10 +351,23 @@ struct Work {
     int32_t m0, n0, step0, k;  // k elements from step0 steps on
 };
 
+// Scales of what is multiplied, for operands that have them: those of two steps at a time (kStages of them), kept by the lane that has
+// the fragment.  begin(w) asks memory for a tile's first ones, ask() for those of the next two steps, put() leaves them in LDS, take()
+// fetches the lane's own from there.  With scales a workgroup has one tile (the registers do not suffice for a next one's beginning).
+struct NoScales {
+    static constexpr bool kScaled = false;
+    __device__ void begin(const Work &) {}
+    __device__ void ask() {}
+    __device__ void put() {}
+    __device__ void take(int, int, int) {}
+};
+
 // Makes tile after tile: work(i, Work &) says whether there is an i-th one and which, store(i, acc, ..) takes its sums.  While
 // the sums of one are stored the first steps of the next are on their way into LDS.
-template <typename T, typename S, typename TileA, typename TileB, typename W, typename E>
-__device__ __forceinline__ void multiply(const Operand &A, const Operand &B, const Stage (&lds)[4], W &&work, E &&store) {
+template <typename T, typename S, typename TileA, typename TileB, typename W, typename E, typename X>
+__device__ __forceinline__ void multiply(const Operand &A, const Operand &B, const Stage (&lds)[4], W &&work, E &&store, X &&scales) {
+    constexpr bool kScaled = std::remove_reference_t<X>::kScaled;
+    static_assert(!kScaled || S::kStages == 2, "scales of two steps at a time");
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int wm = wave / S::WN, wn = wave % S::WN;
     constexpr int kStages = S::kStages, kLoads = TileA::kPer + TileB::kPer;
@@ -354,8 +382,8 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, con
         whole = kStepK;
         if (k_left < kStepK) {
             whole = k_left > 0 ? k_left : 0;
-            ta.not_whole();
-            tb.not_whole();
+            ta.not_whole(whole);
+            tb.not_whole(whole);
         }
     };
     auto advance = [&]() CFGZIP_INLINE {
@@ -389,7 +417,12 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, con
         advance();
         if constexpr (s.value + 1 < kStages) commit(lds[s.value]);
     });
+    if constexpr (kScaled) {
+        scales.begin(w);
+        scales.put();
+    }
     wait_for_loads<(kStages - 1) * kToLds>();
+    if constexpr (kScaled) scales.take(wm, wn, lane);
     Fragments<T, S, TileA, TileB> f0, f1;
     const auto no_load = [](auto) CFGZIP_INLINE {};
     const auto nothing = []() CFGZIP_INLINE {};
@@ -411,17 +444,21 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, con
         do {
             each<kStages>([&](auto s) CFGZIP_INLINE {
                 const Stage &here = lds[s.value], &next = lds[(s.value + 1) % kStages];
-                multiply_and_read<S, 0>(f0, f1, here, wm, wn, 1, lane, acc, no_load, nothing);
+                multiply_and_read<S, 0, 2 * s.value>(f0, f1, here, wm, wn, 1, lane, acc, no_load, nothing, scales);
                 commit(lds[(s.value + kStages - 1) % kStages]);
+                if constexpr (kScaled && s.value == 1) scales.put();
                 wait_for_loads<(kStages - 2) * kToLds>();
                 if constexpr (s.value == 0) {
-                    if (left == 1) {  // from here on it is the next tile's steps that are loaded
+                    if constexpr (kScaled) {
+                        scales.ask();
+                    } else if (left == 1) {  // from here on it is the next tile's steps that are loaded
                         more = work(tile + 1, w);
                         if (more) start();
                     }
                 }
-                multiply_and_read<S, kLoads>(f1, f0, next, wm, wn, 0, lane, acc, load_into(here), advance);
+                multiply_and_read<S, kLoads, 2 * s.value + 1>(f1, f0, next, wm, wn, 0, lane, acc, load_into(here), advance, scales);
             });
+            if constexpr (kScaled) scales.take(wm, wn, lane);
         } while (--left > 0);
         settle<S>(acc);
         store(tile, acc, wm, wn, afresh(lane));

@@ -27,6 +27,15 @@ constexpr int64_t slots() {
     return 256 * (160 * 1024 / (S::kStages * S::kLds));
 }
 
+// What a product's tiles take, in microseconds: rounds of as many as are at work at a time, of so many steps each and a beginning and an
+// end.
+template <typename S>
+double time_of(int64_t m, int64_t n, int64_t steps) {
+    const double step = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : S::BM * S::BN == 8192 ? 0.6 : 0.35;
+    const double ends = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.0 : 4.0;
+    return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * step + ends);
+}
+
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time: the size of the last-level cache
 // Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum instead of lse, which
 // large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
@@ -66,8 +75,8 @@ enum : int { STATISTICS = 0, KEPT = 1, GRADIENT = 2 };
 
 template <typename T, typename S, bool DIRECT, int WHAT>
 __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
-    using TileA = Tile<S::BM, S::kThreads, false, DIRECT>;
-    using TileB = Tile<S::BN, S::kThreads, false, true>;
+    using TileA = Tile<S::BM, S::kThreads, false, DIRECT, ANY>;
+    using TileB = Tile<S::BN, S::kThreads, false, true, PADDED>;
     CFGZIP_STAGES(S, lds);
     auto work = [&](int32_t i, Work &w) CFGZIP_INLINE {
         const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n, t = blockIdx.x + i * gridDim.x;
@@ -84,17 +93,37 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
         const int32_t first = tm * S::BM + wm * S::TM;  // in the piece
         const int32_t v_first = a.v0 + first;
         const bool masked = a.masks.bits || v_first + S::TM > a.V;
+        // What belongs to the rows is asked for before the first of it is used: a load from memory takes as long as hundreds of
+        // the elements' instructions (with a wait for each row in turn a tile of 777 x 50,003 x 1,000 took 43 us, 25 of them products).
+        constexpr int kWords = (S::TM + 31) / 32;
+        const int32_t k_first = v_first >> 5;
+        uint32_t words[S::FN][kWords];
+        int32_t targets[S::FN];
+        float shifts[S::FN], grads[S::FN];
+        each<S::FN>([&](auto j) CFGZIP_INLINE {
+            const int32_t row = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15), at = row < a.N ? row : a.N - 1;
+            targets[j.value] = a.target[at];
+            if constexpr (WHAT == GRADIENT) {
+                grads[j.value] = a.scaled_grad[at];
+                shifts[j.value] = a.lse[at];
+            }
+            each<kWords>([&](auto w) CFGZIP_INLINE { words[j.value][w.value] = ~0u; });
+            if (a.masks.bits) {
+                const int32_t *const bits = a.masks.bits + at * a.masks.words;
+                each<kWords>([&](auto w) CFGZIP_INLINE {  // (what lies behind the last word is cut off below)
+                    const int64_t k = k_first + w.value < a.masks.words ? k_first + w.value : a.masks.words - 1;
+                    words[j.value][w.value] = (uint32_t)bits[k];
+                });
+            }
+        });
         each<S::FN>([&](auto jj) CFGZIP_INLINE {
             constexpr int j = jj.value;
             const int32_t row = tn * S::BN + wn * S::TN + 16 * j + (lane & 15);
             const bool in = row < a.N;
-            const int32_t at = in ? row : a.N - 1;
             if (masked) {  // what a row does not admit becomes -inf, whatever it was
-                each<(S::TM + 31) / 32>([&](auto ww) CFGZIP_INLINE {
-                    const int64_t k = (v_first >> 5) + ww.value;
-                    uint32_t word = 0;
-                    if (k < a.masks.words) word = a.masks.bits ? (uint32_t)a.masks.bits[at * a.masks.words + k] : ~0u;
-                    const int32_t left = a.V - (int32_t)k * 32;  // tokens from the word's first on
+                each<kWords>([&](auto ww) CFGZIP_INLINE {
+                    uint32_t word = words[j][ww.value];
+                    const int64_t left = a.V - (int64_t)(k_first + ww.value) * 32;  // tokens from the word's first on
                     if (left < 32) word &= left > 0 ? (1u << left) - 1u : 0u;
                     each<(S::TM < 32 ? S::FM : 2)>([&](auto ii) CFGZIP_INLINE {
                         constexpr int i = ww.value * 2 + ii.value;
@@ -107,7 +136,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
                     });
                 });
             }
-            const int32_t mark = a.target[at] - v_first - 4 * g;  // the target is element mark % 16 of fragment mark / 16
+            const int32_t mark = targets[j] - v_first - 4 * g;  // the target is element mark % 16 of fragment mark / 16
             const bool marked = __builtin_amdgcn_ballot_w64(in && mark >= 0 && mark < S::TM) != 0;  // seldom
             if constexpr (WHAT != GRADIENT) {
                 float most = -kInf;
@@ -142,9 +171,9 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
                     });
                 }
             } else {
-                const float grad = in ? a.scaled_grad[at] : 0.0f;
+                const float grad = in ? grads[j] : 0.0f;
                 // rows without a gradient have hidden states of 0 here, so logits of 0 or -inf, and exp(-inf) * 0
-                const float shift = grad != 0.0f ? a.lse[at] : kInf;
+                const float shift = grad != 0.0f ? shifts[j] : kInf;
                 uint16_t *const out = a.dz + row * 64 + (first >> 6) * (a.dz_rows * 64) + (first & 63) + 4 * g;
                 each<S::FM>([&](auto i) CFGZIP_INLINE {
                     f32x4 d;
@@ -161,7 +190,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
             }
         });
     };
-    multiply<T, S, TileA, TileB>(a.W, a.H, lds, work, store);
+    multiply<T, S, TileA, TileB>(a.W, a.H, lds, work, store, NoScales{});
 }
 
 // Joins the parts of a row: lse and loss, or (`whole` given) its maximum and sum.  A workgroup has ROWS rows and splits the parts over the other lanes; a lane asks for
@@ -293,15 +322,19 @@ __global__ __launch_bounds__(256) void few_rows_dz_kernel(Rows rows, const float
     }
 }
 
-// Hidden states in rows of whole units of 8 elements, `times` times over; but for `whole`, zeros in those that have no gradient, whatever they
-// hold.
-__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, int32_t times, bool whole,
-                                                        Rows rows, uint16_t *y, int32_t y_ld) {
+// Hidden states in rows of whole steps of 64 elements (zeros behind D), `times` times over, and rows of zeros behind them up to `all`;
+// but for `whole`, zeros in those that have no gradient, whatever they hold.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, int32_t times, int32_t all,
+                                                        bool whole, Rows rows, uint16_t *y, int32_t y_ld) {
     const int32_t units = y_ld / 8;
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (k >= (int64_t)N * units) return;
+    if (k >= (int64_t)(N + all - N * times) * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
     u32x4 v = {0, 0, 0, 0};
+    if (row >= N) {
+        *reinterpret_cast<u32x4 *>(y + ((int64_t)N * (times - 1) + row) * y_ld + c) = v;
+        return;
+    }
     if (whole || rows.grad(row) != 0.0f) {
         const uint16_t *p = x + row * x_ld + c;
         if (c + 8 <= D) {
@@ -341,8 +374,9 @@ struct GradArgs {
 // grad_hidden: A = weight by columns, B = dz by rows.  grad_weight: A = hidden, B = dz, both by columns.
 template <typename T, typename S, bool DIRECT, bool B_COLUMNS>
 __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
-    using TileA = Tile<S::BM, S::kThreads, true, DIRECT>;
-    using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true>;
+    // (weights end where the vocabulary does; hidden states and dz go on with zeros)
+    using TileA = Tile<S::BM, S::kThreads, true, DIRECT, B_COLUMNS ? PADDED : ZERO>;
+    using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true, PADDED>;
     CFGZIP_STAGES(S, lds);
     auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
         const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = blockIdx.x + i * gridDim.x;
@@ -378,19 +412,28 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
             });
         });
     };
-    multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store);
+    multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
+__global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
                                                      const float *unscale, uint16_t *out, int64_t out_ld) {
     const int32_t units = sums_ld / 4;
-    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t k = (int64_t)blockIdx.x * kWave + threadIdx.x;
     if (k >= (int64_t)n * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 4;
+    const float factor = *unscale;
+    const float *p = sums + (int64_t)row * sums_ld + c;
+    const int64_t step = (int64_t)n * sums_ld;
     f32x4 x = {0, 0, 0, 0};
-    for (int32_t s = 0; s < count; ++s) x += *reinterpret_cast<const f32x4 *>(sums + ((int64_t)s * n + row) * sums_ld + c);
-    store4<T>(out + row * out_ld, c, D, x * *unscale);
+    for (int32_t s = 0; s < count; s += 16) {  // 16 loads on their way at a time: with each waited for 32 sums took 9.4 us
+        f32x4 y[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = s + i < count ? *reinterpret_cast<const f32x4 *>(p + (s + i) * step) : f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x += y[i];
+    }
+    store4<T>(out + row * out_ld, c, D, x * factor);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
@@ -414,8 +457,8 @@ struct Plan {
     int logits_rows;    // of a tile of logits
     int32_t parts;      // 16-bit numbers that make up a value of dz
     int rows;           // of a tile of dz
-    int32_t rows_pad;   // rows of dz in whole tiles
-    int32_t d_pad;      // hidden size in units of 8
+    int32_t rows_pad;   // rows of dz in whole tiles and steps
+    int32_t d_pad;      // hidden size in whole steps
     int32_t piece;      // tokens of a piece of dz
     int32_t splits, k_split;
     int32_t sums_ld;
@@ -427,14 +470,14 @@ Plan plan_of(int32_t N, int32_t V, int32_t D) {
     p.logits_rows = rows_of_tile(N);
     p.parts = N <= kFewRows ? 2 : 1;
     p.rows = rows_of_tile(N * p.parts);
-    p.rows_pad = (int32_t)pad(N * p.parts, p.rows);
-    p.d_pad = (int32_t)pad(D, 8);
+    p.rows_pad = (int32_t)pad(N * p.parts, p.rows > kStepK ? p.rows : kStepK);  // (zeros behind N: steps of grad_weight's sum)
+    p.d_pad = (int32_t)pad(D, kStepK);
     int64_t most = (int64_t)(kPieceBytes / 2 / p.rows_pad) / 256 * 256;
     if (most < kPieceLeast) most = kPieceLeast;
     const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, most);
     p.piece = (int32_t)pad(ceil_div(V, pieces), 256);
     // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip
-    const int64_t tiles = ceil_div(D, columns_of_tile(p.rows)) * (p.rows_pad / p.rows);
+    const int64_t tiles = ceil_div(D, columns_of_tile(p.rows)) * ceil_div(N * p.parts, p.rows);
     const int64_t at_a_time = p.rows == 16 ? slots<Shape16>() : p.rows == 64 ? slots<Shape64>() : p.rows == 128 ? slots<Shape128>() : slots<Shape256>();
     int64_t best = 1;
     double best_use = 0;
@@ -543,10 +586,21 @@ int launch_grad_hidden(int rows, const GradArgs &a, hipStream_t stream) {
     }
 }
 
-int copy_rows(const LossCall &c, int32_t times, bool whole, const Rows &rows, uint16_t *y, int32_t y_ld, hipStream_t stream) {
-    const int64_t units = (int64_t)c.N * (y_ld / 8);
+template <typename T>
+int launch_grad_weight(const GradArgs &a, hipStream_t stream) {
+    const int32_t steps = (int32_t)ceil_div(a.k, kStepK);
+    const double large = time_of<Shape256>(a.D, a.n, steps), middle = time_of<Shape128>(a.D, a.n, steps),
+                 flat = time_of<ShapeFlat>(a.D, a.n, steps), small = time_of<Shape64>(a.D, a.n, steps);
+    if (large <= middle && large <= flat && large <= small) return launch_grad_of<T, Shape256, true, true>(a, stream);
+    if (flat <= middle && flat <= small) return launch_grad_of<T, ShapeFlat, true, true>(a, stream);
+    return middle <= small ? launch_grad_of<T, Shape128, true, true>(a, stream) : launch_grad_of<T, Shape64, true, true>(a, stream);
+}
+
+int copy_rows(const LossCall &c, int32_t times, int32_t all, bool whole, const Rows &rows, uint16_t *y, int32_t y_ld,
+              hipStream_t stream) {
+    const int64_t units = (int64_t)(c.N + all - c.N * times) * (y_ld / 8);
     hipLaunchKernelGGL(copy_rows_kernel, dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream,
-                       static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N, c.D, times, whole, rows, y, y_ld);
+                       static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N, c.D, times, all, whole, rows, y, y_ld);
     return check_launch();
 }
 
@@ -569,15 +623,15 @@ int32_t part_count(int rows, int32_t V) {  // one from each wave along the token
 template <typename T>
 int forward(const LossCall &c, float *loss, float *lse, Carver &ws, hipStream_t stream, bool launch) {
     const int rows = rows_of_tile(c.N);
-    const int32_t d_pad = (int32_t)pad(c.D, 8), parts = part_count(rows, c.V);
+    const int32_t d_pad = (int32_t)pad(c.D, kStepK), parts = part_count(rows, c.V);
     LogitsArgs a{};
     CFGZIP_TRY(masks_of(c, ws, stream, a.masks, launch));
     a.parts = ws.take<f32x2>((size_t)parts * c.N);
     a.z_target = ws.take<float>(c.N);
     uint16_t *copy = ws.take<uint16_t>((size_t)c.N * d_pad);
     if (!launch) return CFGZIP_OK;
-    const bool as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.hidden_stride < kMaxStride;
-    if (!as_it_is) CFGZIP_TRY(copy_rows(c, 1, true, Rows{}, copy, d_pad, stream));
+    const bool as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.D % kStepK == 0 && c.hidden_stride < kMaxStride;
+    if (!as_it_is) CFGZIP_TRY(copy_rows(c, 1, c.N, true, Rows{}, copy, d_pad, stream));
     a.W = by_rows(static_cast<const uint16_t *>(c.weight), c.weight_stride, c.V);
     a.H = as_it_is ? by_rows(static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.N) : by_rows(copy, d_pad, c.N);
     a.V = c.V;
@@ -598,7 +652,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
     float *unscale = ws.take<float>(1);
     float *scaled = few ? nullptr : ws.take<float>(c.N);
-    uint16_t *copy = ws.take<uint16_t>((size_t)rows_dz * p.d_pad);
+    const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK);
+    uint16_t *copy = ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad);
     uint16_t *dz = ws.take<uint16_t>((size_t)p.rows_pad * p.piece);
     float *sums = ws.take<float>((size_t)p.splits * rows_dz * p.sums_ld);
     float *z = few ? ws.take<float>((size_t)c.N * p.piece) : nullptr;
@@ -609,7 +664,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale);
         CFGZIP_TRY(check_launch());
     }
-    CFGZIP_TRY(copy_rows(c, p.parts, false, rows, copy, p.d_pad, stream));
+    CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
     for (int64_t v0 = 0; v0 < c.V; v0 += p.piece) {
@@ -671,13 +726,12 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.unscale = unscale;
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
-            CFGZIP_TRY(c.D > 128 ? (launch_grad_of<T, Shape256, true, true>(g, stream))
-                                 : (launch_grad_of<T, ShapeFlat, true, true>(g, stream)));
+            CFGZIP_TRY(launch_grad_weight<T>(g, stream));
         }
     }
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
-        hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream, sums, p.splits * p.parts, c.N,
+        hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, sums, p.splits * p.parts, c.N,
                            c.D, p.sums_ld, unscale, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }

@@ -207,13 +207,14 @@ __device__ __forceinline__ f32x4 multiply4(u32x4 a, u32x4 b, f32x4 c, uint32_t s
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)scale_a, 0, (int)scale_b);
 }
 
-// logits of four tokens from v on in row b; bit r of ok: token v + r is admitted
+// logits of four tokens (WHOLE: all of them there) from v on in row b; bit r of ok: token v + r is admitted
+template <bool WHOLE, bool F32>
 __device__ __forceinline__ void store_logits(const Logits &o, int32_t b, int32_t v, int32_t V, f32x4 z, uint32_t ok) {
-    const int32_t left = V - v;
+    const int32_t left = WHOLE ? 4 : V - v;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
         if (!(ok >> r & 1)) z[r] = -kInf;
-    if (o.f32) {
+    if (F32) {
         float *p = static_cast<float *>(o.p) + b * o.ld + v;
         if (left >= 4) {
             *reinterpret_cast<f32x4_any *>(p) = z;
@@ -420,7 +421,8 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a) {
                 const int32_t b = f * 16 + m;
                 if (b >= B) continue;
                 const uint32_t four = (oks[0] >> b & 1) | (oks[1] >> b & 1) << 1 | (oks[2] >> b & 1) << 2 | (oks[3] >> b & 1) << 3;
-                store_logits(a.out, b, tile * 16 + 4 * g, V, acc[f], four);
+                if (a.out.f32) store_logits<false, true>(a.out, b, tile * 16 + 4 * g, V, acc[f], four);
+                else store_logits<false, false>(a.out, b, tile * 16 + 4 * g, V, acc[f], four);
             }
         }
         ok = ok_next;
@@ -476,6 +478,7 @@ struct ManyArgs {
     int64_t x_part_bytes;  // from one part to the next
     int32_t parts;         // 2 for fp16: bf16 and rest
     int32_t x_units;       // of 16 bytes in a row
+    int32_t part_steps;    // of 128 values in a part's row, where those are whole pairs of steps
     const uint8_t *x_scales;
     Logits out;
     const int32_t *bits;  // over tokens, or null
@@ -488,21 +491,40 @@ __device__ __forceinline__ void store_tile(const ManyArgs &a, int32_t tm, int32_
                                            const f32x4 (&acc)[S::FM][S::FN]) {
     const int g = lane >> 4;
     const int32_t first = tm * S::BM + wm * S::TM;
-#pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int32_t b = tn * S::BN + wn * S::TN + 16 * j + (lane & 15);
-        if (b >= a.out.B) continue;
-        uint32_t words[(S::TM + 31) / 32];
-#pragma unroll
-        for (int w = 0; w < (S::TM + 31) / 32; ++w) {
-            const int64_t k = (first >> 5) + w;
-            words[w] = !a.bits ? 0xFFFFFFFFu : k < a.words ? (uint32_t)a.bits[b * a.words + k] : 0u;
+    constexpr int kWords = (S::TM + 31) / 32;
+    const int32_t b0 = tn * S::BN + wn * S::TN + (lane & 15);
+    uint32_t words[S::FN][kWords];  // all of them are asked for before the first is used
+    each<S::FN>([&](auto j) CFGZIP_INLINE {
+        each<kWords>([&](auto w) CFGZIP_INLINE { words[j.value][w.value] = ~0u; });
+        if (a.bits) {
+            const int32_t b = b0 + 16 * j.value;
+            const int32_t *const bits = a.bits + (b < a.out.B ? b : a.out.B - 1) * a.words;
+            each<kWords>([&](auto w) CFGZIP_INLINE {  // (tokens behind the last word are not stored)
+                const int64_t k = (first >> 5) + w.value < a.words ? (first >> 5) + w.value : a.words - 1;
+                words[j.value][w.value] = (uint32_t)bits[k];
+            });
         }
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int32_t v = first + 16 * i + 4 * g;
-            if (v < a.w.V) store_logits(a.out, b, v, a.w.V, acc[i][j], words[i / 2] >> (v & 31));
-        }
+    });
+    auto store = [&](auto whole, auto f32) CFGZIP_INLINE {
+        each<S::FN>([&](auto j) CFGZIP_INLINE {
+            const int32_t b = b0 + 16 * j.value;
+            if (b >= a.out.B) return;
+            each<S::FM>([&](auto i) CFGZIP_INLINE {
+                const int32_t v = first + 16 * i.value + 4 * g;
+                if (whole.value || v < a.w.V)
+                    store_logits<whole.value, f32.value>(a.out, b, v, a.w.V, acc[i.value][j.value], words[j.value][i.value / 2] >> (v & 31));
+            });
+        });
+    };
+    // (asked once a tile and not once for every four logits)
+    const std::true_type yes;
+    const std::false_type no;
+    if (first + S::TM > a.w.V) {
+        if (a.out.f32) store(no, yes);
+        else store(no, no);
+    } else {
+        if (a.out.f32) store(yes, yes);
+        else store(yes, no);
     }
 }
 
@@ -681,7 +703,337 @@ __global__ __launch_bounds__(S::kThreads) void many_rows4_kernel(ManyArgs a) {
     store_tile<S>(a, tm, tn, wm, wn, lane, acc);
 }
 
-// Hidden states as bf16 in rows of whole blocks, zeros behind K; of fp16 the rests behind all rows
+// 16-bit hidden states, many rows: tiles of 256 x 256 by four waves.  A step has 128 k: lane (r, g) of a fragment has block g of its
+// token, 32 weights, as four fragments of eight that become bf16 while the products of the row before are at work, and the hidden
+// states of the same k.  Hidden states lie in whole pairs of steps, zeros behind K; those of fp16 have a row's rests behind
+// its first numbers, and the weights are gone through twice.  Products a wave: 256 a step; out of LDS 8 KB of codes and 32 of hidden
+// states.
+using Large16 = Shape<256, 256, 2, 2, 2>;
+constexpr int32_t kPairK = 256;
+
+// four products with one fragment of weights, while the next one's `to` is made of eight codes
+__device__ __forceinline__ void mma4_and_convert(u32x4 a, u32x4 b0, u32x4 b1, u32x4 b2, u32x4 b3, f32x4 &c0, f32x4 &c1, f32x4 &c2, f32x4 &c3,
+                                                 u32x4 &to, uint32_t codes, float scale) {
+    uint32_t t0, t1, t2, t3;
+    asm volatile(
+        "s_nop 1\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %8, %9, %0\n\t"
+        "v_cvt_scalef32_pk_bf16_fp4 %4, %13, %14\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %8, %10, %1\n\t"
+        "v_cvt_scalef32_pk_bf16_fp4 %5, %13, %14 op_sel:[1,0,0]\n\t"
+        "v_mfma_f32_16x16x32_bf16 %2, %8, %11, %2\n\t"
+        "v_cvt_scalef32_pk_bf16_fp4 %6, %13, %14 op_sel:[0,1,0]\n\t"
+        "v_mfma_f32_16x16x32_bf16 %3, %8, %12, %3\n\t"
+        "v_cvt_scalef32_pk_bf16_fp4 %7, %13, %14 op_sel:[1,1,0]"
+        : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3), "=&v"(t0), "=&v"(t1), "=&v"(t2), "=&v"(t3)
+        : "v"(a), "v"(b0), "v"(b1), "v"(b2), "v"(b3), "v"(codes), "v"(scale));
+    to = u32x4{t0, t1, t2, t3};
+}
+
+__global__ __launch_bounds__(Large16::kThreads) void large16_kernel(ManyArgs a) {
+    using S = Large16;
+    constexpr int kThreads = S::kThreads, kUnitsW = 4, kUnitsX = 16;  // of 16 bytes of a row and step
+    constexpr int kPerW = S::BM * kUnitsW / kThreads, kPerX = S::BN * kUnitsX / kThreads, kLoads = kPerW + kPerX;
+    typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+    __shared__ __attribute__((aligned(16))) char w0[S::BM * kUnitsW * 16], w1[S::BM * kUnitsW * 16], x0[S::BN * kUnitsX * 16],
+        x1[S::BN * kUnitsX * 16];
+    const Stage lds[2] = {{(lds_char *)w0, (lds_char *)x0}, {(lds_char *)w1, (lds_char *)x1}};
+    int32_t tm, tn;
+    tile_of(blockIdx.x, gridDim.x, a.tiles_m, a.tiles_n, tm, tn);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int wm = wave / S::WN, wn = wave % S::WN, r = lane & 15, g = lane >> 4;
+    const int32_t m0 = tm * S::BM, n0 = tn * S::BN, nb = a.w.nb;
+    const int32_t part_steps = a.part_steps;  // even
+
+    // The loads of a step.  Unit c of a row lies where the 16 lanes of a fragment's read spread over all banks.  Behind the end of a
+    // row of codes its step's first unit is loaded, which is multiplied with zeros.
+    const char *base_w = reinterpret_cast<const char *>(a.w.codes) + (int64_t)m0 * nb * 16, *base_x = a.x + n0 * a.x_row_bytes;
+    const char *const first_w = base_w;
+    uint32_t at_w[kPerW], at_x[kPerX];
+    const int32_t c_w = ((int)threadIdx.x & 3) ^ ((int)threadIdx.x >> 4 & 3);
+    each<kPerW>([&](auto i) CFGZIP_INLINE {
+        const int32_t row = i.value * (kThreads / kUnitsW) + (int)threadIdx.x / kUnitsW, last = a.w.V - m0 - 1;
+        at_w[i.value] = (uint32_t)afresh((int)((uint32_t)(row < last ? row : last) * (uint32_t)nb * 16u + c_w * 16));
+    });
+    each<kPerX>([&](auto i) CFGZIP_INLINE {
+        const int32_t row = i.value * (kThreads / kUnitsX) + (int)threadIdx.x / kUnitsX, last = a.out.B - n0 - 1;
+        const int32_t c = ((int)threadIdx.x & 15) ^ (row & 15);
+        at_x[i.value] = (uint32_t)afresh((int)((uint32_t)(row < last ? row : last) * (uint32_t)a.x_row_bytes + c * 16));
+    });
+    int32_t steps_left = part_steps * a.parts;  // of those to be loaded
+    int32_t step_w = 0;                         // of the weights, of the next to be loaded
+    uint32_t skip_w = 0;                        // what takes the thread's unit back to the step's first where it is not there
+    auto look = [&]() CFGZIP_INLINE {
+        const int32_t there = nb - (base_w == first_w ? 0 : (int32_t)((base_w - first_w) / 64)) * 4;
+        skip_w = c_w >= there ? (uint32_t)c_w * 16u : 0u;
+    };
+    look();
+    auto load_into = [&](const Stage &to) CFGZIP_INLINE {
+        return [&](auto i) CFGZIP_INLINE {
+            if constexpr (i.value < kPerW) {
+                const uint32_t from = (uint32_t)afresh((int)(at_w[i.value] - skip_w));
+                __builtin_amdgcn_global_load_lds((global_void *)(base_w + from), (lds_void *)(to.a + (i.value * kThreads + wave * kWave) * 16),
+                                                 16, 0, 0);
+            } else {
+                const uint32_t from = (uint32_t)afresh((int)at_x[i.value - kPerW]);
+                __builtin_amdgcn_global_load_lds((global_void *)(base_x + from),
+                                                 (lds_void *)(to.b + ((i.value - kPerW) * kThreads + wave * kWave) * 16), 16, 0, 0);
+            }
+        };
+    };
+    auto advance = [&]() CFGZIP_INLINE {
+        ++step_w;
+        if (step_w == part_steps) {
+            step_w = 0;
+            base_w = first_w;
+        } else if (step_w * 4 < nb) {  // else the base stays at blocks that are there
+            base_w += kUnitsW * 16;
+        }
+        if (--steps_left > 0) base_x += kUnitsX * 16;
+        look();
+    };
+
+    // a lane's scales: those of the step at hand, and the next one's bytes on their way
+    const uint8_t *const scale_base = a.w.scales + (int64_t)m0 * nb;
+    uint32_t at_s[S::FM], bytes[S::FM];
+    each<S::FM>([&](auto i) CFGZIP_INLINE {
+        const int32_t row = wm * S::TM + 16 * i.value + r, last = a.w.V - m0 - 1;
+        at_s[i.value] = (uint32_t)(row < last ? row : last) * (uint32_t)nb;
+    });
+    int32_t block = g;
+    auto ask = [&]() CFGZIP_INLINE {
+        const uint32_t from = block < nb ? block : nb - 1;
+        each<S::FM>([&](auto i) CFGZIP_INLINE { bytes[i.value] = scale_base[at_s[i.value] + from]; });
+    };
+    float scale[S::FM];
+    auto take = [&]() CFGZIP_INLINE {  // (a block that is not there: what is loaded in its place is finite, and so has to be its scale)
+        each<S::FM>([&](auto i) CFGZIP_INLINE { scale[i.value] = __builtin_bit_cast(float, block < nb ? scale_bits(bytes[i.value]) : 0x3F800000u); });
+        block += 4;
+        if (block >= part_steps * 4) block = g;
+    };
+
+    // fragments
+    const int32_t from_w = (wm * S::TM + r) * (kUnitsW * 16) + (g ^ (r >> 2 & 3)) * 16;
+    const int32_t from_x = (wn * S::TN + r) * (kUnitsX * 16) + ((4 * g) ^ r) * 16;
+    u32x4 codes[S::FM], next_codes[S::FM], x[2][S::FN];
+    auto read_w = [&](const Stage &from, auto i) CFGZIP_INLINE {
+        next_codes[i.value] = *reinterpret_cast<lds_u32x4 *>(from.a + from_w + i.value * (16 * kUnitsW * 16));
+    };
+    auto read_x = [&](const Stage &from, auto q, auto j) CFGZIP_INLINE {
+        x[q.value & 1][j.value] = *reinterpret_cast<lds_u32x4 *>(from.b + (from_x ^ (q.value * 16)) + j.value * (16 * kUnitsX * 16));
+    };
+    f32x4 acc[S::FM][S::FN];
+    each<S::FM>([&](auto i) CFGZIP_INLINE {
+        each<S::FN>([&](auto j) CFGZIP_INLINE { acc[i.value][j.value] = f32x4{0, 0, 0, 0}; });
+    });
+
+    each<kLoads>(load_into(lds[0]));
+    advance();
+    each<kLoads>(load_into(lds[1]));
+    advance();
+    ask();
+    wait_for_loads<0>();
+    const std::integral_constant<int, 0> zero;
+    each<S::FM>([&](auto i) CFGZIP_INLINE { read_w(lds[0], i); });
+    each<S::FN>([&](auto j) CFGZIP_INLINE { read_x(lds[0], zero, j); });
+    u32x4 w;
+    int32_t left = part_steps * a.parts / 2;
+    do {
+        each<2>([&](auto s) CFGZIP_INLINE {
+            const Stage &here = lds[s.value], &next = lds[1 - s.value];
+            take();
+            each<S::FM>([&](auto i) CFGZIP_INLINE { codes[i.value] = next_codes[i.value]; });
+            w = weights8(codes[0][0], scale[0]);
+            each<4>([&](auto q) CFGZIP_INLINE {
+                if constexpr (q.value == 1) ask();
+                // The next step's loads have come in and this one's have been read by everybody: its buffers are loaded again with what
+                // lies two steps ahead.
+                if constexpr (q.value == 3) wait_for_loads<0>();
+                each<2 * S::FM>([&](auto p) CFGZIP_INLINE {
+                    constexpr int i = p.value / 2, j = p.value % 2 * 4;
+                    u32x4 (&y)[S::FN] = x[q.value & 1];
+                    if constexpr (j == 0) {
+                        Bf16::mma4(w, y[0], y[1], y[2], y[3], acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+                    } else if constexpr (i + 1 < S::FM || q.value < 3) {
+                        constexpr int i1 = (i + 1) % S::FM, q1 = i + 1 < S::FM ? q.value : q.value + 1;
+                        u32x4 to;
+                        mma4_and_convert(w, y[4], y[5], y[6], y[7], acc[i][4], acc[i][5], acc[i][6], acc[i][7], to, codes[i1][q1], scale[i1]);
+                        w = to;
+                    } else {
+                        Bf16::mma4(w, y[4], y[5], y[6], y[7], acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+                    }
+                    constexpr int kLast = 12;
+                    constexpr int kReads = S::FN + (q.value == 3 ? S::FM : 0);
+                    constexpr int f0 = from(p.value, kReads, kLast), f1 = from(p.value + 1, kReads, kLast);
+                    each<f1 - f0>([&](auto f) CFGZIP_INLINE {
+                        constexpr int n = f0 + f.value;
+                        if constexpr (n < S::FN) {
+                            if constexpr (q.value < 3) read_x(here, std::integral_constant<int, q.value + 1>{}, std::integral_constant<int, n>{});
+                            else read_x(next, std::integral_constant<int, 0>{}, std::integral_constant<int, n>{});
+                        } else {
+                            read_w(next, std::integral_constant<int, n - S::FN>{});
+                        }
+                    });
+                    if constexpr (q.value == 3) {
+                        constexpr int l0 = from(p.value, kLoads + 1, 16), l1 = from(p.value + 1, kLoads + 1, 16);
+                        each<l1 - l0>([&](auto l) CFGZIP_INLINE {
+                            if constexpr (l0 + l.value < kLoads) load_into(here)(std::integral_constant<int, l0 + l.value>{});
+                            else advance();
+                        });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+        });
+    } while (--left > 0);
+    settle<S>(acc);
+    store_tile<S>(a, tm, tn, wm, wn, lane, acc);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): nothing is on its way into LDS that may soon be another workgroup's
+}
+
+// Products of 4-bit operands by the loop of the 16-bit ones: a step of 64 16-bit elements is 256 values, lane (r, g) of a fragment has
+// block 4 kk + g of its row in half kk of a step, 16 bytes like eight 16-bit elements.
+struct Mx4 {
+    template <int BYTE>
+    static __device__ __forceinline__ void mma4(u32x4 a, u32x4 b0, u32x4 b1, u32x4 b2, u32x4 b3, f32x4 &c0, f32x4 &c1, f32x4 &c2, f32x4 &c3,
+                                                uint32_t sa, uint32_t s0, uint32_t s1, uint32_t s2, uint32_t s3) {
+        // (four products with one a and the wait states in front of them as in the 16-bit forms; BYTE: of the scales)
+#define CFGZIP_MMA4(op_sel, op_sel_hi)                                                                                                      \
+    asm volatile(                                                                                                                           \
+        "s_nop 1\n\t"                                                                                                                       \
+        "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %4, %5, %0, %9, %10 op_sel:" op_sel " op_sel_hi:" op_sel_hi " cbsz:4 blgp:4\n\t"             \
+        "v_mfma_scale_f32_16x16x128_f8f6f4 %1, %4, %6, %1, %9, %11 op_sel:" op_sel " op_sel_hi:" op_sel_hi " cbsz:4 blgp:4\n\t"             \
+        "v_mfma_scale_f32_16x16x128_f8f6f4 %2, %4, %7, %2, %9, %12 op_sel:" op_sel " op_sel_hi:" op_sel_hi " cbsz:4 blgp:4\n\t"             \
+        "v_mfma_scale_f32_16x16x128_f8f6f4 %3, %4, %8, %3, %9, %13 op_sel:" op_sel " op_sel_hi:" op_sel_hi " cbsz:4 blgp:4"                  \
+        : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)                                                                                            \
+        : "v"(a), "v"(b0), "v"(b1), "v"(b2), "v"(b3), "v"(sa), "v"(s0), "v"(s1), "v"(s2), "v"(s3))
+        if constexpr (BYTE == 0) CFGZIP_MMA4("[0,0,0]", "[0,0,0]");
+        if constexpr (BYTE == 1) CFGZIP_MMA4("[1,1,0]", "[0,0,0]");
+        if constexpr (BYTE == 2) CFGZIP_MMA4("[0,0,0]", "[1,1,0]");
+        if constexpr (BYTE == 3) CFGZIP_MMA4("[1,1,0]", "[1,1,0]");
+#undef CFGZIP_MMA4
+    }
+};
+
+// Scales of a tile's rows, of two steps (16 blocks) at a time.  Thread t has row t of the tile's tokens and row t of its hidden states:
+// it loads a row's 16 bytes at once, and leaves the four that lane group g needs, blocks g, 4 + g, 8 + g and 12 + g, next to each
+// other.  (Two bytes a fragment, step and lane straight from memory take sixteen loads of sixteen pieces a step instead of one load of
+// 64, and as long in the caches as the codes.)
+template <typename S>
+struct TileScales {
+    static constexpr bool kScaled = true;
+    static_assert(S::kThreads == S::BM && S::kThreads == S::BN, "a row of either side to a thread");
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    typedef __attribute__((address_space(3))) const uint32_t lds_u32;
+    static constexpr int kBytes = (S::BM + S::BN) * 16;  // of one of two buffers
+
+    const uint8_t *w, *x;
+    int32_t V, B, nb;
+    lds_char *lds;
+    int32_t at = 0;        // of the buffer to be filled
+    int32_t left;          // blocks of a row from those asked for on
+    int32_t m0, n0;        // the tile's first rows
+    u32x4 asked[2];
+    uint32_t a[S::FM], b[S::FN];
+
+    // Blocks of a row from its `left`-last on, sixteen bytes.  No branch, and nothing behind the array is read: there its last sixteen
+    // are, which whole() moves down.
+    static __device__ __forceinline__ int32_t moved(int32_t row, int32_t rows, int32_t nb, int32_t left) {
+        const int64_t behind = (int64_t)(rows - 1 - row) * nb + left;  // blocks up to the array's end
+        return behind < 16 ? 16 - (int32_t)(behind > 0 ? behind : 1) : 0;
+    }
+    static __device__ __forceinline__ u32x4 sixteen(const uint8_t *base, int32_t row, int32_t rows, int32_t nb, int32_t left) {
+        const int64_t all = (int64_t)rows * nb, at = (int64_t)row * nb + (nb - left);
+        return *reinterpret_cast<const u32x4_bytes *>(base + (at < all - 16 ? at : all - 16));
+    }
+    // What belongs to the row, and 0 behind its end (a scale that is a NaN would make its products with the zeros there NaN).
+    static __device__ __forceinline__ u32x4 whole(u32x4 v, int32_t moved, int32_t left) {
+        const uint32_t down = moved * 8;
+        uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+        const uint64_t over = hi << 1 << (63 - (down & 63));
+        lo = down & 64 ? hi >> (down & 63) : lo >> (down & 63) | over;
+        hi = down & 64 ? 0 : hi >> (down & 63);
+        u32x4 out = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const int32_t here = left - 4 * d;
+            out[d] &= here >= 4 ? ~0u : here <= 0 ? 0u : (1u << (8 * here)) - 1u;
+        }
+        return out;
+    }
+    static __device__ __forceinline__ u32x4 transposed(u32x4 v) {
+        const uint32_t lo01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400), hi01 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602);
+        const uint32_t lo23 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400), hi23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602);
+        return u32x4{__builtin_amdgcn_perm(lo23, lo01, 0x05040100), __builtin_amdgcn_perm(lo23, lo01, 0x07060302),
+                     __builtin_amdgcn_perm(hi23, hi01, 0x05040100), __builtin_amdgcn_perm(hi23, hi01, 0x07060302)};
+    }
+    __device__ __forceinline__ int32_t v() const { return clamped(m0, V); }
+    __device__ __forceinline__ int32_t r() const { return clamped(n0, B); }
+    static __device__ __forceinline__ int32_t clamped(int32_t first, int32_t rows) {
+        const int32_t row = first + afresh(threadIdx.x);
+        return row < rows ? row : rows - 1;
+    }
+    __device__ __forceinline__ void load() {
+        asked[0] = sixteen(w, v(), V, nb, left);
+        asked[1] = sixteen(x, r(), B, nb, left);
+    }
+    __device__ __forceinline__ void begin(const Work &work) {
+        m0 = work.m0, n0 = work.n0, left = nb;
+        load();
+    }
+    __device__ __forceinline__ void ask() {
+        left -= 16;
+        load();
+    }
+    __device__ __forceinline__ void put() {
+        const int32_t t = (int32_t)afresh(threadIdx.x) * 16 + at;
+        u32x4 s = asked[0], z = asked[1];
+        if (left < 16) {
+            s = whole(s, moved(v(), V, nb, left), left);
+            z = whole(z, moved(r(), B, nb, left), left);
+        }
+        *reinterpret_cast<lds_u32x4 *>(lds + t) = transposed(s);
+        *reinterpret_cast<lds_u32x4 *>(lds + (t + S::BM * 16)) = transposed(z);
+    }
+    __device__ __forceinline__ void take(int wm, int wn, int lane) {
+        const int32_t from = at + (lane & 15) * 16 + (lane >> 4) * 4;
+        each<S::FM>([&](auto i) CFGZIP_INLINE { a[i.value] = *reinterpret_cast<lds_u32 *>(lds + (from + (wm * S::TM + 16 * i.value) * 16)); });
+        each<S::FN>([&](auto j) CFGZIP_INLINE {
+            b[j.value] = *reinterpret_cast<lds_u32 *>(lds + (from + (S::BM + wn * S::TN + 16 * j.value) * 16));
+        });
+        at ^= kBytes;
+    }
+};
+
+// Both sides in 4 bits, many rows of both: tiles of 256 x 256 by four waves.
+using Large4 = Shape<256, 256, 2, 2, 2>;
+__global__ __launch_bounds__(Large4::kThreads) void large4_kernel(ManyArgs a) {
+    using S = Large4;
+    // behind a row's end both sides hold some codes, with scales of 2^-127 each: products far below the smallest number
+    using TileW = Tile<S::BM, S::kThreads, false, true, ANY>;
+    using TileX = Tile<S::BN, S::kThreads, false, true, ANY>;
+    CFGZIP_STAGES(S, lds);
+    __shared__ __attribute__((aligned(16))) char scales_lds[2 * TileScales<S>::kBytes];
+    const int32_t elements = a.w.nb * 8;  // 16-bit ones of a row
+    int32_t tm, tn;
+    tile_of(blockIdx.x, gridDim.x, a.tiles_m, a.tiles_n, tm, tn);
+    auto work = [&](int32_t, Work &w) CFGZIP_INLINE {
+        w = Work{tm * S::BM, tn * S::BN, 0, elements};
+        return true;
+    };
+    auto store = [&](int32_t, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE { store_tile<S>(a, tm, tn, wm, wn, lane, acc); };
+    TileScales<S> scales;
+    scales.w = a.w.scales;
+    scales.x = a.x_scales;
+    scales.V = a.w.V;
+    scales.B = a.out.B;
+    scales.nb = a.w.nb;
+    scales.lds = (lds_char *)scales_lds;
+    multiply<Mx4, S, TileW, TileX>(by_rows(reinterpret_cast<const uint16_t *>(a.w.codes), elements, a.w.V),
+                                   by_rows(reinterpret_cast<const uint16_t *>(a.x), elements, a.out.B), lds, work, store, scales);
+}
+
+// Hidden states as bf16 in rows of whole pairs of steps, zeros behind K; of fp16 a row's rests behind its first numbers
 template <bool F16>
 __global__ __launch_bounds__(256) void split_kernel(const uint16_t *x, int64_t x_ld, int32_t B, int32_t K, int32_t y_ld, uint16_t *y) {
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -700,8 +1052,9 @@ __global__ __launch_bounds__(256) void split_kernel(const uint16_t *x, int64_t x
         hi[j / 2] |= h << (j % 2 * 16);
         lo[j / 2] |= l << (j % 2 * 16);
     }
-    *reinterpret_cast<u32x4 *>(y + (int64_t)b * y_ld + c) = hi;
-    if constexpr (F16) *reinterpret_cast<u32x4 *>(y + (int64_t)(B + b) * y_ld + c) = lo;
+    y += (int64_t)b * y_ld * (F16 ? 2 : 1) + c;
+    *reinterpret_cast<u32x4 *>(y) = hi;
+    if constexpr (F16) *reinterpret_cast<u32x4 *>(y + y_ld) = lo;
 }
 
 // ---------------------------------------------------------------- host
@@ -710,6 +1063,7 @@ constexpr size_t kLdsBytes = 160 * 1024;
 constexpr int32_t kMaxBlocks = 1 << 17;  // K <= 2^22: offsets of a tile's rows stay below 2^32
 
 int32_t blocks_of(int32_t K) { return (int32_t)ceil_div(K, 32); }
+int32_t whole_pairs(int32_t K) { return (int32_t)ceil_div(K, kPairK) * kPairK; }  // K in whole pairs of steps
 
 // Rows in LDS of the kernel for few rows and the bytes of one, so that 16 of them spread over all banks; 0 bytes: does not fit
 size_t few_lds(int x, int32_t B, int32_t nb, int32_t &row, int &fragments) {
@@ -738,9 +1092,25 @@ int launch_few(const FewArgs &a, size_t lds, hipStream_t stream) {
 }
 
 using Many64 = Shape<128, 64, 4, 1>;
-using Many128 = Shape<256, 128, 4, 2>;
 using Many4_64 = Shape<256, 64, 4, 1>;
-using Many4_256 = Shape<256, 256, 2, 4>;
+
+int launch_large16(ManyArgs a, hipStream_t stream) {
+    a.tiles_m = (int32_t)ceil_div(a.w.V, Large16::BM);
+    a.tiles_n = (int32_t)ceil_div(a.out.B, Large16::BN);
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n;
+    if (work > 0x7FFFFFFF) return CFGZIP_E_TOO_LARGE;
+    hipLaunchKernelGGL(large16_kernel, dim3((uint32_t)work), dim3(Large16::kThreads), 0, stream, a);
+    return check_launch();
+}
+
+int launch_large4(ManyArgs a, hipStream_t stream) {
+    a.tiles_m = (int32_t)ceil_div(a.w.V, Large4::BM);
+    a.tiles_n = (int32_t)ceil_div(a.out.B, Large4::BN);
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n;
+    if (work > 0x7FFFFFFF) return CFGZIP_E_TOO_LARGE;
+    hipLaunchKernelGGL(large4_kernel, dim3((uint32_t)work), dim3(Large4::kThreads), 0, stream, a);
+    return check_launch();
+}
 
 template <typename S, bool FOUR>
 int launch_many(ManyArgs a, hipStream_t stream) {
@@ -767,7 +1137,7 @@ LogitsWorkspace logits_workspace(void *ws, int32_t dtype, int32_t B, int32_t V, 
     int fragments;
     if (!few_lds(x_kind(dtype), B, blocks_of(K), row, fragments)) {
         if (bits_kind == CFGZIP_BITS_CLASS) w.tok_bits = c.take<int32_t>((size_t)B * words_for(V));
-        if (dtype != CFGZIP_DTYPE_MX4) w.x = c.take<uint16_t>((size_t)B * blocks_of(K) * 32 * (dtype == CFGZIP_DTYPE_F16 ? 2 : 1));
+        if (dtype != CFGZIP_DTYPE_MX4) w.x = c.take<uint16_t>((size_t)B * whole_pairs(K) * (dtype == CFGZIP_DTYPE_F16 ? 2 : 1));
     }
     w.bytes = c.used;
     return w;
@@ -895,23 +1265,25 @@ extern "C" int cfgzip_mx4_logits(const void *hidden, int32_t hidden_dtype, int64
         a.x_row_bytes = (int64_t)nb * 16;
         a.x_scales = hidden_scales;
         a.x_units = nb;
-        return B <= 64 ? launch_many<Many4_64, true>(a, s) : launch_many<Many4_256, true>(a, s);
+        return B <= 64 || (int64_t)V * nb < 16 ? launch_many<Many4_64, true>(a, s) : launch_large4(a, s);
     }
-    if (x == X_BF16 && K % 8 == 0 && hidden_stride % 8 == 0 && hidden_stride < kMaxStride && aligned_to(hidden, 16)) {
+    a.parts = x == X_F16 ? 2 : 1;
+    a.part_steps = whole_pairs(K) / 128;
+    if (x == X_BF16 && K % kPairK == 0 && hidden_stride % 8 == 0 && hidden_stride < kMaxStride && aligned_to(hidden, 16)) {
         a.x = static_cast<const char *>(hidden);
         a.x_row_bytes = hidden_stride * 2;
-        a.x_units = K / 8;
     } else {
-        const dim3 g((uint32_t)ceil_div((int64_t)B * nb * 4, 256)), t(256);
+        const int32_t ld = whole_pairs(K);
+        const dim3 g((uint32_t)ceil_div((int64_t)B * (ld / 8), 256)), t(256);
         const uint16_t *h = static_cast<const uint16_t *>(hidden);
-        if (x == X_F16) hipLaunchKernelGGL(split_kernel<true>, g, t, 0, s, h, hidden_stride, B, K, nb * 32, w.x);
-        else hipLaunchKernelGGL(split_kernel<false>, g, t, 0, s, h, hidden_stride, B, K, nb * 32, w.x);
+        if (x == X_F16) hipLaunchKernelGGL(split_kernel<true>, g, t, 0, s, h, hidden_stride, B, K, ld, w.x);
+        else hipLaunchKernelGGL(split_kernel<false>, g, t, 0, s, h, hidden_stride, B, K, ld, w.x);
         CFGZIP_TRY(check_launch());
         a.x = reinterpret_cast<const char *>(w.x);
-        a.x_row_bytes = (int64_t)nb * 64;
-        a.x_part_bytes = (int64_t)B * nb * 64;
-        a.x_units = nb * 4;
-        a.parts = x == X_F16 ? 2 : 1;
+        a.x_part_bytes = (int64_t)ld * 2;
+        a.x_row_bytes = a.x_part_bytes * a.parts;
     }
-    return B <= 64 ? launch_many<Many64, false>(a, s) : launch_many<Many128, false>(a, s);
+    a.x_units = nb * 4;
+    if (B > 64) return launch_large16(a, s);
+    return launch_many<Many64, false>(a, s);
 }
