@@ -30,6 +30,11 @@ _build_classes = None
 _displacements = None
 _nfa_signatures = None
 _CALLS = ("decode_step", "engine_step", "signatures", "build_classes", "displacements", "nfa_signatures")
+# the vocabulary projection's: calls of the extension, and what they need of the library
+_HEAD_CALLS = ("head_loss", "head_loss_grad", "mx4_quantize", "mx4_values", "mx4_logits")
+_HEAD_ENTRIES = ("head_loss_workspace_bytes", "head_loss", "head_loss_grad_workspace_bytes", "head_loss_grad", "mx4_quantize",
+                 "mx4_values", "mx4_logits_workspace_bytes", "mx4_logits")
+_head_loss = _head_loss_grad = _mx4_quantize = _mx4_values = _mx4_logits = None
 
 DEFAULT_HASH_SEED = 0x5EED_CF62_1234_ABCD
 
@@ -73,6 +78,8 @@ def _by_ctypes(*_args) -> None:
 def _load_stepcall(lib: ctypes.CDLL):
     """The calls of the extension.  They save host time and nothing else: every call goes through ctypes as
     well, so an extension that is not there, or was built for another torch or Python, is done without."""
+    global _head_loss, _head_loss_grad, _mx4_quantize, _mx4_values, _mx4_logits
+    _head_loss = _head_loss_grad = _mx4_quantize = _mx4_values = _mx4_logits = _by_ctypes
     try:
         loader = importlib.machinery.ExtensionFileLoader("cfgzip_stepcall", _STEPCALL_PATH)
         spec = importlib.util.spec_from_file_location("cfgzip_stepcall", _STEPCALL_PATH, loader=loader)
@@ -86,6 +93,8 @@ def _load_stepcall(lib: ctypes.CDLL):
                       "`python -m paper_2605_29986_amd.build` builds it.", RuntimeWarning, stacklevel=3)
         return (_by_ctypes,) * len(_CALLS)
     stepcall.connect(*(ctypes.cast(getattr(lib, "cfgzip_" + f), ctypes.c_void_p).value for f in _CALLS))
+    stepcall.connect_head(*(ctypes.cast(getattr(lib, "cfgzip_" + f), ctypes.c_void_p).value for f in _HEAD_ENTRIES))
+    _head_loss, _head_loss_grad, _mx4_quantize, _mx4_values, _mx4_logits = (getattr(stepcall, f) for f in _HEAD_CALLS)
     return tuple(getattr(stepcall, f) for f in _CALLS)
 
 
@@ -751,6 +760,12 @@ def cfgzip_head_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.T
     [V, D] against target int32 [N], over the tokens that `bits` admits (masks over classes with `class_of_token` and `C`, over
     tokens without, every token without `bits`).  A target outside [0, V) has loss 0, one that is not admitted +inf."""
     lib = _lib or load_library()
+    if loss is None and lse is None and workspace is None and stream is None:
+        out = _head_loss(hidden, weight, target, bits, class_of_token, C)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_head_loss", out)
+            return out
     args = _head(hidden, weight, target, bits, class_of_token, C)
     N, V, D, kind = args[5], args[6], args[7], args[10]
     dev = weight.device
@@ -774,6 +789,12 @@ def cfgzip_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: to
     """(grad_hidden [N, D], grad_weight [V, D]) in the inputs' type for grad_loss float32 [N], with the lse of cfgzip_head_loss
     on the same inputs.  Rows without a target, or with one that is not admitted, have no gradient."""
     lib = _lib or load_library()
+    if grad_hidden is None and grad_weight is None and workspace is None and stream is None:
+        out = _head_loss_grad(hidden, weight, target, bits, class_of_token, C, lse, grad_loss, want_hidden, want_weight)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_head_loss_grad", out)
+            return out
     args = _head(hidden, weight, target, bits, class_of_token, C)
     N, V, D, kind = args[5], args[6], args[7], args[10]
     dev = weight.device
@@ -819,6 +840,12 @@ def cfgzip_mx4_quantize(x: torch.Tensor, *, codes: Optional[torch.Tensor] = None
     """(codes uint8 [R, 16 * nb], scales uint8 [R, nb]), nb = ceil(K / 32), of x [R, K] (float32, bfloat16 or float16, rows any
     stride apart): blocks of 32 values in 4 bits with a shared power of two."""
     lib = _lib or load_library()
+    if codes is None and scales is None and stream is None:
+        out = _mx4_quantize(x)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_mx4_quantize", out)
+            return out
     p, stride = _rows(x, "x", tuple(_DTYPE))
     R, K = x.shape
     nb = _blocks(K)
@@ -838,6 +865,12 @@ def cfgzip_mx4_values(codes: torch.Tensor, scales: torch.Tensor, K: int, *, dtyp
                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """What codes and scales of rows of K values stand for, [R, K] in `dtype`."""
     lib = _lib or load_library()
+    if out is None and stream is None:
+        made = _mx4_values(codes, scales, K, _DTYPE.get(dtype))
+        if made is not None:
+            if type(made) is int:
+                _check("cfgzip_mx4_values", made)
+            return made
     c, s, R, nb = _mx4(codes, scales, "")
     if _blocks(K) != nb:
         raise ValueError("scales must have ceil(K / 32) columns")
@@ -858,6 +891,12 @@ def cfgzip_mx4_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.T
     """Logits [B, V] (float32 or bfloat16) of hidden [B, K] (bfloat16 or float16; or codes uint8 [B, 16 * nb] with hidden_scales
     uint8 [B, nb]) and weights in 4 bits (codes, scales of V rows of K values), -inf where `bits` does not admit the token."""
     lib = _lib or load_library()
+    if logits is None and workspace is None and stream is None:
+        out = _mx4_logits(hidden, codes, scales, hidden_scales, _DTYPE.get(dtype), bits, class_of_token, C)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_mx4_logits", out)
+            return out
     c, s, V, nb = _mx4(codes, scales, "")
     dev = codes.device
     if hidden_scales is None:

@@ -3,6 +3,7 @@
 // and checks of tensors, the conversion of as many arguments for ctypes) took 5 us of the 8 that a step on small logits
 // takes, and the kernel 3; and of the 44 us of signatures and classes of 4,096 tokens, 157 of displacements and classes of
 // 32,000 and 165 of relations and classes of 32,000 it took 5, 6 and 4, as the GPU has nothing to do before the first launch.
+// The vocabulary projection's calls are here for the same reason, with results and workspace of their own only.
 //
 // Marshalling only, and only of the plain case: exact torch.Tensor objects in GPU memory of the types and layouts the
 // binding asks for, the current stream.  For anything else a function returns None and has done nothing; the binding then
@@ -43,6 +44,26 @@ Signatures g_signatures = nullptr;
 BuildClasses g_build_classes = nullptr;
 Displacements g_displacements = nullptr;
 NfaSignatures g_nfa_signatures = nullptr;
+
+using HeadLossBytes = size_t (*)(int32_t, int32_t, int32_t, int32_t);
+using HeadLoss = int (*)(const void *, int64_t, const void *, int64_t, int32_t, int32_t, int32_t, int32_t, const int32_t *,
+                         const int32_t *, int32_t, const int32_t *, int32_t, float *, float *, void *, size_t, void *);
+using HeadLossGrad = int (*)(const void *, int64_t, const void *, int64_t, int32_t, int32_t, int32_t, int32_t, const int32_t *,
+                             const int32_t *, int32_t, const int32_t *, int32_t, const float *, const float *, void *, int64_t,
+                             void *, int64_t, void *, size_t, void *);
+using Mx4Quantize = int (*)(const void *, int32_t, int64_t, int32_t, int64_t, uint8_t *, uint8_t *, void *);
+using Mx4Values = int (*)(const uint8_t *, const uint8_t *, int64_t, int32_t, void *, int32_t, int64_t, void *);
+using Mx4LogitsBytes = size_t (*)(int32_t, int32_t, int32_t, int32_t, int32_t);
+using Mx4Logits = int (*)(const void *, int32_t, int64_t, const uint8_t *, const uint8_t *, const uint8_t *, int32_t, int32_t,
+                          int32_t, const int32_t *, int32_t, const int32_t *, int32_t, void *, int32_t, int64_t, void *, size_t,
+                          void *);
+HeadLossBytes g_head_loss_bytes = nullptr, g_head_loss_grad_bytes = nullptr;
+HeadLoss g_head_loss = nullptr;
+HeadLossGrad g_head_loss_grad = nullptr;
+Mx4Quantize g_mx4_quantize = nullptr;
+Mx4Values g_mx4_values = nullptr;
+Mx4LogitsBytes g_mx4_logits_bytes = nullptr;
+Mx4Logits g_mx4_logits = nullptr;
 
 constexpr int64_t kMost = std::numeric_limits<int32_t>::max();
 
@@ -420,6 +441,294 @@ PyObject *nfa_signatures(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return finish(rc, result);
 }
 
+// ---------------------------------------------------------------- the vocabulary projection
+
+// A matrix whose rows are any distance apart, types by the library's numbers.
+struct Matrix {
+    const at::Tensor *t;
+    void *data;
+    int64_t stride;
+    int32_t type, rows, columns;
+};
+constexpr at::ScalarType kTypes[] = {at::kFloat, at::kBFloat16, at::kHalf};
+bool matrix_of(PyObject *o, Matrix *out) {
+    const at::Tensor *t = plain(o);
+    if (!t || t->dim() != 2) return false;
+    out->type = -1;
+    for (int i = 0; i < 3; ++i)
+        if (t->scalar_type() == kTypes[i]) out->type = i;
+    const int64_t rows = t->size(0), columns = t->size(1);
+    if (out->type < 0 || rows > kMost || columns < 1 || columns > kMost || (columns > 1 && t->stride(1) != 1)) return false;
+    out->stride = rows > 1 || t->stride(0) > columns ? t->stride(0) : columns;
+    if (out->stride < columns) return false;
+    out->t = t;
+    out->data = t->data_ptr();
+    out->rows = (int32_t)rows;
+    out->columns = (int32_t)columns;
+    return true;
+}
+// Codes and scales of rows of 4-bit values.
+struct Blocks {
+    const at::Tensor *t;
+    const uint8_t *codes, *scales;
+    int32_t rows, blocks;
+};
+bool blocks_of(PyObject *codes, PyObject *scales, Blocks *out) {
+    const at::Tensor *c = plain(codes, at::kByte), *s = plain(scales, at::kByte);
+    if (!c || !s || c->dim() != 2 || s->dim() != 2 || c->size(0) != s->size(0) || c->size(1) != 16 * s->size(1) || s->size(0) > kMost ||
+        s->size(1) < 1 || s->size(1) > kMost / 32 || c->device() != s->device())
+        return false;
+    out->t = c;
+    out->codes = static_cast<const uint8_t *>(c->data_ptr());
+    out->scales = static_cast<const uint8_t *>(s->data_ptr());
+    out->rows = (int32_t)s->size(0);
+    out->blocks = (int32_t)s->size(1);
+    return true;
+}
+// Masks of `rows` rows over V tokens: (bits, class_of_token, C), each None (C: 0) where there is none.
+struct Masks {
+    const int32_t *bits = nullptr, *class_of_token = nullptr;
+    int32_t kind = 2, C = 0;
+};
+bool masks_of(PyObject *bits, PyObject *class_of_token, PyObject *C, int64_t rows, int64_t V, const at::Tensor &beside, Masks *out) {
+    if (bits == Py_None) return class_of_token == Py_None && PyLong_CheckExact(C) && PyLong_AsLong(C) == 0;
+    const at::Tensor *b = plain(bits, at::kInt);
+    if (!b || b->dim() != 2 || b->size(0) != rows || b->device() != beside.device()) return false;
+    out->kind = 0;
+    int64_t n = V;
+    if (class_of_token != Py_None) {
+        const at::Tensor *c = plain(class_of_token, at::kInt);
+        n = small_int(C);
+        if (!c || !n || c->numel() != V || c->device() != beside.device()) return false;
+        out->class_of_token = static_cast<const int32_t *>(c->data_ptr());
+        out->kind = 1;
+        out->C = (int32_t)n;
+    }
+    out->bits = static_cast<const int32_t *>(b->data_ptr());
+    return b->size(1) == (n + 31) / 32;
+}
+// n values of `type` beside a tensor, in a row
+void *vector_of(PyObject *o, at::ScalarType type, int64_t n, const at::Tensor &beside) {
+    const at::Tensor *t = plain(o, type);
+    return t && t->numel() == n && t->device() == beside.device() ? t->data_ptr() : nullptr;
+}
+at::Tensor workspace_of(size_t bytes, const at::Tensor &beside) {
+    return at::empty({(int64_t)(bytes > 256 ? bytes : 256)}, beside.options().dtype(at::kByte));
+}
+
+// (hidden, weight, target, bits, class_of_token, C[, lse, grad_loss, want_hidden, want_weight]): what the loss and its gradients
+// share.  No rows are left to the general way.
+struct Head {
+    Matrix hidden, weight;
+    const int32_t *target;
+    Masks masks;
+};
+bool head_of(PyObject *const *args, Head *out) {
+    if (!matrix_of(args[0], &out->hidden) || !matrix_of(args[1], &out->weight) || out->weight.type == 0 ||
+        out->hidden.type != out->weight.type || out->hidden.columns != out->weight.columns || out->hidden.rows < 1 ||
+        out->hidden.t->device() != out->weight.t->device())
+        return false;
+    out->target = static_cast<const int32_t *>(vector_of(args[2], at::kInt, out->hidden.rows, *out->weight.t));
+    return out->target && masks_of(args[3], args[4], args[5], out->hidden.rows, out->weight.rows, *out->weight.t, &out->masks);
+}
+
+PyObject *head_loss(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 6 || !g_head_loss || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Head h{};
+    float *loss = nullptr, *lse = nullptr;
+    void *ws = nullptr, *stream = nullptr;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        if (!head_of(args, &h)) return leave_it();
+        const auto options = h.weight.t->options().dtype(at::kFloat);
+        const at::Tensor made_loss = at::empty({h.hidden.rows}, options), made_lse = at::empty({h.hidden.rows}, options);
+        workspace = workspace_of(g_head_loss_bytes(h.hidden.rows, h.weight.rows, h.weight.columns, h.masks.kind), *h.weight.t);
+        loss = static_cast<float *>(made_loss.data_ptr());
+        lse = static_cast<float *>(made_lse.data_ptr());
+        ws = workspace.data_ptr();
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(THPVariable_Wrap(made_loss)), b(THPVariable_Wrap(made_lse));
+        if (a.o && b.o) result = PyTuple_Pack(2, a.o, b.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_head_loss(h.hidden.data, h.hidden.stride, h.weight.data, h.weight.stride, h.weight.type, h.hidden.rows, h.weight.rows,
+                     h.weight.columns, h.target, h.masks.bits, h.masks.kind, h.masks.class_of_token, h.masks.C, loss, lse, ws,
+                     (size_t)workspace.numel(), stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+PyObject *head_loss_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 10 || !g_head_loss_grad || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Head h{};
+    const float *lse = nullptr, *grad_loss = nullptr;
+    void *gh = nullptr, *gw = nullptr, *ws = nullptr, *stream = nullptr;
+    bool want_hidden = false, want_weight = false;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        if (!head_of(args, &h) || !bool_of(args[8], &want_hidden) || !bool_of(args[9], &want_weight) || (!want_hidden && !want_weight))
+            return leave_it();
+        lse = static_cast<const float *>(vector_of(args[6], at::kFloat, h.hidden.rows, *h.weight.t));
+        grad_loss = static_cast<const float *>(vector_of(args[7], at::kFloat, h.hidden.rows, *h.weight.t));
+        if (!lse || !grad_loss) Py_RETURN_NONE;
+        at::Tensor made_gh, made_gw;
+        if (want_hidden) {
+            made_gh = at::empty({h.hidden.rows, h.weight.columns}, h.weight.t->options());
+            gh = made_gh.data_ptr();
+        }
+        if (want_weight) {
+            made_gw = at::empty({h.weight.rows, h.weight.columns}, h.weight.t->options());
+            gw = made_gw.data_ptr();
+        }
+        workspace = workspace_of(g_head_loss_grad_bytes(h.hidden.rows, h.weight.rows, h.weight.columns, h.masks.kind), *h.weight.t);
+        ws = workspace.data_ptr();
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(want_hidden ? THPVariable_Wrap(made_gh) : Py_NewRef(Py_None)), b(want_weight ? THPVariable_Wrap(made_gw) : Py_NewRef(Py_None));
+        if (a.o && b.o) result = PyTuple_Pack(2, a.o, b.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_head_loss_grad(h.hidden.data, h.hidden.stride, h.weight.data, h.weight.stride, h.weight.type, h.hidden.rows, h.weight.rows,
+                          h.weight.columns, h.target, h.masks.bits, h.masks.kind, h.masks.class_of_token, h.masks.C, lse, grad_loss, gh,
+                          gh ? h.weight.columns : 0, gw, gw ? h.weight.columns : 0, ws, (size_t)workspace.numel(), stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// (x)
+PyObject *mx4_quantize(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 1 || !g_mx4_quantize || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Matrix x{};
+    uint8_t *codes = nullptr, *scales = nullptr;
+    void *stream = nullptr;
+    PyObject *result = nullptr;
+    try {
+        if (!matrix_of(args[0], &x)) Py_RETURN_NONE;
+        const int64_t nb = ((int64_t)x.columns + 31) / 32;
+        const auto options = x.t->options().dtype(at::kByte);
+        const at::Tensor made_codes = at::empty({x.rows, 16 * nb}, options), made_scales = at::empty({x.rows, nb}, options);
+        codes = static_cast<uint8_t *>(made_codes.data_ptr());
+        scales = static_cast<uint8_t *>(made_scales.data_ptr());
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(THPVariable_Wrap(made_codes)), b(THPVariable_Wrap(made_scales));
+        if (a.o && b.o) result = PyTuple_Pack(2, a.o, b.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_mx4_quantize(x.data, x.type, x.rows, x.columns, x.stride, codes, scales, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// The type that an argument names by the library's number, 0 .. last, or -1
+int32_t type_of(PyObject *o, long last) {
+    if (!PyLong_CheckExact(o)) return -1;
+    const long v = PyLong_AsLong(o);
+    return v < 0 || v > last ? -1 : (int32_t)v;
+}
+
+// (codes, scales, K, the result's type)
+PyObject *mx4_values(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 4 || !g_mx4_values || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Blocks w{};
+    int32_t K = 0, type = -1;
+    void *out = nullptr, *stream = nullptr;
+    PyObject *result = nullptr;
+    try {
+        K = (int32_t)small_int(args[2]);
+        type = type_of(args[3], 2);
+        if (!blocks_of(args[0], args[1], &w) || !K || type < 0 || ((int64_t)K + 31) / 32 != w.blocks) return leave_it();
+        const at::Tensor made = at::empty({w.rows, K}, w.t->options().dtype(kTypes[type]));
+        out = made.data_ptr();
+        stream = c10::hip::getCurrentHIPStream().stream();
+        result = THPVariable_Wrap(made);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_mx4_values(w.codes, w.scales, w.rows, K, out, type, K, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// (hidden, codes, scales, hidden_scales, the result's type, bits, class_of_token, C)
+PyObject *mx4_logits(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 8 || !g_mx4_logits || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Blocks w{}, x4{};
+    Matrix x{};
+    Masks m;
+    const void *hidden = nullptr;
+    int64_t stride = 0;
+    int32_t kind = 3, B = 0, K = 0, type = -1;
+    void *out = nullptr, *ws = nullptr, *stream = nullptr;
+    size_t bytes = 0;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        type = type_of(args[4], 1);
+        if (!blocks_of(args[1], args[2], &w) || type < 0 || w.rows < 1) return leave_it();
+        if (args[3] == Py_None) {
+            if (!matrix_of(args[0], &x) || x.type == 0 || ((int64_t)x.columns + 31) / 32 != w.blocks || x.t->device() != w.t->device())
+                Py_RETURN_NONE;
+            hidden = x.data, stride = x.stride, kind = x.type, B = x.rows, K = x.columns;
+        } else {
+            if (!blocks_of(args[0], args[3], &x4) || x4.blocks != w.blocks || x4.t->device() != w.t->device()) Py_RETURN_NONE;
+            hidden = x4.codes, stride = 16 * (int64_t)w.blocks, B = x4.rows, K = 32 * w.blocks;
+        }
+        if (B < 1 || !masks_of(args[5], args[6], args[7], B, w.rows, *w.t, &m)) return leave_it();
+        const at::Tensor made = at::empty({B, w.rows}, w.t->options().dtype(kTypes[type]));
+        out = made.data_ptr();
+        bytes = g_mx4_logits_bytes(kind, B, w.rows, K, m.kind);
+        if (bytes) {
+            workspace = workspace_of(bytes, *w.t);
+            ws = workspace.data_ptr();
+            bytes = (size_t)workspace.numel();
+        }
+        stream = c10::hip::getCurrentHIPStream().stream();
+        result = THPVariable_Wrap(made);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_mx4_logits(hidden, kind, stride, x4.scales, w.codes, w.scales, B, w.rows, K, m.bits, m.kind, m.class_of_token, m.C, out, type,
+                      w.rows, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// The addresses of the vocabulary projection's calls: cfgzip_head_loss_workspace_bytes, cfgzip_head_loss,
+// cfgzip_head_loss_grad_workspace_bytes, cfgzip_head_loss_grad, cfgzip_mx4_quantize, cfgzip_mx4_values,
+// cfgzip_mx4_logits_workspace_bytes and cfgzip_mx4_logits
+PyObject *connect_head(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    void *at[8];
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "connect_head takes eight addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 8; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+    if (PyErr_Occurred()) return nullptr;
+    g_head_loss_bytes = reinterpret_cast<HeadLossBytes>(at[0]);
+    g_head_loss = reinterpret_cast<HeadLoss>(at[1]);
+    g_head_loss_grad_bytes = reinterpret_cast<HeadLossBytes>(at[2]);
+    g_head_loss_grad = reinterpret_cast<HeadLossGrad>(at[3]);
+    g_mx4_quantize = reinterpret_cast<Mx4Quantize>(at[4]);
+    g_mx4_values = reinterpret_cast<Mx4Values>(at[5]);
+    g_mx4_logits_bytes = reinterpret_cast<Mx4LogitsBytes>(at[6]);
+    g_mx4_logits = reinterpret_cast<Mx4Logits>(at[7]);
+    Py_RETURN_NONE;
+}
+
 // The addresses of cfgzip_decode_step, cfgzip_engine_step, cfgzip_signatures, cfgzip_build_classes, cfgzip_displacements and
 // cfgzip_nfa_signatures, of the library that the binding has loaded
 PyObject *connect(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -450,6 +759,12 @@ PyMethodDef g_methods[] = {{"decode_step", fast<decode_step>(), METH_FASTCALL, n
                            {"displacements", fast<displacements>(), METH_FASTCALL, nullptr},
                            {"nfa_signatures", fast<nfa_signatures>(), METH_FASTCALL, nullptr},
                            {"connect", fast<connect>(), METH_FASTCALL, nullptr},
+                           {"head_loss", fast<head_loss>(), METH_FASTCALL, nullptr},
+                           {"head_loss_grad", fast<head_loss_grad>(), METH_FASTCALL, nullptr},
+                           {"mx4_quantize", fast<mx4_quantize>(), METH_FASTCALL, nullptr},
+                           {"mx4_values", fast<mx4_values>(), METH_FASTCALL, nullptr},
+                           {"mx4_logits", fast<mx4_logits>(), METH_FASTCALL, nullptr},
+                           {"connect_head", fast<connect_head>(), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "cfgzip_stepcall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
