@@ -10,6 +10,8 @@
 // again, for a piece of the vocabulary at a time, turned into dz in the accumulators, and stored in 16 bits; the two products
 // that read the piece follow while it is in the last-level cache.  All sums are fp32.
 
+#include <algorithm>
+
 #include "gemm16.hpp"
 
 namespace cfgzip {
@@ -30,10 +32,12 @@ constexpr int64_t slots() {
 // What a product's tiles take, in microseconds: rounds of as many as are at work at a time, of so many steps each and a beginning and an
 // end.
 template <typename S>
+constexpr double kStepTime = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : S::BM * S::BN == 8192 ? 0.6 : 0.35;
+template <typename S>
+constexpr double kEndsTime = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.0 : 4.0;
+template <typename S>
 double time_of(int64_t m, int64_t n, int64_t steps) {
-    const double step = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : S::BM * S::BN == 8192 ? 0.6 : 0.35;
-    const double ends = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.0 : 4.0;
-    return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * step + ends);
+    return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * kStepTime<S> + kEndsTime<S>);
 }
 
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time: the size of the last-level cache
@@ -469,28 +473,38 @@ Plan plan_of(int32_t N, int32_t V, int32_t D) {
     Plan p{};
     p.logits_rows = rows_of_tile(N);
     p.parts = N <= kFewRows ? 2 : 1;
-    p.rows = rows_of_tile(N * p.parts);
-    p.rows_pad = (int32_t)pad(N * p.parts, p.rows > kStepK ? p.rows : kStepK);  // (zeros behind N: steps of grad_weight's sum)
     p.d_pad = (int32_t)pad(D, kStepK);
-    int64_t most = (int64_t)(kPieceBytes / 2 / p.rows_pad) / 256 * 256;
+    const int32_t rows_dz = N * p.parts;
+    // (tiles of logits leave zeros behind N as well, and grad_weight's sum goes over whole steps of rows)
+    int64_t most = (int64_t)(kPieceBytes / 2 / pad(rows_dz, 256)) / 256 * 256;
     if (most < kPieceLeast) most = kPieceLeast;
     const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, most);
     p.piece = (int32_t)pad(ceil_div(V, pieces), 256);
-    // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip
-    const int64_t tiles = ceil_div(D, columns_of_tile(p.rows)) * ceil_div(N * p.parts, p.rows);
-    const int64_t at_a_time = p.rows == 16 ? slots<Shape16>() : p.rows == 64 ? slots<Shape64>() : p.rows == 128 ? slots<Shape128>() : slots<Shape256>();
-    int64_t best = 1;
-    double best_use = 0;
-    for (int64_t s = 1; s * kSplitLeast <= p.piece && tiles * s <= at_a_time * 2; ++s) {
-        const int64_t rounds = ceil_div(tiles * s, at_a_time);
-        const double use = (double)(tiles * s) / (double)(rounds * at_a_time);
-        if (use > best_use * 1.05) {  // a further share of the sums costs a pass over them
-            best_use = use;
-            best = s;
+    // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip, which costs a pass over the shares
+    const int64_t first = V < p.piece ? V : p.piece;
+    double best = 0;
+    auto look = [&](auto shape, int rows) {
+        using S = decltype(shape);
+        const int64_t tiles = ceil_div(D, S::BM) * ceil_div(rows_dz, S::BN);
+        for (int64_t s = 1; s == 1 || (s * kSplitLeast <= p.piece && tiles * s <= slots<S>() * 2); ++s) {
+            const int64_t k_split = pad(ceil_div(p.piece, s), kStepK);
+            const double shares = s > 1 || pieces > 1 || p.parts > 1 ? 4.0 + (double)s * rows_dz * D * 8.0 / 4e6 : 0.0;
+            const double tiles_time = (double)ceil_div(tiles * s, slots<S>()) * ((double)(k_split / kStepK) * kStepTime<S> + kEndsTime<S>);
+            // (or reading the weights, which rows of several tiles read more than once, partly from the caches)
+            const double time = std::max(tiles_time, (double)first * D * 2.0 / 4.5e6 * (0.5 + 0.5 * (double)ceil_div(rows_dz, S::BN))) + shares;
+            if (best == 0 || time < best) {
+                best = time;
+                p.rows = rows;
+                p.k_split = (int32_t)k_split;
+            }
         }
-    }
-    p.k_split = (int32_t)pad(ceil_div(p.piece, best), kStepK);
-    p.splits = (int32_t)ceil_div(V < p.piece ? V : p.piece, p.k_split);  // of the first piece; later ones add to them
+    };
+    if (rows_dz <= 16) look(Shape16{}, 16);
+    if (rows_dz <= 512) look(Shape64{}, 64);
+    look(Shape128{}, 128);
+    look(Shape256{}, 256);
+    p.rows_pad = (int32_t)pad(rows_dz, std::max(std::max(p.rows, p.logits_rows), (int)kStepK));
+    p.splits = (int32_t)ceil_div(first, p.k_split);  // of the first piece; later ones add to them
     p.sums_ld = (int32_t)pad(D, 4);
     p.direct_out = pieces == 1 && p.splits == 1 && p.parts == 1;
     return p;
