@@ -9,6 +9,11 @@
 // every row and the sum of exponentials against that maximum, and a second kernel joins them.  Backward: the logits are made
 // again, for a piece of the vocabulary at a time, turned into dz in the accumulators, and stored in 16 bits; the two products
 // that read the piece follow while it is in the last-level cache.  All sums are fp32.
+//
+// What bounds it: with many rows the matrix cores.  Tiles of 256 x 256 by four waves, whose sums are in the 256 accumulation registers
+// of each, need 64 KB of operands for every 8.4 MFLOP; loss of 2,048 x 128,256 x 2,048 860 us, 1.25 PFLOP/s, as a large library
+// product of that shape (1.23).  With few rows it is reading the weights (one row of 32,000 x 2,048: 6.1 TB/s from the caches, the
+// rest of the call's 40 us three launches and the host), with small sizes the chain of launches, 4 to 14 us each.
 
 #include <algorithm>
 
@@ -98,7 +103,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
         const int32_t v_first = a.v0 + first;
         const bool masked = a.masks.bits || v_first + S::TM > a.V;
         // What belongs to the rows is asked for before the first of it is used: a load from memory takes as long as hundreds of
-        // the elements' instructions (with a wait for each row in turn a tile of 777 x 50,003 x 1,000 took 43 us, 25 of them products).
+        // the elements' instructions (with a wait for each row in turn dz of 777 x 50,003 x 1,000 took 191 us for 174).
         constexpr int kWords = (S::TM + 31) / 32;
         const int32_t k_first = v_first >> 5;
         uint32_t words[S::FN][kWords];
@@ -189,7 +194,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
                             if (mark == 16 * i.value + r.value && acc[i.value][j][r.value] > -kInf) d[r.value] -= grad;
                         });
                     }
-                    *reinterpret_cast<u32x2 *>(out + (i.value / 4) * (a.dz_rows * 64) + i.value % 4 * 16) = round4<T>(d);
+                    *reinterpret_cast<u32x2 *>(out + (i.value / 4) * (a.dz_rows * 64) + i.value % 4 * 16) = round4<Fp16>(d);
                 });
             }
         });
@@ -281,11 +286,14 @@ struct Rows {
     }
 };
 
-__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale) {
+__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale, uint32_t *largest) {
     __shared__ float shared[16];
     const float factor = rows.scale(shared);
     for (int32_t i = threadIdx.x; i < rows.N; i += 1024) scaled[i] = rows.grad(i) * factor;
-    if (threadIdx.x == 0) *unscale = 1.0f / factor;
+    if (threadIdx.x == 0) {
+        *unscale = 1.0f / factor;
+        largest[0] = largest[1] = 0;
+    }
 }
 
 // dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
@@ -362,6 +370,60 @@ __device__ __forceinline__ void store4(uint16_t *row, int32_t c, int32_t n, f32x
     }
 }
 
+// The largest finite |x| of bf16 rows as its bits; a wave takes a row at a time.
+__global__ __launch_bounds__(256) void largest_kernel(const uint16_t *x, int64_t x_ld, int64_t R, int32_t D, uint32_t *largest) {
+    const int lane = threadIdx.x % kWave;
+    uint32_t most = 0;
+    auto take = [&](uint32_t bits) {
+        bits &= 0x7FFFu;
+        most = bits > most && bits < 0x7F80u ? bits : most;
+    };
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < R; row += (int64_t)gridDim.x * 4) {
+        const uint16_t *const p = x + row * x_ld;
+        for (int32_t c = lane * 8; c < D; c += kWave * 8) {
+            if (c + 8 <= D) {
+                const u32x4 v = *reinterpret_cast<const u32x4_any *>(p + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) take(v[j]), take(v[j] >> 16);
+            } else {
+                for (int32_t j = c; j < D; ++j) take(p[j]);
+            }
+        }
+    }
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t other = __shfl_xor(most, d);
+        most = other > most ? other : most;
+    }
+    if (lane == 0 && most) atomicMax(largest, most);  // (the same in any order)
+}
+
+// bf16 rows as fp16, times the power of two that brings the largest below 2^15: what lies within 2^32 of the largest keeps its eight
+// bits, the rest is 2^-40 of the largest or less off.  Rows of y_ld elements, zeros behind D and from row R on.  Leaves the
+// factor's inverse times `before` in `unscale`.
+__global__ __launch_bounds__(256) void halves_kernel(const uint16_t *x, int64_t x_ld, int32_t R, int32_t D, const uint32_t *largest,
+                                                     uint16_t *y, int32_t y_ld, int32_t all, const float *before, float *unscale) {
+    const int32_t e = (int32_t)(*largest >> 7) - 127;  // 2^e <= the largest < 2^(e + 1)
+    const int32_t k = 14 - e < 126 ? 14 - e : 126;
+    const float factor = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = *before * __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
+    const int32_t units = y_ld / 8;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (int64_t)all * units) return;
+    const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 8;
+    u32x4 v = {0, 0, 0, 0};
+    if (row < R) {
+        const uint16_t *const p = x + row * x_ld + c;
+        if (c + 8 <= D) {
+            v = *reinterpret_cast<const u32x4_any *>(p);
+        } else {
+            for (int j = 0; c + j < D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = Fp16::round2(Bf16::value((uint16_t)v[j]) * factor, Bf16::value((uint16_t)(v[j] >> 16)) * factor);
+    *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = v;
+}
+
 struct GradArgs {
     Operand A, B;  // A: m = hidden size; B: n = rows (grad_hidden) or tokens (grad_weight)
     int32_t n, D;  // extents of the result
@@ -376,7 +438,8 @@ struct GradArgs {
 };
 
 // grad_hidden: A = weight by columns, B = dz by rows.  grad_weight: A = hidden, B = dz, both by columns.
-template <typename T, typename S, bool DIRECT, bool B_COLUMNS>
+// T: the operands' type, O: the results'.
+template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS>
 __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     // (weights end where the vocabulary does; hidden states and dz go on with zeros)
     using TileA = Tile<S::BM, S::kThreads, true, DIRECT, B_COLUMNS ? PADDED : ZERO>;
@@ -411,7 +474,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
                     f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
                     *p = a.add ? *p + acc[i.value][j.value] : acc[i.value][j.value];
                 } else {
-                    store4<T>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale);
+                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale);
                 }
             });
         });
@@ -419,6 +482,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
 }
 
+// Joins grad_hidden's shares of the sum (and the two numbers of few rows' dz).
 template <typename T>
 __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
                                                      const float *unscale, uint16_t *out, int64_t out_ld) {
@@ -491,7 +555,7 @@ Plan plan_of(int32_t N, int32_t V, int32_t D) {
             const double shares = s > 1 || pieces > 1 || p.parts > 1 ? 4.0 + (double)s * rows_dz * D * 8.0 / 4e6 : 0.0;
             const double tiles_time = (double)ceil_div(tiles * s, slots<S>()) * ((double)(k_split / kStepK) * kStepTime<S> + kEndsTime<S>);
             // (or reading the weights, which rows of several tiles read more than once, partly from the caches)
-            const double time = std::max(tiles_time, (double)first * D * 2.0 / 4.5e6 * (0.5 + 0.5 * (double)ceil_div(rows_dz, S::BN))) + shares;
+            const double time = std::max(tiles_time, (double)first * D * 2.0 / 4.5e6 * (0.5 + 0.5 * (double)ceil_div(rows_dz, S::BN)) * (D % 8 ? 2 : 1)) + shares;
             if (best == 0 || time < best) {
                 best = time;
                 p.rows = rows;
@@ -580,34 +644,34 @@ int launch_logits(int rows, LogitsArgs a, int32_t tokens, bool direct, hipStream
     }
 }
 
-template <typename T, typename S, bool DIRECT, bool B_COLUMNS>
+template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS>
 int launch_grad_of(GradArgs a, hipStream_t stream) {
     a.tiles_m = (int32_t)ceil_div(a.D, S::BM);
     a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
     const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = work < slots<S>() ? work : slots<S>();
     if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
-    hipLaunchKernelGGL((grad_kernel<T, S, DIRECT, B_COLUMNS>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
+    hipLaunchKernelGGL((grad_kernel<T, O, S, DIRECT, B_COLUMNS>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
     return check_launch();
 }
 
-template <typename T, bool DIRECT>
+template <typename T, typename O, bool DIRECT>
 int launch_grad_hidden(int rows, const GradArgs &a, hipStream_t stream) {
     switch (rows) {
-        case 16: return launch_grad_of<T, Shape16, DIRECT, false>(a, stream);
-        case 64: return launch_grad_of<T, Shape64, DIRECT, false>(a, stream);
-        case 128: return launch_grad_of<T, Shape128, DIRECT, false>(a, stream);
-        default: return launch_grad_of<T, Shape256, DIRECT, false>(a, stream);
+        case 16: return launch_grad_of<T, O, Shape16, DIRECT, false>(a, stream);
+        case 64: return launch_grad_of<T, O, Shape64, DIRECT, false>(a, stream);
+        case 128: return launch_grad_of<T, O, Shape128, DIRECT, false>(a, stream);
+        default: return launch_grad_of<T, O, Shape256, DIRECT, false>(a, stream);
     }
 }
 
-template <typename T>
+template <typename T, typename O>
 int launch_grad_weight(const GradArgs &a, hipStream_t stream) {
     const int32_t steps = (int32_t)ceil_div(a.k, kStepK);
     const double large = time_of<Shape256>(a.D, a.n, steps), middle = time_of<Shape128>(a.D, a.n, steps),
                  flat = time_of<ShapeFlat>(a.D, a.n, steps), small = time_of<Shape64>(a.D, a.n, steps);
-    if (large <= middle && large <= flat && large <= small) return launch_grad_of<T, Shape256, true, true>(a, stream);
-    if (flat <= middle && flat <= small) return launch_grad_of<T, ShapeFlat, true, true>(a, stream);
-    return middle <= small ? launch_grad_of<T, Shape128, true, true>(a, stream) : launch_grad_of<T, Shape64, true, true>(a, stream);
+    if (large <= middle && large <= flat && large <= small) return launch_grad_of<T, O, Shape256, true, true>(a, stream);
+    if (flat <= middle && flat <= small) return launch_grad_of<T, O, ShapeFlat, true, true>(a, stream);
+    return middle <= small ? launch_grad_of<T, O, Shape128, true, true>(a, stream) : launch_grad_of<T, O, Shape64, true, true>(a, stream);
 }
 
 int copy_rows(const LossCall &c, int32_t times, int32_t all, bool whole, const Rows &rows, uint16_t *y, int32_t y_ld,
@@ -663,11 +727,18 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     Masks masks;
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
     const bool few = p.parts == 2;
+    // Of many rows dz is fp16, whose eleven bits leave a gradient as near to the truth as its own rounding does: in bf16 its largest
+    // element, the target's, was off by as much as all of that.  The products' other sides, where they are bf16, become fp16 too.
+    constexpr bool kBf16 = std::is_same_v<T, Bf16>;
+    const bool halves = kBf16 && !few;
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
-    float *unscale = ws.take<float>(1);
+    float *unscale = ws.take<float>(3);  // of dz; with weights; with hidden states
+    uint32_t *largest = ws.take<uint32_t>(2);
     float *scaled = few ? nullptr : ws.take<float>(c.N);
-    const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK);
+    const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK), w_pad = (int32_t)pad(c.D, 8);
     uint16_t *copy = ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad);
+    uint16_t *copy16 = halves ? ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad) : copy;
+    uint16_t *weight16 = halves ? ws.take<uint16_t>((size_t)std::min(p.piece, c.V) * w_pad) : nullptr;
     uint16_t *dz = ws.take<uint16_t>((size_t)p.rows_pad * p.piece);
     float *sums = ws.take<float>((size_t)p.splits * rows_dz * p.sums_ld);
     float *z = few ? ws.take<float>((size_t)c.N * p.piece) : nullptr;
@@ -675,10 +746,31 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     if (!launch) return CFGZIP_OK;
     const Rows rows{grad_loss, c.target, c.N, c.V, masks};
     if (!few) {
-        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale);
+        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale, largest);
         CFGZIP_TRY(check_launch());
     }
     CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
+    const float *unscale_hidden = unscale, *unscale_weight = unscale;  // of the two gradients
+    auto to_halves = [&](const uint16_t *x, int64_t ld, int32_t n, int32_t D, int32_t all, const uint32_t *most, uint16_t *y, int32_t y_ld,
+                         float *to) {
+        hipLaunchKernelGGL(halves_kernel, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 256)), dim3(256), 0, stream, x, ld, n, D, most, y,
+                           y_ld, all, unscale, to);
+        return check_launch();
+    };
+    if (halves && grad_weight) {
+        const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(c.N, 4), 2048);
+        hipLaunchKernelGGL(largest_kernel, dim3(grid), dim3(256), 0, stream, copy, (int64_t)p.d_pad, (int64_t)c.N, c.D, largest);
+        CFGZIP_TRY(check_launch());
+        CFGZIP_TRY(to_halves(copy, p.d_pad, c.N, c.D, copy_rows_pad, largest, copy16, p.d_pad, unscale + 2));
+        unscale_weight = unscale + 2;
+    }
+    if (halves && grad_hidden) {
+        const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(c.V, 4), 2048);
+        hipLaunchKernelGGL(largest_kernel, dim3(grid), dim3(256), 0, stream, static_cast<const uint16_t *>(c.weight), c.weight_stride,
+                           (int64_t)c.V, c.D, largest + 1);
+        CFGZIP_TRY(check_launch());
+        unscale_hidden = unscale + 1;
+    }
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
     for (int64_t v0 = 0; v0 < c.V; v0 += p.piece) {
@@ -712,41 +804,46 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         }
         if (grad_hidden) {
             GradArgs g{};
-            g.A = by_columns(first, c.weight_stride, c.D);
+            g.A = halves ? by_columns(weight16, w_pad, w_pad) : by_columns(first, c.weight_stride, c.D);
             g.B = Operand{dz, 64, 64, (int64_t)p.rows_pad * 64, p.rows_pad};
             g.n = rows_dz;
             g.D = c.D;
             g.k = tokens;
             g.k_split = p.k_split;
-            g.unscale = unscale;
+            g.unscale = unscale_hidden;
             g.out = grad_hidden;
             g.out_ld = gh_stride;
             g.sums = p.direct_out ? nullptr : sums;
             g.sums_ld = p.sums_ld;
             g.add = v0 > 0;
             g.splits = (int32_t)ceil_div(tokens, p.k_split);
-            CFGZIP_TRY(direct ? (launch_grad_hidden<T, true>(p.rows, g, stream))
-                              : (launch_grad_hidden<T, false>(p.rows, g, stream)));
+            if (halves) {
+                CFGZIP_TRY(to_halves(first, c.weight_stride, tokens, c.D, tokens, largest + 1, weight16, w_pad, unscale + 1));
+                CFGZIP_TRY((launch_grad_hidden<Fp16, T, true>(p.rows, g, stream)));
+            } else {
+                CFGZIP_TRY(direct ? (launch_grad_hidden<T, T, true>(p.rows, g, stream))
+                                  : (launch_grad_hidden<T, T, false>(p.rows, g, stream)));
+            }
         }
         if (grad_weight) {
             GradArgs g{};
-            g.A = by_columns(copy, p.d_pad, p.d_pad);
+            g.A = by_columns(copy16, p.d_pad, p.d_pad);
             g.B = Operand{dz, 64, (int64_t)p.rows_pad * 64, kStepK * 64, p.piece};
             g.n = tokens;
             g.D = c.D;
             g.k = rows_dz;
             g.k_split = (int32_t)pad(rows_dz, kStepK);
             g.splits = 1;
-            g.unscale = unscale;
+            g.unscale = unscale_weight;
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
-            CFGZIP_TRY(launch_grad_weight<T>(g, stream));
+            CFGZIP_TRY(halves ? (launch_grad_weight<Fp16, T>(g, stream)) : (launch_grad_weight<T, T>(g, stream)));
         }
     }
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
         hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, sums, p.splits * p.parts, c.N,
-                           c.D, p.sums_ld, unscale, grad_hidden, gh_stride);
+                           c.D, p.sums_ld, unscale_hidden, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }
     return CFGZIP_OK;
