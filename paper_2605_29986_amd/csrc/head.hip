@@ -286,14 +286,11 @@ struct Rows {
     }
 };
 
-__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale, uint32_t *largest) {
+__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale) {
     __shared__ float shared[16];
     const float factor = rows.scale(shared);
     for (int32_t i = threadIdx.x; i < rows.N; i += 1024) scaled[i] = rows.grad(i) * factor;
-    if (threadIdx.x == 0) {
-        *unscale = 1.0f / factor;
-        largest[0] = largest[1] = 0;
-    }
+    if (threadIdx.x == 0) *unscale = 1.0f / factor;
 }
 
 // dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
@@ -370,58 +367,97 @@ __device__ __forceinline__ void store4(uint16_t *row, int32_t c, int32_t n, f32x
     }
 }
 
-// The largest finite |x| of bf16 rows as its bits; a wave takes a row at a time.
-__global__ __launch_bounds__(256) void largest_kernel(const uint16_t *x, int64_t x_ld, int64_t R, int32_t D, uint32_t *largest) {
-    const int lane = threadIdx.x % kWave;
+// The largest finite |x| of bf16 rows as its bits, of two matrices in one launch: workgroup b leaves that of the rows it took in
+// largest[b], of the first matrix in kLargestFirst of them.  A wave takes a row at a time.  (One word and atomic maxima took 250 us for
+// 128,256 x 4,096: as many waves, one after the other.)
+constexpr int kLargestFirst = 1024, kLargestSecond = 256;
+struct Bf16Rows {
+    const uint16_t *x;
+    int64_t ld;
+    int32_t rows, D;
+};
+__global__ __launch_bounds__(256) void largest_kernel(Bf16Rows first, Bf16Rows second, uint32_t *largest) {
+    __shared__ uint32_t shared[4];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const bool in_first = blockIdx.x < kLargestFirst;
+    const Bf16Rows &m = in_first ? first : second;
+    const int32_t block = in_first ? blockIdx.x : blockIdx.x - kLargestFirst, blocks = in_first ? kLargestFirst : kLargestSecond;
     uint32_t most = 0;
     auto take = [&](uint32_t bits) {
         bits &= 0x7FFFu;
         most = bits > most && bits < 0x7F80u ? bits : most;
     };
-    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < R; row += (int64_t)gridDim.x * 4) {
-        const uint16_t *const p = x + row * x_ld;
-        for (int32_t c = lane * 8; c < D; c += kWave * 8) {
-            if (c + 8 <= D) {
-                const u32x4 v = *reinterpret_cast<const u32x4_any *>(p + c);
+    constexpr int kUnits = 8;  // on their way at a time
+    for (int64_t row = (int64_t)block * 4 + wave; row < m.rows; row += (int64_t)blocks * 4) {
+        const uint16_t *const p = m.x + row * m.ld;
+        for (int32_t c = lane * 8; c < m.D; c += kWave * 8 * kUnits) {
+            u32x4 v[kUnits];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) take(v[j]), take(v[j] >> 16);
-            } else {
-                for (int32_t j = c; j < D; ++j) take(p[j]);
+            for (int i = 0; i < kUnits; ++i) {
+                const int32_t at = c + i * kWave * 8;
+                v[i] = u32x4{0, 0, 0, 0};
+                if (at + 8 <= m.D) {
+                    v[i] = *reinterpret_cast<const u32x4_any *>(p + at);
+                } else {
+                    for (int32_t j = at; j < m.D; ++j) take(p[j]);
+                }
             }
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) take(v[i][j]), take(v[i][j] >> 16);
         }
     }
     for (int d = 1; d < kWave; d *= 2) {
         const uint32_t other = __shfl_xor(most, d);
         most = other > most ? other : most;
     }
-    if (lane == 0 && most) atomicMax(largest, most);  // (the same in any order)
+    if (lane == 0) shared[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 4; ++i) most = shared[i] > most ? shared[i] : most;
+        largest[blockIdx.x] = most;
+    }
 }
 
-// bf16 rows as fp16, times the power of two that brings the largest below 2^15: what lies within 2^32 of the largest keeps its eight
-// bits, the rest is 2^-40 of the largest or less off.  Rows of y_ld elements, zeros behind D and from row R on.  Leaves the
-// factor's inverse times `before` in `unscale`.
-__global__ __launch_bounds__(256) void halves_kernel(const uint16_t *x, int64_t x_ld, int32_t R, int32_t D, const uint32_t *largest,
-                                                     uint16_t *y, int32_t y_ld, int32_t all, const float *before, float *unscale) {
-    const int32_t e = (int32_t)(*largest >> 7) - 127;  // 2^e <= the largest < 2^(e + 1)
+// bf16 rows as fp16, times the power of two that brings the largest of the `count` (1,024 or 256) below 2^15: what lies within 2^32 of the
+// largest keeps its eight bits, the rest is 2^-40 of the largest or less off.  Rows of y_ld elements, zeros behind D and from
+// row R on.  Leaves the factor's inverse times `before` in `unscale`.  A thread has four units of eight.
+__global__ __launch_bounds__(256) void halves_kernel(Bf16Rows x, const uint32_t *largest, int32_t count, uint16_t *y, int32_t y_ld, int32_t all,
+                                                     const float *before, float *unscale) {
+    __shared__ uint32_t shared[4];
+    uint32_t most = 0;
+    for (int32_t i = threadIdx.x; i < count; i += 256) most = largest[i] > most ? largest[i] : most;
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t other = __shfl_xor(most, d);
+        most = other > most ? other : most;
+    }
+    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
+    __syncthreads();
+    for (int i = 0; i < 4; ++i) most = shared[i] > most ? shared[i] : most;
+    const int32_t e = (int32_t)(most >> 7) - 127;  // 2^e <= the largest < 2^(e + 1)
     const int32_t k = 14 - e < 126 ? 14 - e : 126;
     const float factor = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
     if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = *before * __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
     const int32_t units = y_ld / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)all * units) return;
-    const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 8;
-    u32x4 v = {0, 0, 0, 0};
-    if (row < R) {
-        const uint16_t *const p = x + row * x_ld + c;
-        if (c + 8 <= D) {
-            v = *reinterpret_cast<const u32x4_any *>(p);
-        } else {
-            for (int j = 0; c + j < D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
-        }
-    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = Fp16::round2(Bf16::value((uint16_t)v[j]) * factor, Bf16::value((uint16_t)(v[j] >> 16)) * factor);
-    *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = v;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t at = ((int64_t)blockIdx.x * 4 + i) * 256 + threadIdx.x;
+        if (at >= (int64_t)all * units) break;
+        const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 8;
+        u32x4 v = {0, 0, 0, 0};
+        if (row < x.rows) {
+            const uint16_t *const p = x.x + row * x.ld + c;
+            if (c + 8 <= x.D) {
+                v = *reinterpret_cast<const u32x4_any *>(p);
+            } else {
+                for (int j = 0; c + j < x.D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = Fp16::round2(Bf16::value((uint16_t)v[j]) * factor, Bf16::value((uint16_t)(v[j] >> 16)) * factor);
+        *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = v;
+    }
 }
 
 struct GradArgs {
@@ -733,7 +769,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     const bool halves = kBf16 && !few;
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
     float *unscale = ws.take<float>(3);  // of dz; with weights; with hidden states
-    uint32_t *largest = ws.take<uint32_t>(2);
+    uint32_t *largest = ws.take<uint32_t>(kLargestFirst + kLargestSecond);  // of the weights, of the hidden states
     float *scaled = few ? nullptr : ws.take<float>(c.N);
     const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK), w_pad = (int32_t)pad(c.D, 8);
     uint16_t *copy = ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad);
@@ -746,30 +782,24 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     if (!launch) return CFGZIP_OK;
     const Rows rows{grad_loss, c.target, c.N, c.V, masks};
     if (!few) {
-        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale, largest);
+        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale);
         CFGZIP_TRY(check_launch());
     }
     CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
     const float *unscale_hidden = unscale, *unscale_weight = unscale;  // of the two gradients
-    auto to_halves = [&](const uint16_t *x, int64_t ld, int32_t n, int32_t D, int32_t all, const uint32_t *most, uint16_t *y, int32_t y_ld,
-                         float *to) {
-        hipLaunchKernelGGL(halves_kernel, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 256)), dim3(256), 0, stream, x, ld, n, D, most, y,
+    auto to_halves = [&](const Bf16Rows &x, int32_t all, const uint32_t *most, int32_t many, uint16_t *y, int32_t y_ld, float *to) {
+        hipLaunchKernelGGL(halves_kernel, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, most, many, y,
                            y_ld, all, unscale, to);
         return check_launch();
     };
-    if (halves && grad_weight) {
-        const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(c.N, 4), 2048);
-        hipLaunchKernelGGL(largest_kernel, dim3(grid), dim3(256), 0, stream, copy, (int64_t)p.d_pad, (int64_t)c.N, c.D, largest);
+    if (halves) {
+        const Bf16Rows w{static_cast<const uint16_t *>(c.weight), c.weight_stride, grad_hidden ? c.V : 0, c.D};
+        const Bf16Rows h{copy, p.d_pad, c.N, c.D};
+        hipLaunchKernelGGL(largest_kernel, dim3(kLargestFirst + kLargestSecond), dim3(256), 0, stream, w, h, largest);
         CFGZIP_TRY(check_launch());
-        CFGZIP_TRY(to_halves(copy, p.d_pad, c.N, c.D, copy_rows_pad, largest, copy16, p.d_pad, unscale + 2));
-        unscale_weight = unscale + 2;
-    }
-    if (halves && grad_hidden) {
-        const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(c.V, 4), 2048);
-        hipLaunchKernelGGL(largest_kernel, dim3(grid), dim3(256), 0, stream, static_cast<const uint16_t *>(c.weight), c.weight_stride,
-                           (int64_t)c.V, c.D, largest + 1);
-        CFGZIP_TRY(check_launch());
+        if (grad_weight) CFGZIP_TRY(to_halves(h, copy_rows_pad, largest + kLargestFirst, kLargestSecond, copy16, p.d_pad, unscale + 2));
         unscale_hidden = unscale + 1;
+        unscale_weight = unscale + 2;
     }
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
@@ -818,7 +848,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.add = v0 > 0;
             g.splits = (int32_t)ceil_div(tokens, p.k_split);
             if (halves) {
-                CFGZIP_TRY(to_halves(first, c.weight_stride, tokens, c.D, tokens, largest + 1, weight16, w_pad, unscale + 1));
+                const Bf16Rows w{first, c.weight_stride, tokens, c.D};
+                CFGZIP_TRY(to_halves(w, tokens, largest, kLargestFirst, weight16, w_pad, unscale + 1));
                 CFGZIP_TRY((launch_grad_hidden<Fp16, T, true>(p.rows, g, stream)));
             } else {
                 CFGZIP_TRY(direct ? (launch_grad_hidden<T, T, true>(p.rows, g, stream))
