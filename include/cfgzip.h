@@ -463,9 +463,8 @@ int cfgzip_nfa_advance_states(const int32_t *rel_rep, int32_t C, int32_t S,
  * Rows whose target is none or not admitted (no step lowers an infinite loss), and rows whose grad_loss is 0, have dz = 0
  * whatever their hidden states hold.  The weights have to be finite, those of masked tokens too.
  *   grad_hidden, grad_weight   out, [N] and [V] rows of D elements of the inputs' type; either may be NULL
- * dz is kept in fp16 (up to 128 rows: as the sum of two numbers of the inputs' type) for a piece of the vocabulary at a time, beside
- * bf16 operands that are brought to fp16 by a power of two (what is below 2^-32 of the largest loses bits); all sums are fp32, and
- * nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
+ * dz is kept in fp16 for a piece of the vocabulary at a time, beside bf16 operands that are brought to fp16 by a power of two (what
+ * is below 2^-32 of the largest loses bits); of few rows, up to 128 or 256, as the sum of two numbers of the inputs' type.  All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
  */
 size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);
 int cfgzip_head_loss(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,

@@ -48,8 +48,11 @@ double time_of(int64_t m, int64_t n, int64_t steps) {
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time: the size of the last-level cache
 // Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum instead of lse, which
 // large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
-// than the products, which are twice as many.
-constexpr int32_t kFewRows = 128;
+// than the products, which are twice as many.  With more rows dz is one fp16 number, for which bf16 weights are read and written once
+// more: 200 rows of 32,000 x 2,048 take 361 us so and 304 as two numbers (50,003 x 333, whose rows lie at no multiples of 16 bytes
+// until they are fp16, 213 and 292).
+template <typename T>
+int32_t few_rows_of(int32_t D) { return std::is_same_v<T, Bf16> && D % 8 == 0 ? 256 : 128; }
 constexpr int32_t kPieceLeast = 2048;              // columns
 constexpr int32_t kSplitLeast = 256;               // of the sum over the vocabulary: the steps that a workgroup takes at the least
 constexpr int32_t kMaxRows = 1 << 22;               // offsets in a tile of dz stay below 2^32
@@ -422,9 +425,9 @@ __global__ __launch_bounds__(256) void largest_kernel(Bf16Rows first, Bf16Rows s
 
 // bf16 rows as fp16, times the power of two that brings the largest of the `count` (1,024 or 256) below 2^15: what lies within 2^32 of the
 // largest keeps its eight bits, the rest is 2^-40 of the largest or less off.  Rows of y_ld elements, zeros behind D and from
-// row R on.  Leaves the factor's inverse times `before` in `unscale`.  A thread has four units of eight.
+// row R on.  Leaves the factor's inverse in `unscale`.  A thread has four units of eight.
 __global__ __launch_bounds__(256) void halves_kernel(Bf16Rows x, const uint32_t *largest, int32_t count, uint16_t *y, int32_t y_ld, int32_t all,
-                                                     const float *before, float *unscale) {
+                                                     float *unscale) {
     __shared__ uint32_t shared[4];
     uint32_t most = 0;
     for (int32_t i = threadIdx.x; i < count; i += 256) most = largest[i] > most ? largest[i] : most;
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(256) void halves_kernel(Bf16Rows x, const uint32_t 
     const int32_t e = (int32_t)(most >> 7) - 127;  // 2^e <= the largest < 2^(e + 1)
     const int32_t k = 14 - e < 126 ? 14 - e : 126;
     const float factor = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = *before * __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
     const int32_t units = y_ld / 8;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -465,7 +468,7 @@ struct GradArgs {
     int32_t n, D;  // extents of the result
     int32_t k, k_split, splits;
     int32_t tiles_m, tiles_n;
-    const float *unscale;
+    const float *unscale, *unscale16;  // of dz; of the other operand or null (their product alone may be too small for fp32)
     uint16_t *out;  // [n][out_ld]
     int64_t out_ld;
     float *sums;  // [splits][n][sums_ld], sums_ld = D rounded up to 4; null: the result goes to `out` at once
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
         int32_t tm = 0, tn = 0, split = 0;
         place(i, tm, tn, split);
-        const float unscale = *a.unscale;
+        const float unscale = *a.unscale, unscale16 = a.unscale16 ? *a.unscale16 : 1.0f;
         each<S::FN>([&](auto j) CFGZIP_INLINE {
             const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
             if (n >= a.n) return;
@@ -510,7 +513,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
                     f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
                     *p = a.add ? *p + acc[i.value][j.value] : acc[i.value][j.value];
                 } else {
-                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale);
+                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale * unscale16);
                 }
             });
         });
@@ -521,12 +524,12 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
 // Joins grad_hidden's shares of the sum (and the two numbers of few rows' dz).
 template <typename T>
 __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
-                                                     const float *unscale, uint16_t *out, int64_t out_ld) {
+                                                         const float *unscale, const float *unscale16, uint16_t *out, int64_t out_ld) {
     const int32_t units = sums_ld / 4;
     const int64_t k = (int64_t)blockIdx.x * kWave + threadIdx.x;
     if (k >= (int64_t)n * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 4;
-    const float factor = *unscale;
+    const float factor = *unscale, factor16 = unscale16 ? *unscale16 : 1.0f;
     const float *p = sums + (int64_t)row * sums_ld + c;
     const int64_t step = (int64_t)n * sums_ld;
     f32x4 x = {0, 0, 0, 0};
@@ -537,7 +540,7 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_
 #pragma unroll
         for (int i = 0; i < 16; ++i) x += y[i];
     }
-    store4<T>(out + row * out_ld, c, D, x * factor);
+    store4<T>(out + row * out_ld, c, D, x * factor * factor16);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
@@ -569,10 +572,10 @@ struct Plan {
     bool direct_out;    // grad_hidden in one go
 };
 
-Plan plan_of(int32_t N, int32_t V, int32_t D) {
+Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows) {
     Plan p{};
-    p.logits_rows = rows_of_tile(N);
-    p.parts = N <= kFewRows ? 2 : 1;
+    p.parts = N <= few_rows ? 2 : 1;
+    p.logits_rows = p.parts == 2 ? std::min(rows_of_tile(N), 128) : rows_of_tile(N);
     p.d_pad = (int32_t)pad(D, kStepK);
     const int32_t rows_dz = N * p.parts;
     // (tiles of logits leave zeros behind N as well, and grad_weight's sum goes over whole steps of rows)
@@ -759,7 +762,7 @@ int forward(const LossCall &c, float *loss, float *lse, Carver &ws, hipStream_t 
 template <typename T>
 int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16_t *grad_hidden, int64_t gh_stride,
              uint16_t *grad_weight, int64_t gw_stride, Carver &ws, hipStream_t stream, bool launch) {
-    const Plan p = plan_of(c.N, c.V, c.D);
+    const Plan p = plan_of(c.N, c.V, c.D, few_rows_of<T>(c.D));
     Masks masks;
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
     const bool few = p.parts == 2;
@@ -768,7 +771,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
     const bool halves = kBf16 && !few;
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
-    float *unscale = ws.take<float>(3);  // of dz; with weights; with hidden states
+    float *unscale = ws.take<float>(3);  // of dz; of weights in fp16; of hidden states in fp16
     uint32_t *largest = ws.take<uint32_t>(kLargestFirst + kLargestSecond);  // of the weights, of the hidden states
     float *scaled = few ? nullptr : ws.take<float>(c.N);
     const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK), w_pad = (int32_t)pad(c.D, 8);
@@ -786,10 +789,10 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         CFGZIP_TRY(check_launch());
     }
     CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
-    const float *unscale_hidden = unscale, *unscale_weight = unscale;  // of the two gradients
+    const float *unscale_w = nullptr, *unscale_h = nullptr;
     auto to_halves = [&](const Bf16Rows &x, int32_t all, const uint32_t *most, int32_t many, uint16_t *y, int32_t y_ld, float *to) {
         hipLaunchKernelGGL(halves_kernel, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, most, many, y,
-                           y_ld, all, unscale, to);
+                           y_ld, all, to);
         return check_launch();
     };
     if (halves) {
@@ -798,8 +801,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         hipLaunchKernelGGL(largest_kernel, dim3(kLargestFirst + kLargestSecond), dim3(256), 0, stream, w, h, largest);
         CFGZIP_TRY(check_launch());
         if (grad_weight) CFGZIP_TRY(to_halves(h, copy_rows_pad, largest + kLargestFirst, kLargestSecond, copy16, p.d_pad, unscale + 2));
-        unscale_hidden = unscale + 1;
-        unscale_weight = unscale + 2;
+        unscale_w = unscale + 1;
+        unscale_h = unscale + 2;
     }
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
@@ -840,7 +843,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.D = c.D;
             g.k = tokens;
             g.k_split = p.k_split;
-            g.unscale = unscale_hidden;
+            g.unscale = unscale;
+            g.unscale16 = unscale_w;
             g.out = grad_hidden;
             g.out_ld = gh_stride;
             g.sums = p.direct_out ? nullptr : sums;
@@ -865,7 +869,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.k = rows_dz;
             g.k_split = (int32_t)pad(rows_dz, kStepK);
             g.splits = 1;
-            g.unscale = unscale_weight;
+            g.unscale = unscale;
+            g.unscale16 = unscale_h;
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
             CFGZIP_TRY(halves ? (launch_grad_weight<Fp16, T>(g, stream)) : (launch_grad_weight<T, T>(g, stream)));
@@ -874,7 +879,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
         hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, sums, p.splits * p.parts, c.N,
-                           c.D, p.sums_ld, unscale_hidden, grad_hidden, gh_stride);
+                           c.D, p.sums_ld, unscale, unscale_w, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }
     return CFGZIP_OK;
@@ -898,9 +903,10 @@ extern "C" size_t cfgzip_head_loss_grad_workspace_bytes(int32_t N, int32_t V, in
     if (N <= 0 || V <= 0 || D <= 0 || N > kMaxRows || V > 0x7FFFFC00 || D >= kMaxStride - 8 || !kind_ok(bits_kind)) return 0;
     LossCall c{};
     c.N = N, c.V = V, c.D = D, c.bits_kind = bits_kind;
-    Carver ws(nullptr);
-    backward<Bf16>(c, nullptr, nullptr, nullptr, 0, nullptr, 0, ws, nullptr, false);
-    return ws.used;
+    Carver bf16(nullptr), fp16(nullptr);  // (the call's type is not asked for: the larger)
+    backward<Bf16>(c, nullptr, nullptr, nullptr, 0, nullptr, 0, bf16, nullptr, false);
+    backward<Fp16>(c, nullptr, nullptr, nullptr, 0, nullptr, 0, fp16, nullptr, false);
+    return std::max(bf16.used, fp16.used);
 }
 
 extern "C" int cfgzip_head_loss(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
