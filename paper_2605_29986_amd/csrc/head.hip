@@ -52,7 +52,7 @@ constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time:
 // more: 200 rows of 32,000 x 2,048 take 361 us so and 304 as two numbers (50,003 x 333, whose rows lie at no multiples of 16 bytes
 // until they are fp16, 213 and 292).
 template <typename T>
-int32_t few_rows_of(int32_t D) { return std::is_same_v<T, Bf16> && D % 8 == 0 ? 256 : 128; }
+int32_t few_rows_of(int32_t D) { return std::is_same_v<T, Bf16> && D % 8 ? 128 : 256; }
 constexpr int32_t kPieceLeast = 2048;              // columns
 constexpr int32_t kSplitLeast = 256;               // of the sum over the vocabulary: the steps that a workgroup takes at the least
 constexpr int32_t kMaxRows = 1 << 22;               // offsets in a tile of dz stay below 2^32
