@@ -8,7 +8,7 @@
 // Forward: a tile of logits stays in the accumulators of the product that makes it; each wave leaves the maximum of its part of
 // every row and the sum of exponentials against that maximum, and a second kernel joins them.  Backward: the logits are made
 // again, for a piece of the vocabulary at a time, turned into dz in the accumulators, and stored in 16 bits; the two products
-// that read the piece follow while it is in the last-level cache.  All sums are fp32.
+// that read the piece follow, where it is one of several while most of it is in the last-level cache.  All sums are fp32.
 //
 // What bounds it: with many rows the matrix cores.  Tiles of 256 x 256 by four waves, whose sums are in the 256 accumulation registers
 // of each, need 64 KB of operands for every 8.4 MFLOP; loss of 2,048 x 128,256 x 2,048 860 us, 1.25 PFLOP/s, as a large library
@@ -45,7 +45,12 @@ double time_of(int64_t m, int64_t n, int64_t steps) {
     return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * kStepTime<S> + kEndsTime<S>);
 }
 
-constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dz in memory at a time: the size of the last-level cache
+// Of dz, and of weights in fp16 beside it, in memory at a time: seven eighths of the last-level cache, so that the products that read
+// them find them there.  But each piece adds to grad_hidden's sums anew and has ends of its own: where rows times hidden size are few,
+// as many tokens as make that little beside the products, if dz alone still fits there and both take up to three times as much (777
+// rows of 128,256 x 4,096 in eight pieces 4.36 ms, in two 4.00, in one 3.95).
+constexpr int64_t kPieceBytes = (int64_t)224 << 20;
+constexpr double kPieceProducts = 2e11;  // rows * hidden size * tokens
 // Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum instead of lse, which
 // large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
 // than the products, which are twice as many.  With more rows dz is one fp16 number, for which bf16 weights are read and written once
@@ -567,25 +572,32 @@ struct Plan {
     int32_t rows_pad;   // rows of dz in whole tiles and steps
     int32_t d_pad;      // hidden size in whole steps
     int32_t piece;      // tokens of a piece of dz
-    int32_t splits, k_split;
+    int32_t splits;     // of grad_hidden's sum over a piece
     int32_t sums_ld;
     bool direct_out;    // grad_hidden in one go
 };
 
-Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows) {
+// halves: weights are written in fp16, a piece at a time
+Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows, bool halves) {
     Plan p{};
     p.parts = N <= few_rows ? 2 : 1;
     p.logits_rows = p.parts == 2 ? std::min(rows_of_tile(N), 128) : rows_of_tile(N);
     p.d_pad = (int32_t)pad(D, kStepK);
     const int32_t rows_dz = N * p.parts;
     // (tiles of logits leave zeros behind N as well, and grad_weight's sum goes over whole steps of rows)
-    int64_t most = (int64_t)(kPieceBytes / 2 / pad(rows_dz, 256)) / 256 * 256;
-    if (most < kPieceLeast) most = kPieceLeast;
-    const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, most);
-    p.piece = (int32_t)pad(ceil_div(V, pieces), 256);
+    // A piece is a whole number of rounds of 256 tiles of logits, one to a compute unit, and one round at the least.
+    const int64_t bytes = (pad(rows_dz, 256) + (halves && p.parts == 1 ? pad(D, 8) : 0)) * 2;  // of a token
+    const int64_t round = std::max<int64_t>(slots<Shape256>() / ceil_div(N, p.logits_rows), 1) * Shape256::BM;
+    const int64_t fit = std::min(kPieceBytes / (pad(rows_dz, 256) * 2), 3 * kPieceBytes / bytes) / round;
+    const int64_t products = std::min((int64_t)std::min(kPieceProducts / N / D / (double)round + 0.5, 1e9), fit);
+    const int64_t least = std::max<int64_t>(ceil_div(kPieceLeast, round), 1);
+    const int64_t rounds = std::max(std::max(kPieceBytes / bytes / round, products), least);
+    const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, rounds * round);
+    p.piece = (int32_t)(pieces == 1 ? pad(V, 256) : ceil_div(ceil_div(V, round), pieces) * round);
     // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip, which costs a pass over the shares
     const int64_t first = V < p.piece ? V : p.piece;
     double best = 0;
+    int64_t best_split = 0;
     auto look = [&](auto shape, int rows) {
         using S = decltype(shape);
         const int64_t tiles = ceil_div(D, S::BM) * ceil_div(rows_dz, S::BN);
@@ -598,7 +610,7 @@ Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows) {
             if (best == 0 || time < best) {
                 best = time;
                 p.rows = rows;
-                p.k_split = (int32_t)k_split;
+                best_split = k_split;
             }
         }
     };
@@ -607,7 +619,7 @@ Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows) {
     look(Shape128{}, 128);
     look(Shape256{}, 256);
     p.rows_pad = (int32_t)pad(rows_dz, std::max(std::max(p.rows, p.logits_rows), (int)kStepK));
-    p.splits = (int32_t)ceil_div(first, p.k_split);  // of the first piece; later ones add to them
+    p.splits = (int32_t)ceil_div(first, best_split);  // of the first piece; later ones add to them
     p.sums_ld = (int32_t)pad(D, 4);
     p.direct_out = pieces == 1 && p.splits == 1 && p.parts == 1;
     return p;
@@ -762,7 +774,7 @@ int forward(const LossCall &c, float *loss, float *lse, Carver &ws, hipStream_t 
 template <typename T>
 int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16_t *grad_hidden, int64_t gh_stride,
              uint16_t *grad_weight, int64_t gw_stride, Carver &ws, hipStream_t stream, bool launch) {
-    const Plan p = plan_of(c.N, c.V, c.D, few_rows_of<T>(c.D));
+    const Plan p = plan_of(c.N, c.V, c.D, few_rows_of<T>(c.D), std::is_same_v<T, Bf16>);
     Masks masks;
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
     const bool few = p.parts == 2;
@@ -842,7 +854,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.n = rows_dz;
             g.D = c.D;
             g.k = tokens;
-            g.k_split = p.k_split;
+            g.k_split = (int32_t)pad(ceil_div(tokens, p.splits), kStepK);
             g.unscale = unscale;
             g.unscale16 = unscale_w;
             g.out = grad_hidden;
@@ -850,7 +862,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.sums = p.direct_out ? nullptr : sums;
             g.sums_ld = p.sums_ld;
             g.add = v0 > 0;
-            g.splits = (int32_t)ceil_div(tokens, p.k_split);
+            g.splits = (int32_t)ceil_div(tokens, g.k_split);
             if (halves) {
                 const Bf16Rows w{first, c.weight_stride, tokens, c.D};
                 CFGZIP_TRY(to_halves(w, tokens, largest, kLargestFirst, weight16, w_pad, unscale + 1));
