@@ -461,10 +461,15 @@ int cfgzip_nfa_advance_states(const int32_t *rel_rep, int32_t C, int32_t S,
  *     dz[i][v] = grad_loss[i] * (exp(z[i][v] - lse[i]) - [v = target[i]])   for admitted v, else 0
  *     grad_hidden[i] = sum_v dz[i][v] * weight[v],     grad_weight[v] = sum_i dz[i][v] * hidden[i]
  * Rows whose target is none or not admitted (no step lowers an infinite loss), and rows whose grad_loss is 0, have dz = 0
- * whatever their hidden states hold.  The weights have to be finite, those of masked tokens too.
+ * whatever their hidden states hold.  The weights have to be finite, those of masked tokens too, and so has grad_loss: one that is not
+ * makes its row of grad_hidden and any of grad_weight infinite or NaN.
  *   grad_hidden, grad_weight   out, [N] and [V] rows of D elements of the inputs' type; either may be NULL
- * dz is kept in fp16 for a piece of the vocabulary at a time, beside bf16 operands that are brought to fp16 by a power of two (what
- * is below 2^-32 of the largest loses bits); of few rows, up to 128 or 256, as the sum of two numbers of the inputs' type.  All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
+ * Up to 256 rows (128 of BF16 where D is no multiple of 8) dz is kept as the sum of two numbers of the inputs' type, of more rows in
+ * fp16 for a piece of the vocabulary at a time.  In fp16 a row's dz has a factor of its own, so grad_loss may be of any size, rows of
+ * any sizes beside each other; what dz is multiplied with is brought to fp16 as well: BF16 weights by a power of two (within 2^31 of
+ * the largest they stay what they are, what is smaller is 2^-39 of the largest or less off), and for grad_weight
+ * grad_loss[i] * hidden[i], rounded to fp16 where dz is one number (2^-37 of the largest or less off where it is small beside that).
+ * All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
  */
 size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);
 int cfgzip_head_loss(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,

@@ -81,7 +81,7 @@ struct LogitsArgs {
     float *z_target;
     // backward
     const float *lse;
-    const float *scaled_grad;  // 0: the row has no gradient
+    const float *factor;       // of a row's dz; 0: it has no gradient
     uint16_t *dz;              // [piece / 64][dz_rows][64]
     int64_t dz_rows;
     float *z;                  // [tokens / 64][N][64], -inf where not admitted
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
             const int32_t row = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15), at = row < a.N ? row : a.N - 1;
             targets[j.value] = a.target[at];
             if constexpr (WHAT == GRADIENT) {
-                grads[j.value] = a.scaled_grad[at];
+                grads[j.value] = a.factor[at];
                 shifts[j.value] = a.lse[at];
             }
             each<kWords>([&](auto w) CFGZIP_INLINE { words[j.value][w.value] = ~0u; });
@@ -277,10 +277,8 @@ struct Rows {
         if (masks.bits && !(masks.bits[i * masks.words + (t >> 5)] >> (t & 31) & 1)) return 0.0f;
         return grad_loss[i];
     }
-    // The factor that makes the largest finite gradient 2^14, so that dz fills the range of fp16 (bf16 would not need it), and where all
-    // are the same, as those of a mean, a row that is certain and wrong has dz without a rounding.  For all threads of a workgroup,
-    // whose waves leave their maxima in `shared`.
-    __device__ float scale(float *shared) const {
+    // The largest finite gradient.  For all threads of a workgroup, whose waves leave their maxima in `shared`.
+    __device__ float largest(float *shared) const {
         float most = 0.0f;
         for (int32_t i = threadIdx.x; i < N; i += blockDim.x) {
             const float x = fabsf(grad(i));
@@ -290,25 +288,41 @@ struct Rows {
         if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
         __syncthreads();
         for (int i = 0; i < (int)blockDim.x / kWave; ++i) most = fmaxf(most, shared[i]);
-        return 0x1p14f / fminf(fmaxf(most, 0x1p-86f), 0x1p114f);
+        return most;
     }
+    // The factor that makes it 2^14, for dz in bf16, whose range holds what the clamps leave beyond that and rows of any size beside each other.
+    __device__ float scale(float *shared) const { return 0x1p14f / fminf(fmaxf(largest(shared), 0x1p-86f), 0x1p114f); }
 };
 
-__global__ __launch_bounds__(1024) void rows_kernel(Rows rows, float *scaled, float *unscale) {
-    __shared__ float shared[16];
-    const float factor = rows.scale(shared);
-    for (int32_t i = threadIdx.x; i < rows.N; i += 1024) scaled[i] = rows.grad(i) * factor;
-    if (threadIdx.x == 0) *unscale = 1.0f / factor;
-}
+// floor(log2 |x|) of a finite x other than 0
+__device__ __forceinline__ int32_t exponent_of(float x) { return __builtin_amdgcn_frexp_expf(x) - 1; }
+
+// dz in fp16.  Its range holds a row's probabilities beside the row's own gradient, but not those of a row beside a gradient that
+// is 2^28 times as large, nor every gradient that there is.  So each row's dz has a factor of its own, 2^14 for any gradient, and the gradient,
+// digits * 2^(power + 14) with digits of 1 to 2, goes where it costs nothing: into the row of grad_hidden on its way out, and for grad_weight's
+// sum over the rows into the row's hidden states, as they become fp16 with a common power of two.  (With digits too: half the rounding of dz's
+// largest element, the target's, is none so.)  Where two numbers make up dz, and hidden states would be rounded more than it is, the digits
+// stay with dz.
+struct RowFactors {
+    float *dz;       // 0: the row has no gradient
+    float *digits;   // null: they stay with dz
+    int32_t *power;
+    // [0] takes from the digits what they have in common, so that the same gradient for all rows, as that of a mean, costs no rounding;
+    // [1] its inverse.  null like the digits.
+    float *common;
+};
 
 // dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
 // leave, the rest 0.  A thread has four tokens.
 template <typename T>
 __global__ __launch_bounds__(256) void few_rows_dz_kernel(Rows rows, const float *z, int32_t blocks, const f32x2 *whole, uint16_t *dz,
-                                                          int32_t dz_rows, float *unscale) {
-    __shared__ float shared[4];
-    const float factor = rows.scale(shared);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = 1.0f / factor;
+                                                          int32_t dz_rows, const float *factors, float *unscale) {
+    float factor = 1.0f;
+    if constexpr (std::is_same_v<T, Bf16>) {
+        __shared__ float shared[4];
+        factor = rows.scale(shared);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = 1.0f / factor;
+    }
     const int32_t N = rows.N, span = dz_rows - N;
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int32_t q = (int32_t)(k & 15), r = (int32_t)((k >> 4) % span);
@@ -317,7 +331,7 @@ __global__ __launch_bounds__(256) void few_rows_dz_kernel(Rows rows, const float
     uint16_t *const out = dz + block * dz_rows * 64 + q * 4;
     u32x2 hi = {0, 0}, lo = {0, 0};
     if (r < N) {
-        const float grad = rows.grad(r) * factor;
+        const float grad = std::is_same_v<T, Bf16> ? rows.grad(r) * factor : factors[r];
         if (grad != 0.0f) {
             const f32x4 x = *reinterpret_cast<const f32x4 *>(z + (block * N + r) * 64 + q * 4);
             const f32x2 w = whole[r];
@@ -325,8 +339,8 @@ __global__ __launch_bounds__(256) void few_rows_dz_kernel(Rows rows, const float
             f32x4 d, rest;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = x[j] == -kInf ? 0.0f : __expf(x[j] - w[0]) / w[1];
-                d[j] = (p - (j == mark ? 1.0f : 0.0f)) * grad;
+                const float p = __expf(x[j] - w[0]) / w[1];
+                d[j] = x[j] == -kInf ? 0.0f : (p - (j == mark ? 1.0f : 0.0f)) * grad;
                 rest[j] = d[j] - T::value(T::round(d[j]));
             }
             hi = round4<T>(d);
@@ -375,28 +389,106 @@ __device__ __forceinline__ void store4(uint16_t *row, int32_t c, int32_t n, f32x
     }
 }
 
-// The largest finite |x| of bf16 rows as its bits, of two matrices in one launch: workgroup b leaves that of the rows it took in
-// largest[b], of the first matrix in kLargestFirst of them.  A wave takes a row at a time.  (One word and atomic maxima took 250 us for
-// 128,256 x 4,096: as many waves, one after the other.)
-constexpr int kLargestFirst = 1024, kLargestSecond = 256;
-struct Bf16Rows {
+constexpr int32_t kNone = -100000;  // floor(log2 0)
+
+// The largest finite |x| of 16-bit numbers as bits
+template <typename T>
+__device__ __forceinline__ void take_largest(uint32_t &most, uint32_t bits) {
+    bits &= 0x7FFFu;
+    most = bits > most && bits < (std::is_same_v<T, Bf16> ? 0x7F80u : 0x7C00u) ? bits : most;
+}
+// The largest of a workgroup's WAVES waves, for thread 0
+template <int WAVES>
+__device__ __forceinline__ int32_t largest_of(int32_t x, int32_t *shared) {
+    for (int d = 1; d < kWave; d *= 2) {
+        const int32_t other = __shfl_xor(x, d);
+        x = other > x ? other : x;
+    }
+    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = x;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 1; i < WAVES; ++i) x = shared[i] > x ? shared[i] : x;
+    return x;
+}
+
+// For dz in fp16: the rows' factors, their hidden states in rows of whole steps of 64 elements (zeros behind D, and in those without a
+// gradient, whatever they hold), and floor(log2) of the largest |hidden| times its row's power of two, which workgroup b leaves of the
+// rows that it took in largest[b], kNone where all is 0.  A wave takes a row at a time; the last workgroup has the digits' common part.
+constexpr int kRowsOfBlock = 16, kRowBlocks = 256;
+template <typename T>
+__global__ __launch_bounds__(kRowsOfBlock *kWave) void rows_kernel(Rows rows, const uint16_t *x, int64_t x_ld, int32_t D, uint16_t *y, int32_t y_ld,
+                                                                   RowFactors f, int32_t *largest) {
+    __shared__ int32_t shared[kRowsOfBlock];
+    const int32_t blocks = gridDim.x - 1;
+    if ((int32_t)blockIdx.x == blocks) {
+        if (!f.common) return;
+        const float most = rows.largest(reinterpret_cast<float *>(shared));
+        if (threadIdx.x == 0) {
+            const float digits = most == 0.0f ? 1.0f : ldexpf(most, -exponent_of(most));
+            f.common[0] = 1.0f / digits;
+            f.common[1] = digits;
+        }
+        return;
+    }
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    int32_t most = kNone;
+    for (int32_t row = blockIdx.x * kRowsOfBlock + wave; row < rows.N; row += blocks * kRowsOfBlock) {
+        const float grad = rows.grad(row);
+        const bool finite = fabsf(grad) < kInf && grad != 0.0f;
+        const int32_t e = finite ? exponent_of(grad) : 0, power = e - 14;
+        const float digits = finite ? ldexpf(grad, -e) : grad;
+        if (lane == 0) {
+            f.dz[row] = grad == 0.0f ? 0.0f : f.digits ? 0x1p14f : digits * 0x1p14f;
+            if (f.digits) f.digits[row] = digits;
+            f.power[row] = power;
+        }
+        const uint16_t *const p = x + row * x_ld;
+        uint16_t *const to = y + (int64_t)row * y_ld;
+        uint32_t bits = 0;
+        constexpr int kUnits = 4;  // on their way at a time
+        for (int32_t c = lane * 8; c < y_ld; c += kWave * 8 * kUnits) {
+            u32x4 v[kUnits];
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int32_t at = c + i * kWave * 8;
+                v[i] = u32x4{0, 0, 0, 0};
+                if (grad != 0.0f && at + 8 <= D) {
+                    v[i] = *reinterpret_cast<const u32x4_any *>(p + at);
+                } else if (grad != 0.0f) {
+                    for (int j = 0; at + j < D; ++j) v[i][j / 2] |= (uint32_t)p[at + j] << (j % 2 * 16);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int32_t at = c + i * kWave * 8;
+                if (at < y_ld) *reinterpret_cast<u32x4 *>(to + at) = v[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) take_largest<T>(bits, v[i][j]), take_largest<T>(bits, v[i][j] >> 16);
+            }
+        }
+        if (bits) {
+            const int32_t here = exponent_of(T::value((uint16_t)bits)) + power;
+            most = here > most ? here : most;
+        }
+    }
+    most = largest_of<kRowsOfBlock>(most, shared);
+    if (threadIdx.x == 0) largest[blockIdx.x] = most;
+}
+
+// floor(log2) of the largest finite |x| of bf16 weights: workgroup b leaves that of the rows it took in largest[b], kNone where all is 0.
+// A wave takes a row at a time.  (One word and atomic maxima took 250 us for 128,256 x 4,096: as many waves, one after the other.)
+constexpr int kWeightBlocks = 1024;
+struct Matrix16 {
     const uint16_t *x;
     int64_t ld;
     int32_t rows, D;
 };
-__global__ __launch_bounds__(256) void largest_kernel(Bf16Rows first, Bf16Rows second, uint32_t *largest) {
-    __shared__ uint32_t shared[4];
+__global__ __launch_bounds__(256) void largest_kernel(Matrix16 m, int32_t *largest) {
+    __shared__ int32_t shared[4];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const bool in_first = blockIdx.x < kLargestFirst;
-    const Bf16Rows &m = in_first ? first : second;
-    const int32_t block = in_first ? blockIdx.x : blockIdx.x - kLargestFirst, blocks = in_first ? kLargestFirst : kLargestSecond;
-    uint32_t most = 0;
-    auto take = [&](uint32_t bits) {
-        bits &= 0x7FFFu;
-        most = bits > most && bits < 0x7F80u ? bits : most;
-    };
+    uint32_t bits = 0;
     constexpr int kUnits = 8;  // on their way at a time
-    for (int64_t row = (int64_t)block * 4 + wave; row < m.rows; row += (int64_t)blocks * 4) {
+    for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < m.rows; row += kWeightBlocks * 4) {
         const uint16_t *const p = m.x + row * m.ld;
         for (int32_t c = lane * 8; c < m.D; c += kWave * 8 * kUnits) {
             u32x4 v[kUnits];
@@ -407,53 +499,55 @@ __global__ __launch_bounds__(256) void largest_kernel(Bf16Rows first, Bf16Rows s
                 if (at + 8 <= m.D) {
                     v[i] = *reinterpret_cast<const u32x4_any *>(p + at);
                 } else {
-                    for (int32_t j = at; j < m.D; ++j) take(p[j]);
+                    for (int32_t j = at; j < m.D; ++j) take_largest<Bf16>(bits, p[j]);
                 }
             }
 #pragma unroll
             for (int i = 0; i < kUnits; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) take(v[i][j]), take(v[i][j] >> 16);
+                for (int j = 0; j < 4; ++j) take_largest<Bf16>(bits, v[i][j]), take_largest<Bf16>(bits, v[i][j] >> 16);
         }
     }
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t other = __shfl_xor(most, d);
-        most = other > most ? other : most;
-    }
-    if (lane == 0) shared[wave] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 4; ++i) most = shared[i] > most ? shared[i] : most;
-        largest[blockIdx.x] = most;
-    }
+    const int32_t most = largest_of<4>(bits ? exponent_of(Bf16::value((uint16_t)bits)) : kNone, shared);
+    if (threadIdx.x == 0) largest[blockIdx.x] = most;
 }
 
-// bf16 rows as fp16, times the power of two that brings the largest of the `count` (1,024 or 256) below 2^15: what lies within 2^32 of the
-// largest keeps its eight bits, the rest is 2^-40 of the largest or less off.  Rows of y_ld elements, zeros behind D and from
-// row R on.  Leaves the factor's inverse in `unscale`.  A thread has four units of eight.
-__global__ __launch_bounds__(256) void halves_kernel(Bf16Rows x, const uint32_t *largest, int32_t count, uint16_t *y, int32_t y_ld, int32_t all,
-                                                     float *unscale) {
-    __shared__ uint32_t shared[4];
-    uint32_t most = 0;
-    for (int32_t i = threadIdx.x; i < count; i += 256) most = largest[i] > most ? largest[i] : most;
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t other = __shfl_xor(most, d);
-        most = other > most ? other : most;
+// 2^e in two factors: one alone may be too much for fp32, and what is beyond both is 0 in 16 bits.  (ldexp is half as fast as a product.)
+struct PowerOfTwo {
+    float a, b;
+    __device__ __forceinline__ explicit PowerOfTwo(int32_t e) {
+        const int32_t first = e < -126 ? -126 : e > 127 ? 127 : e, rest = e - first;
+        a = __builtin_bit_cast(float, (uint32_t)(127 + first) << 23);
+        b = __builtin_bit_cast(float, (uint32_t)(127 + (rest < -126 ? -126 : rest > 127 ? 127 : rest)) << 23);
     }
-    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
+};
+
+// 16-bit rows as fp16, times a row's factors where there are some and the power of two that brings the largest of the `count` to 2^14
+// to 2^15 (with digits 2^12 to 2^15): bf16 weights within 2^31 of the largest keep their eight bits, what is smaller is 2^-39 of the
+// largest or less off (2^-37 with digits).  The rows `times` times over, y_ld elements each, zeros behind D and behind the last up to
+// `all`.  Leaves the power of two that takes that back in `back`.  A thread has four units of eight.
+template <typename T>
+__global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, RowFactors f, const int32_t *largest, int32_t count, int32_t times,
+                                                     uint16_t *y, int32_t y_ld, int32_t all, int32_t *back) {
+    __shared__ int32_t shared[5];
+    int32_t most = kNone;
+    for (int32_t i = threadIdx.x; i < count; i += 256) most = largest[i] > most ? largest[i] : most;
+    most = largest_of<4>(most, shared);
+    if (threadIdx.x == 0) shared[4] = most;
     __syncthreads();
-    for (int i = 0; i < 4; ++i) most = shared[i] > most ? shared[i] : most;
-    const int32_t e = (int32_t)(most >> 7) - 127;  // 2^e <= the largest < 2^(e + 1)
-    const int32_t k = 14 - e < 126 ? 14 - e : 126;
-    const float factor = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *unscale = __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
+    most = shared[4];
+    const int32_t power = most == kNone ? 0 : (f.digits ? 13 : 14) - most;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *back = -power;
     const int32_t units = y_ld / 8;
+    const float common = f.digits ? f.common[0] : 1.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t at = ((int64_t)blockIdx.x * 4 + i) * 256 + threadIdx.x;
         if (at >= (int64_t)all * units) break;
-        const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 8;
+        const int32_t to = (int32_t)(at / units), c = (int32_t)(at % units) * 8, row = times == 2 && to >= x.rows ? to - x.rows : to;
         u32x4 v = {0, 0, 0, 0};
+        int32_t e = power;
+        float factor = common;
         if (row < x.rows) {
             const uint16_t *const p = x.x + row * x.ld + c;
             if (c + 8 <= x.D) {
@@ -461,19 +555,40 @@ __global__ __launch_bounds__(256) void halves_kernel(Bf16Rows x, const uint32_t 
             } else {
                 for (int j = 0; c + j < x.D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
             }
+            if (f.power) e += f.power[row];
+            if (f.digits) factor *= f.digits[row];
         }
+        const PowerOfTwo scale(e);
+        const float last = scale.b * factor;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = Fp16::round2(Bf16::value((uint16_t)v[j]) * factor, Bf16::value((uint16_t)(v[j] >> 16)) * factor);
-        *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = v;
+        for (int j = 0; j < 4; ++j)
+            v[j] = Fp16::round2(T::value((uint16_t)v[j]) * scale.a * last, T::value((uint16_t)(v[j] >> 16)) * scale.a * last);
+        *reinterpret_cast<u32x4 *>(y + (int64_t)to * y_ld + c) = v;
     }
 }
+
+// What a result takes back of the factors of dz and of the product's other operand, each null where there is none.
+struct Factors {
+    const float *all;      // of all results
+    const float *digits;   // of a row
+    const int32_t *power;  // of a row
+    const int32_t *back;   // of all results
+    __device__ __forceinline__ f32x2 of_all() const {
+        const PowerOfTwo scale(back ? *back : 0);
+        return f32x2{scale.a, scale.b * (all ? *all : 1.0f)};
+    }
+    __device__ __forceinline__ f32x2 of(int32_t row) const {
+        const PowerOfTwo scale((power ? power[row] : 0) + (back ? *back : 0));
+        return f32x2{scale.a, scale.b * (all ? *all : 1.0f) * (digits ? digits[row] : 1.0f)};
+    }
+};
 
 struct GradArgs {
     Operand A, B;  // A: m = hidden size; B: n = rows (grad_hidden) or tokens (grad_weight)
     int32_t n, D;  // extents of the result
     int32_t k, k_split, splits;
     int32_t tiles_m, tiles_n;
-    const float *unscale, *unscale16;  // of dz; of the other operand or null (their product alone may be too small for fp32)
+    Factors factors;
     uint16_t *out;  // [n][out_ld]
     int64_t out_ld;
     float *sums;  // [splits][n][sums_ld], sums_ld = D rounded up to 4; null: the result goes to `out` at once
@@ -507,10 +622,12 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
         int32_t tm = 0, tn = 0, split = 0;
         place(i, tm, tn, split);
-        const float unscale = *a.unscale, unscale16 = a.unscale16 ? *a.unscale16 : 1.0f;
+        f32x2 factor = {1.0f, 1.0f};
+        if (B_COLUMNS) factor = a.factors.of_all();  // (asked for once: 32,000 x 2,048 with 64 rows 69 us for 79)
         each<S::FN>([&](auto j) CFGZIP_INLINE {
             const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
             if (n >= a.n) return;
+            if (!B_COLUMNS && !a.sums) factor = a.factors.of(n);
             each<S::FM>([&](auto i) CFGZIP_INLINE {
                 const int32_t c = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
                 if (c >= a.D) return;
@@ -518,7 +635,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
                     f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
                     *p = a.add ? *p + acc[i.value][j.value] : acc[i.value][j.value];
                 } else {
-                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * unscale * unscale16);
+                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * factor[0] * factor[1]);
                 }
             });
         });
@@ -529,12 +646,12 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
 // Joins grad_hidden's shares of the sum (and the two numbers of few rows' dz).
 template <typename T>
 __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
-                                                         const float *unscale, const float *unscale16, uint16_t *out, int64_t out_ld) {
+                                                         Factors factors, uint16_t *out, int64_t out_ld) {
     const int32_t units = sums_ld / 4;
     const int64_t k = (int64_t)blockIdx.x * kWave + threadIdx.x;
     if (k >= (int64_t)n * units) return;
     const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 4;
-    const float factor = *unscale, factor16 = unscale16 ? *unscale16 : 1.0f;
+    const f32x2 factor = factors.of(row);
     const float *p = sums + (int64_t)row * sums_ld + c;
     const int64_t step = (int64_t)n * sums_ld;
     f32x4 x = {0, 0, 0, 0};
@@ -545,7 +662,7 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_
 #pragma unroll
         for (int i = 0; i < 16; ++i) x += y[i];
     }
-    store4<T>(out + row * out_ld, c, D, x * factor * factor16);
+    store4<T>(out + row * out_ld, c, D, x * factor[0] * factor[1]);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
@@ -778,17 +895,28 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     Masks masks;
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
     const bool few = p.parts == 2;
-    // Of many rows dz is fp16, whose eleven bits leave a gradient as near to the truth as its own rounding does: in bf16 its largest
-    // element, the target's, was off by as much as all of that.  The products' other sides, where they are bf16, become fp16 too.
+    // Of many rows dz is one fp16 number, whose eleven bits leave bf16 gradients as near to the truth as their own rounding does (in bf16
+    // dz's largest element, the target's, was off by as much as all of that) and fp16 ones up to 1.4 times as far off.  The products'
+    // other sides, where they are bf16, become fp16 too.
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
-    const bool halves = kBf16 && !few;
+    const bool halves = kBf16 && !few, fp16_dz = !kBf16 || !few;
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
-    float *unscale = ws.take<float>(3);  // of dz; of weights in fp16; of hidden states in fp16
-    uint32_t *largest = ws.take<uint32_t>(kLargestFirst + kLargestSecond);  // of the weights, of the hidden states
-    float *scaled = few ? nullptr : ws.take<float>(c.N);
+    float *unscale = ws.take<float>(1);  // of dz in two bf16 numbers
+    RowFactors of_rows{};                // of dz in fp16
+    int32_t *back = ws.take<int32_t>(2);  // of weights in fp16; of hidden states times their rows' factors
+    int32_t *largest_w = ws.take<int32_t>(kWeightBlocks), *largest_h = ws.take<int32_t>(kRowBlocks);
+    if (fp16_dz) {
+        of_rows.dz = ws.take<float>(c.N);
+        of_rows.power = ws.take<int32_t>(c.N);
+        if (!few) {
+            of_rows.digits = ws.take<float>(c.N);
+            of_rows.common = ws.take<float>(2);
+        }
+    }
     const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK), w_pad = (int32_t)pad(c.D, 8);
-    uint16_t *copy = ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad);
-    uint16_t *copy16 = halves ? ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad) : copy;
+    // hidden states, 0 where a row has no gradient: for the logits, and for grad_weight as dz needs them
+    uint16_t *copy = ws.take<uint16_t>((size_t)(fp16_dz ? c.N : copy_rows_pad) * p.d_pad);
+    uint16_t *copy16 = fp16_dz ? ws.take<uint16_t>((size_t)copy_rows_pad * p.d_pad) : copy;
     uint16_t *weight16 = halves ? ws.take<uint16_t>((size_t)std::min(p.piece, c.V) * w_pad) : nullptr;
     uint16_t *dz = ws.take<uint16_t>((size_t)p.rows_pad * p.piece);
     float *sums = ws.take<float>((size_t)p.splits * rows_dz * p.sums_ld);
@@ -796,26 +924,32 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     f32x2 *parts = few ? ws.take<f32x2>((size_t)count * c.N) : nullptr, *whole = few ? ws.take<f32x2>(c.N) : nullptr;
     if (!launch) return CFGZIP_OK;
     const Rows rows{grad_loss, c.target, c.N, c.V, masks};
-    if (!few) {
-        hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, stream, rows, scaled, unscale);
-        CFGZIP_TRY(check_launch());
-    }
-    CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
-    const float *unscale_w = nullptr, *unscale_h = nullptr;
-    auto to_halves = [&](const Bf16Rows &x, int32_t all, const uint32_t *most, int32_t many, uint16_t *y, int32_t y_ld, float *to) {
-        hipLaunchKernelGGL(halves_kernel, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, most, many, y,
-                           y_ld, all, to);
+    auto to_halves = [&](const Matrix16 &x, const RowFactors &f, const int32_t *most, int32_t many, int32_t times, uint16_t *y, int32_t y_ld,
+                         int32_t all, int32_t *to) {
+        hipLaunchKernelGGL(halves_kernel<T>, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, f, most,
+                           many, times, y, y_ld, all, to);
         return check_launch();
     };
-    if (halves) {
-        const Bf16Rows w{static_cast<const uint16_t *>(c.weight), c.weight_stride, grad_hidden ? c.V : 0, c.D};
-        const Bf16Rows h{copy, p.d_pad, c.N, c.D};
-        hipLaunchKernelGGL(largest_kernel, dim3(kLargestFirst + kLargestSecond), dim3(256), 0, stream, w, h, largest);
+    if (fp16_dz) {
+        const int32_t blocks = std::min((int32_t)ceil_div(c.N, kRowsOfBlock), kRowBlocks);
+        hipLaunchKernelGGL(rows_kernel<T>, dim3(blocks + 1), dim3(kRowsOfBlock * kWave), 0, stream, rows,
+                           static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.D, copy, p.d_pad, of_rows, largest_h);
         CFGZIP_TRY(check_launch());
-        if (grad_weight) CFGZIP_TRY(to_halves(h, copy_rows_pad, largest + kLargestFirst, kLargestSecond, copy16, p.d_pad, unscale + 2));
-        unscale_w = unscale + 1;
-        unscale_h = unscale + 2;
+        if (grad_weight)
+            CFGZIP_TRY(to_halves(Matrix16{copy, p.d_pad, c.N, c.D}, of_rows, largest_h, blocks, p.parts, copy16, p.d_pad, copy_rows_pad,
+                                 back + 1));
+    } else {
+        CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
     }
+    if (halves && grad_hidden) {
+        hipLaunchKernelGGL(largest_kernel, dim3(kWeightBlocks), dim3(256), 0, stream,
+                           Matrix16{static_cast<const uint16_t *>(c.weight), c.weight_stride, c.V, c.D}, largest_w);
+        CFGZIP_TRY(check_launch());
+    }
+    const Factors factors_h = fp16_dz ? Factors{nullptr, of_rows.digits, of_rows.power, halves ? back : nullptr}
+                                      : Factors{unscale, nullptr, nullptr, nullptr};
+    const Factors factors_w = fp16_dz ? Factors{few ? nullptr : of_rows.common + 1, nullptr, nullptr, back + 1}
+                                      : Factors{unscale, nullptr, nullptr, nullptr};
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
     for (int64_t v0 = 0; v0 < c.V; v0 += p.piece) {
@@ -831,7 +965,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         a.masks = masks;
         a.target = c.target;
         a.lse = lse;
-        a.scaled_grad = scaled;
+        a.factor = of_rows.dz;
         a.dz = dz;
         a.dz_rows = p.rows_pad;
         a.parts = parts;
@@ -842,7 +976,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             const int32_t blocks = (int32_t)(pad(tokens, 64) / 64);
             const int64_t threads = (int64_t)blocks * (p.rows_pad - c.N) * 16;
             hipLaunchKernelGGL((few_rows_dz_kernel<T>), dim3((uint32_t)ceil_div(threads, 256)), dim3(256), 0, stream, rows, z, blocks, whole,
-                               dz, p.rows_pad, unscale);
+                               dz, p.rows_pad, of_rows.dz, unscale);
             CFGZIP_TRY(check_launch());
         } else {
             CFGZIP_TRY((launch_logits<T, GRADIENT>(p.logits_rows, a, tokens, direct, stream)));
@@ -855,8 +989,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.D = c.D;
             g.k = tokens;
             g.k_split = (int32_t)pad(ceil_div(tokens, p.splits), kStepK);
-            g.unscale = unscale;
-            g.unscale16 = unscale_w;
+            g.factors = factors_h;
             g.out = grad_hidden;
             g.out_ld = gh_stride;
             g.sums = p.direct_out ? nullptr : sums;
@@ -864,8 +997,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.add = v0 > 0;
             g.splits = (int32_t)ceil_div(tokens, g.k_split);
             if (halves) {
-                const Bf16Rows w{first, c.weight_stride, tokens, c.D};
-                CFGZIP_TRY(to_halves(w, tokens, largest, kLargestFirst, weight16, w_pad, unscale + 1));
+                const Matrix16 w{first, c.weight_stride, tokens, c.D};
+                CFGZIP_TRY(to_halves(w, RowFactors{}, largest_w, kWeightBlocks, 1, weight16, w_pad, tokens, back));
                 CFGZIP_TRY((launch_grad_hidden<Fp16, T, true>(p.rows, g, stream)));
             } else {
                 CFGZIP_TRY(direct ? (launch_grad_hidden<T, T, true>(p.rows, g, stream))
@@ -881,8 +1014,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.k = rows_dz;
             g.k_split = (int32_t)pad(rows_dz, kStepK);
             g.splits = 1;
-            g.unscale = unscale;
-            g.unscale16 = unscale_h;
+            g.factors = factors_w;
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
             CFGZIP_TRY(halves ? (launch_grad_weight<Fp16, T>(g, stream)) : (launch_grad_weight<T, T>(g, stream)));
@@ -891,7 +1023,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
         hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, sums, p.splits * p.parts, c.N,
-                           c.D, p.sums_ld, unscale, unscale_w, grad_hidden, gh_stride);
+                           c.D, p.sums_ld, factors_h, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }
     return CFGZIP_OK;
