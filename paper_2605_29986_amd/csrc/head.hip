@@ -51,7 +51,7 @@ double time_of(int64_t m, int64_t n, int64_t steps) {
 // rows of 128,256 x 4,096 in eight pieces 4.36 ms, in two 4.00, in one 3.95).
 constexpr int64_t kPieceBytes = (int64_t)224 << 20;
 constexpr double kPieceProducts = 2e11;  // rows * hidden size * tokens
-// Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum instead of lse, which
+// Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum beside lse, which
 // large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
 // than the products, which are twice as many.  With more rows dz is one fp16 number, for which bf16 weights are read and written once
 // more: 200 rows of 32,000 x 2,048 take 361 us so and 304 as two numbers (50,003 x 333, whose rows lie at no multiples of 16 bytes
@@ -210,12 +210,13 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
     multiply<T, S, TileA, TileB>(a.W, a.H, lds, work, store, NoScales{});
 }
 
-// Joins the parts of a row: lse and loss, or (`whole` given) its maximum and sum.  A workgroup has ROWS rows and splits the parts over the other lanes; a lane asks for
-// eight parts before it uses the first.
+// Joins the parts of a row: lse and loss; or (`whole` given) its maximum and sum, so that exp(z - maximum) / sum is exp(z - lse) of the lse
+// that the caller gave, without its rounding where it is the row's own.  A workgroup has ROWS rows and splits the parts over the other
+// lanes; a lane asks for eight parts before it uses the first.
 template <int ROWS>
 __global__ __launch_bounds__(1024) void join_kernel(const f32x2 *parts, int32_t count, int32_t N, int32_t V, Masks masks,
                                                     const int32_t *target, const float *z_target, float *loss, float *lse,
-                                                    f32x2 *whole) {
+                                                    f32x2 *whole) {  // lse: out, with `whole` in
     constexpr int kShares = 1024 / ROWS;
     struct Part {
         float most;
@@ -250,11 +251,13 @@ __global__ __launch_bounds__(1024) void join_kernel(const f32x2 *parts, int32_t 
         }
     }
     if (s != 0 || row >= N) return;
+    const float l = (most == -kInf ? 0.0f : most) + logf((float)sum);
     if (whole) {
-        whole[row] = f32x2{most, (float)sum};
+        float apart = l - lse[row];
+        if (fabsf(apart) <= 0x1p-22f * fabsf(l)) apart = 0.0f;  // the same number, by sums of other parts or their roundings
+        whole[row] = f32x2{most - apart, (float)sum};
         return;
     }
-    const float l = (most == -kInf ? 0.0f : most) + logf((float)sum);
     const int32_t t = target[row];
     float out = 0.0f;
     if (t >= 0 && t < V) {
@@ -972,7 +975,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         a.z = z;
         if (few) {
             CFGZIP_TRY((launch_logits<T, KEPT>(p.logits_rows, a, tokens, direct, stream)));
-            CFGZIP_TRY(join(parts, count, c, masks, nullptr, nullptr, nullptr, whole, stream));
+            CFGZIP_TRY(join(parts, count, c, masks, nullptr, nullptr, const_cast<float *>(lse), whole, stream));
             const int32_t blocks = (int32_t)(pad(tokens, 64) / 64);
             const int64_t threads = (int64_t)blocks * (p.rows_pad - c.N) * 16;
             hipLaunchKernelGGL((few_rows_dz_kernel<T>), dim3((uint32_t)ceil_div(threads, 256)), dim3(256), 0, stream, rows, z, blocks, whole,
