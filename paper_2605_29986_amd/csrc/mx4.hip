@@ -548,7 +548,8 @@ __device__ __forceinline__ void store_tile(const ManyArgs &a, int32_t tm, int32_
 }
 
 // 16-bit hidden states.  A step has 128 k: lane (r, g) of a fragment has block g of its token, 32 weights, as four fragments of
-// eight, and the hidden states of the same k.
+// eight, and the hidden states of the same k.  Every barrier that hands on what was loaded to LDS waits for the wave's own loads
+// first: the compiler need not know that they write it.
 template <typename S>
 __global__ __launch_bounds__(S::kThreads) void many_rows_kernel(ManyArgs a) {
     using RowsW = Rows<S::BM, S::kThreads, 4>;
@@ -609,21 +610,21 @@ __global__ __launch_bounds__(S::kThreads) void many_rows_kernel(ManyArgs a) {
             }
         };
         int32_t steps = (a.w.nb + 3) / 4;
-        __syncthreads();  // the part before has been read
+        wait_for_loads<0>();  // (none yet:) the part before has been read
         load(lds0);
         scales();
-        __syncthreads();
+        wait_for_loads<0>();
         while (true) {
             if (steps > 1) load(lds1);
             step(lds0);
             if (steps == 1) break;
             scales();
-            __syncthreads();
+            wait_for_loads<0>();
             if (steps > 2) load(lds0);
             step(lds1);
             if (steps == 2) break;
             scales();
-            __syncthreads();
+            wait_for_loads<0>();
             steps -= 2;
         }
     }
@@ -707,16 +708,16 @@ __global__ __launch_bounds__(S::kThreads) void many_rows4_kernel(ManyArgs a) {
     int32_t steps = (nb + 7) / 8;
     load(lds0);
     scales();
-    __syncthreads();
+    wait_for_loads<0>();
     while (true) {
         if (steps > 1) load(lds1);
         step(lds0, steps > 1);
         if (steps == 1) break;
-        __syncthreads();
+        wait_for_loads<0>();
         if (steps > 2) load(lds0);
         step(lds1, steps > 2);
         if (steps == 2) break;
-        __syncthreads();
+        wait_for_loads<0>();
         steps -= 2;
     }
     store_tile<S>(a, tm, tn, wm, wn, lane, acc);
