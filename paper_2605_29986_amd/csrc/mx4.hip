@@ -260,6 +260,10 @@ constexpr int kFewThreads = 1024;
 constexpr int kFewWaves = kFewThreads / kWave;
 constexpr int kAhead = 8;  // loads of 64 bytes a token: a KB and four blocks each
 
+// Blocks of a row in LDS.  Where a load's four go beyond the last one, lanes have codes of 0 there, and one more block, of zeros, to multiply
+// with them: of an infinity they would make a NaN.
+__host__ __device__ inline int32_t lds_blocks(int32_t nb) { return nb % 4 ? nb + 1 : nb; }
+
 // ROWS: LDS rows of hidden states in fragments of 16.  fp16 has two bf16 rows of each: the rest lies 8 rows behind (up to 8 rows,
 // one fragment) or 16.
 template <int X, int FRAGMENTS>
@@ -271,16 +275,22 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a) {
     const int rest = FRAGMENTS == 2 ? 16 : 8;  // where the rests of fp16 lie
 
     // hidden states to LDS; what lies behind K is 0
+    const int32_t there = lds_blocks(nb);
     if constexpr (X == X_4) {
-        for (int32_t k = threadIdx.x; k < B * nb; k += kFewThreads) {
-            const int32_t b = k / nb, c = k % nb;
-            *reinterpret_cast<u32x4 *>(lds + b * a.lds_row + c * 16) =
-                *reinterpret_cast<const u32x4_bytes *>(static_cast<const uint8_t *>(a.x) + b * a.x_ld + c * 16);
-            lds[b * a.lds_row + nb * 16 + c] = (char)a.x_scales[(int64_t)b * nb + c];
+        for (int32_t k = threadIdx.x; k < B * there; k += kFewThreads) {
+            const int32_t b = k / there, c = k % there;
+            u32x4 v = {0, 0, 0, 0};
+            uint8_t scale = 0;
+            if (c < nb) {
+                v = *reinterpret_cast<const u32x4_bytes *>(static_cast<const uint8_t *>(a.x) + b * a.x_ld + c * 16);
+                scale = a.x_scales[(int64_t)b * nb + c];
+            }
+            *reinterpret_cast<u32x4 *>(lds + b * a.lds_row + c * 16) = v;
+            lds[b * a.lds_row + there * 16 + c] = (char)scale;
         }
     } else {
         const uint16_t *x = static_cast<const uint16_t *>(a.x);
-        const int32_t units = nb * 4;
+        const int32_t units = there * 4;
         for (int32_t k = threadIdx.x; k < B * units; k += kFewThreads) {
             const int32_t b = k / units, c = k % units, left = a.K - c * 8;
             uint16_t e[8];
@@ -394,11 +404,11 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int32_t last = nb - 1, block = (l + i) * 4 + g < nb ? (l + i) * 4 + g : last;
+                const int32_t block = (l + i) * 4 + g < nb ? (l + i) * 4 + g : nb;
                 if (l + i >= l1) break;
                 if constexpr (X == X_4) {
                     const u32x4 x = *reinterpret_cast<const u32x4 *>(xs[0] + block * 16);
-                    acc[0] = multiply4(code[i], x, acc[0], byte[i], (uint8_t)xs[0][nb * 16 + block]);
+                    acc[0] = multiply4(code[i], x, acc[0], byte[i], (uint8_t)xs[0][there * 16 + block]);
                 } else {
                     const float scale = __builtin_bit_cast(float, scale_bits(byte[i]));
 #pragma unroll
@@ -1091,6 +1101,7 @@ int32_t whole_pairs(int32_t K) { return (int32_t)ceil_div(K, kPairK) * kPairK; }
 
 // Rows in LDS of the kernel for few rows and the bytes of one, so that 16 of them spread over all banks; 0 bytes: does not fit
 size_t few_lds(int x, int32_t B, int32_t nb, int32_t &row, int &fragments) {
+    nb = lds_blocks(nb);
     row = x == X_4 ? (int32_t)align_up((size_t)nb * 17, 16) + (nb * 17 % 256 <= 240 ? 16 : 0) : nb * 64 + 16;
     int64_t rows = B;
     fragments = B <= 16 ? 1 : 2;
