@@ -7,6 +7,7 @@ stream.  Function names and argument order follow ``include/cfgzip.h``.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -220,9 +221,11 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream)
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
-    # torch's caching allocator hands out 512-byte aligned blocks
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def _workspace(nbytes: int, device, stream) -> torch.Tensor:
+    # torch's caching allocator hands out 512-byte aligned blocks.  It is gone when the call returns, with the work still queued: so it
+    # belongs to the stream of that work, where nothing that takes it over can come before.
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
 def cfgzip_signatures(tok_bytes: torch.Tensor, tok_off: torch.Tensor, table: torch.Tensor, *,
@@ -252,7 +255,7 @@ def cfgzip_signatures(tok_bytes: torch.Tensor, tok_off: torch.Tensor, table: tor
         hash_out = torch.empty((V,), dtype=torch.int64, device=dev)
     need = query(V, S)
     if workspace is None:
-        workspace = _workspace(need, dev)
+        workspace = _workspace(need, dev, stream)
     rc = entry(
         _dev(tok_bytes, torch.uint8, "tok_bytes") if tok_bytes.numel() else None,
         _dev(tok_off, torch.int64, "tok_off"), V,
@@ -316,7 +319,7 @@ def cfgzip_build_classes(tok_bytes: torch.Tensor, tok_off: torch.Tensor,
         rep_of_class = torch.empty((V,), dtype=torch.int32, device=dev)
     need = lib.cfgzip_build_classes_workspace_bytes(V, S)
     if workspace is None:
-        workspace = _workspace(need, dev)
+        workspace = _workspace(need, dev, stream)
     c_host = ctypes.c_int32(0)
     coll_host = ctypes.c_int32(0)
     rc = lib.cfgzip_build_classes(
@@ -519,7 +522,7 @@ def cfgzip_stack_adjacency(prod_head: torch.Tensor, prod_byte: torch.Tensor,
     adj = torch.empty((N, words_for(N)), dtype=torch.int32, device=dev)
     invalid = torch.empty((1,), dtype=torch.int32, device=dev)
     if workspace is None:
-        workspace = _workspace(lib.cfgzip_displacements_workspace_bytes(0, N, prod_head.numel()), dev)
+        workspace = _workspace(lib.cfgzip_displacements_workspace_bytes(0, N, prod_head.numel()), dev, stream)
     h, b, off, bd, P = _grammar_args(prod_head, prod_byte, prod_body_off, prod_body)
     total = prod_body.numel() if body_total is None else int(body_total)
     rc = lib.cfgzip_stack_adjacency(h, b, off, bd, total, P, N, adj.data_ptr(), invalid.data_ptr(),
@@ -548,7 +551,7 @@ def cfgzip_displacements(tok_bytes: torch.Tensor, tok_off: torch.Tensor, prod_he
     hashes = torch.empty((V,), dtype=torch.int64, device=dev)
     status = torch.empty((V,), dtype=torch.int32, device=dev)
     if workspace is None:
-        workspace = _workspace(lib.cfgzip_displacements_workspace_bytes(V, N, prod_head.numel()), dev)
+        workspace = _workspace(lib.cfgzip_displacements_workspace_bytes(V, N, prod_head.numel()), dev, stream)
     h, b, off, bd, P = _grammar_args(prod_head, prod_byte, prod_body_off, prod_body)
     total = prod_body.numel() if body_total is None else int(body_total)
     rc = lib.cfgzip_displacements(
@@ -772,7 +775,7 @@ def cfgzip_head_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.T
     loss = torch.empty((N,), dtype=torch.float32, device=dev) if loss is None else loss
     lse = torch.empty((N,), dtype=torch.float32, device=dev) if lse is None else lse
     if workspace is None:
-        workspace = _workspace(lib.cfgzip_head_loss_workspace_bytes(N, V, D, kind), dev)
+        workspace = _workspace(lib.cfgzip_head_loss_workspace_bytes(N, V, D, kind), dev, stream)
     _same_device(dev, loss=loss, lse=lse, workspace=workspace)
     rc = lib.cfgzip_head_loss(*args, _vector(loss, torch.float32, N, "loss"), _vector(lse, torch.float32, N, "lse"),
                               _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
@@ -814,7 +817,7 @@ def cfgzip_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: to
     if outs[0] is None and outs[2] is None:
         raise ValueError("one of the gradients must be wanted")
     if workspace is None:
-        workspace = _workspace(lib.cfgzip_head_loss_grad_workspace_bytes(N, V, D, kind), dev)
+        workspace = _workspace(lib.cfgzip_head_loss_grad_workspace_bytes(N, V, D, kind), dev, stream)
     _same_device(dev, lse=lse, grad_loss=grad_loss, grad_hidden=grad_hidden, grad_weight=grad_weight, workspace=workspace)
     rc = lib.cfgzip_head_loss_grad(*args, _vector(lse, torch.float32, N, "lse"),
                                    _vector(grad_loss, torch.float32, N, "grad_loss"), *outs,
@@ -917,7 +920,7 @@ def cfgzip_mx4_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.T
         raise ValueError(f"logits must have {B} rows")
     if workspace is None:
         need = lib.cfgzip_mx4_logits_workspace_bytes(kind, B, V, K, masks[1])
-        workspace = _workspace(need, dev) if need else None
+        workspace = _workspace(need, dev, stream) if need else None
     _same_device(dev, hidden=hidden, scales=scales, hidden_scales=hidden_scales, bits=bits, class_of_token=class_of_token,
                  logits=logits, workspace=workspace)
     rc = lib.cfgzip_mx4_logits(
