@@ -442,33 +442,36 @@ int cfgzip_nfa_advance_states(const int32_t *rel_rep, int32_t C, int32_t S,
  * The vocabulary projection at the end of a model, under the grammar's masks.  The masked logits that the calls above take are
  *     z[i][v] = sum_d hidden[i][d] * weight[v][d],
  * with -infinity where row i does not admit token v (paper Section 2.2).  The calls below train that projection without the
- * logits in memory, keep its weights in 4 bits, and make the masked logits from those.
+ * logits in memory (the gradients of few rows, up to 256, keep theirs in the workspace), keep its weights in 4 bits, and make the
+ * masked logits from those.
  *
  * Masks of all of them: bits_kind CFGZIP_BITS_TOKEN (int32 [rows][W(V)]), CFGZIP_BITS_CLASS (int32 [rows][W(C)], gathered through
- * class_of_token) or CFGZIP_BITS_NONE (bits, class_of_token NULL: every token is admitted).
+ * class_of_token, every entry in [0, C)) or CFGZIP_BITS_NONE (bits, class_of_token NULL: every token is admitted).
  */
 /*
  * cfgzip_head_loss: cross entropy of every row against its target over the tokens that the row admits,
  *     lse[i]  = log sum over admitted v of exp z[i][v]          (-inf if the row admits none)
  *     loss[i] = lse[i] - z[i][target[i]]
- * A target outside [0, V) is none: loss 0.  A target that the row does not admit: loss +inf.
+ * A target outside [0, V) is none: loss 0.  A target that the row does not admit: loss +inf.  Weights of tokens that no row admits may
+ * hold anything, those of the others have to be finite.
  *   hidden, weight   [N] and [V] rows of D elements, BF16 or F16 alike, hidden_stride and weight_stride ELEMENTS apart (>= D);
  *                    any alignment to whole elements, fastest at multiples of 16 bytes and D, strides multiples of 8
  *   target   int32 [N]
  *   loss, lse   out, float [N]
  *   ws       cfgzip_head_loss_workspace_bytes(N, V, D, bits_kind) bytes, 256-byte aligned
- * cfgzip_head_loss_grad: with grad_loss float [N] and the lse of the call above,
+ * cfgzip_head_loss_grad: with grad_loss float [N] and the lse of the call above (or a larger one: of a sum over more tokens than these),
  *     dz[i][v] = grad_loss[i] * (exp(z[i][v] - lse[i]) - [v = target[i]])   for admitted v, else 0
  *     grad_hidden[i] = sum_v dz[i][v] * weight[v],     grad_weight[v] = sum_i dz[i][v] * hidden[i]
  * Rows whose target is none or not admitted (no step lowers an infinite loss), and rows whose grad_loss is 0, have dz = 0
  * whatever their hidden states hold.  The weights have to be finite, those of masked tokens too, and so has grad_loss: one that is not
  * makes its row of grad_hidden and any of grad_weight infinite or NaN.
  *   grad_hidden, grad_weight   out, [N] and [V] rows of D elements of the inputs' type; either may be NULL
- * Up to 256 rows (128 of BF16 where D is no multiple of 8) dz is kept as the sum of two numbers of the inputs' type, of more rows in
- * fp16 for a piece of the vocabulary at a time.  In fp16 a row's dz has a factor of its own, so grad_loss may be of any size, rows of
- * any sizes beside each other; what dz is multiplied with is brought to fp16 as well: BF16 weights by a power of two (within 2^31 of
- * the largest they stay what they are, what is smaller is 2^-39 of the largest or less off), and for grad_weight
- * grad_loss[i] * hidden[i], rounded to fp16 where dz is one number (2^-37 of the largest or less off where it is small beside that).
+ * Up to 256 rows (128 of BF16 where D is no multiple of 8) logits and dz of the whole vocabulary are kept in the workspace (8 N V
+ * bytes), dz as the sum of two numbers of the inputs' type; of more rows dz in fp16, for a piece of the vocabulary at a time.
+ * In fp16 a row's dz has a factor of its own, so grad_loss may be of any size, rows of any sizes beside each other; what dz is
+ * multiplied with is brought to fp16 as well: BF16 weights by a power of two (within 2^31 of the largest they stay what they are, what
+ * is smaller is 2^-39 of the largest or less off), and for grad_weight grad_loss[i] * hidden[i], rounded to fp16 where dz is one
+ * number (2^-37 of the largest or less off where it is small beside that).
  * All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
  */
 size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);

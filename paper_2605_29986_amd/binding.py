@@ -761,7 +761,8 @@ def cfgzip_head_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.T
                      workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(loss, lse) float32 [N]: cross entropy of hidden [N, D] (bfloat16 or float16, rows any stride apart) through weight
     [V, D] against target int32 [N], over the tokens that `bits` admits (masks over classes with `class_of_token` and `C`, over
-    tokens without, every token without `bits`).  A target outside [0, V) has loss 0, one that is not admitted +inf."""
+    tokens without, every token without `bits`).  A target outside [0, V) has loss 0, one that is not admitted +inf.  Autograd knows nothing
+    of it: the loss of inputs that require a gradient has none, cfgzip_head_loss_grad makes it."""
     lib = _lib or load_library()
     if loss is None and lse is None and workspace is None and stream is None:
         out = _head_loss(hidden, weight, target, bits, class_of_token, C)

@@ -1,4 +1,5 @@
-// The vocabulary projection's loss under a grammar's masks, and its gradients, without the logits in memory.
+// The vocabulary projection's loss under a grammar's masks, and its gradients, without the logits in memory (but for gradients of few
+// rows).
 //
 //     z[i][v] = sum_d hidden[i][d] weight[v][d]
 //     lse[i] = log sum over admitted v of exp z[i][v],   loss[i] = lse[i] - z[i][target[i]]
@@ -35,7 +36,7 @@ constexpr int64_t slots() {
 }
 
 // What a product's tiles take, in microseconds: rounds of as many as are at work at a time, of so many steps each and a beginning and an
-// end.
+// end.  (Estimates from traces of whole calls, to choose between tiles by; not measured one by one.)
 template <typename S>
 constexpr double kStepTime = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : S::BM * S::BN == 8192 ? 0.6 : 0.35;
 template <typename S>
@@ -54,12 +55,13 @@ constexpr double kPieceProducts = 2e11;  // rows * hidden size * tokens
 // Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum beside lse, which
 // large logits round to few digits behind the point: a few rows' roundings do not average out, and reading the weights takes longer
 // than the products, which are twice as many.  With more rows dz is one fp16 number, for which bf16 weights are read and written once
-// more: 200 rows of 32,000 x 2,048 take 361 us so and 304 as two numbers (50,003 x 333, whose rows lie at no multiples of 16 bytes
-// until they are fp16, 213 and 292).
+// more.  Gradients of 200 bf16 rows of 32,000 x 2,048 take 298 us so and 244 as two numbers, of 128,256 x 4,096 1,840 and 1,607; of 50,003 x
+// 333, whose rows lie at no multiples of 16 bytes until they are fp16, 181 and 249.  fp16 rows would be faster in one number as well (200 of
+// 50,003 x 1,000 163 us for 247): there it is the precision.
 template <typename T>
 int32_t few_rows_of(int32_t D) { return std::is_same_v<T, Bf16> && D % 8 ? 128 : 256; }
-constexpr int32_t kPieceLeast = 2048;              // columns
-constexpr int32_t kSplitLeast = 256;               // of the sum over the vocabulary: the steps that a workgroup takes at the least
+constexpr int32_t kPieceLeast = 2048;              // tokens
+constexpr int32_t kSplitLeast = 256;               // tokens of grad_hidden's sum that a workgroup takes at the least
 constexpr int32_t kMaxRows = 1 << 22;               // offsets in a tile of dz stay below 2^32
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kInf = __builtin_inff();
@@ -723,9 +725,11 @@ Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows, bool halves) {
         const int64_t tiles = ceil_div(D, S::BM) * ceil_div(rows_dz, S::BN);
         for (int64_t s = 1; s == 1 || (s * kSplitLeast <= p.piece && tiles * s <= slots<S>() * 2); ++s) {
             const int64_t k_split = pad(ceil_div(p.piece, s), kStepK);
+            // a launch, and the shares written and read at 4 TB/s
             const double shares = s > 1 || pieces > 1 || p.parts > 1 ? 4.0 + (double)s * rows_dz * D * 8.0 / 4e6 : 0.0;
             const double tiles_time = (double)ceil_div(tiles * s, slots<S>()) * ((double)(k_split / kStepK) * kStepTime<S> + kEndsTime<S>);
-            // (or reading the weights, which rows of several tiles read more than once, partly from the caches)
+            // (or reading the weights at 4.5 TB/s, which rows of several tiles read more than once, half of it from the caches, and
+            // which takes twice as long through registers)
             const double time = std::max(tiles_time, (double)first * D * 2.0 / 4.5e6 * (0.5 + 0.5 * (double)ceil_div(rows_dz, S::BN)) * (D % 8 ? 2 : 1)) + shares;
             if (best == 0 || time < best) {
                 best = time;
