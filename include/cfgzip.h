@@ -469,9 +469,9 @@ int cfgzip_nfa_advance_states(const int32_t *rel_rep, int32_t C, int32_t S,
  * Up to 256 rows (128 of BF16 where D is no multiple of 8) logits and dz of the whole vocabulary are kept in the workspace (8 N V
  * bytes), dz as the sum of two numbers of the inputs' type; of more rows dz in fp16, for a piece of the vocabulary at a time.
  * In fp16 a row's dz has a factor of its own, so grad_loss may be of any size, rows of any sizes beside each other; what dz is
- * multiplied with is brought to fp16 as well: BF16 weights by a power of two (within 2^31 of the largest they stay what they are, what
- * is smaller is 2^-39 of the largest or less off), and for grad_weight grad_loss[i] * hidden[i], rounded to fp16 where dz is one
- * number (2^-37 of the largest or less off where it is small beside that).
+ * multiplied with is brought to fp16 as well: BF16 weights by a power of two, and for grad_weight hidden[i] by its row's power of two
+ * (what is not within 2^31 of the largest loses bits; it is 2^-39 of the largest weight, or grad_loss * hidden, or less off).  Of F16
+ * rows the target's dz, the largest of a row, is kept whole.
  * All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight is set to 0).
  */
 size_t cfgzip_head_loss_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t bits_kind);

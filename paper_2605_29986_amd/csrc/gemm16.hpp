@@ -302,7 +302,8 @@ struct Fragments {
     }
 };
 
-// behind the last of mma4's products: their sums may be read by what the compiler writes
+// behind the last of mma4's products: their sums may be read by what the compiler writes.  Read only: with something added to them in place
+// in lanes that a condition picks the compiler moved them about between the products, and results were wrong.
 template <typename S>
 __device__ __forceinline__ void settle(f32x4 (&acc)[S::FM][S::FN]) {
     if constexpr (S::kGroup == 4) {

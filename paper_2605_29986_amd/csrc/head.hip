@@ -46,7 +46,7 @@ double time_of(int64_t m, int64_t n, int64_t steps) {
     return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * kStepTime<S> + kEndsTime<S>);
 }
 
-// Of dz, and of weights in fp16 beside it, in memory at a time: seven eighths of the last-level cache, so that the products that read
+// Of dz, and of bf16 weights in fp16 or fp16 rows' rests beside it, in memory at a time: seven eighths of the last-level cache, so that the products that read
 // them find them there.  But each piece adds to grad_hidden's sums anew and has ends of its own: where rows times hidden size are few,
 // as many tokens as make that little beside the products, if dz alone still fits there and both take up to three times as much (777
 // rows of 128,256 x 4,096 in eight pieces 4.36 ms, in two 4.00, in one 3.95).
@@ -71,6 +71,18 @@ struct Masks {
     int64_t words;
 };
 
+// Of dz in one number for fp16 results its largest element, the target's, is kept to the last bit: what its rounding leaves goes to
+// grad_hidden as rest * weight[target], and to the token's row of grad_weight as the sum of rest * hidden over the token's rows, in their
+// order.  (Without, 777 rows of 50,003 x 1,000 were 1.7 times as far from 64 bits as their own rounding makes them.)
+struct Rests {
+    float *rest;       // [N]
+    int32_t *first;    // [V]: the first row whose target the token is
+    int32_t *count;    // [V]: how many there are
+    float *sums;       // [N + 1][ld]: at a token's first row; zeros at the last
+    int32_t ld;
+};
+constexpr int32_t kNoRow = 0x7FFFFFFF;
+
 struct LogitsArgs {
     Operand W, H;  // [V][D], [N][D]
     int32_t V, N, D;
@@ -84,6 +96,8 @@ struct LogitsArgs {
     // backward
     const float *lse;
     const float *factor;       // of a row's dz; 0: it has no gradient
+    const float *common;       // of all
+    Rests rests;               // fp16
     uint16_t *dz;              // [piece / 64][dz_rows][64]
     int64_t dz_rows;
     float *z;                  // [tokens / 64][N][64], -inf where not admitted
@@ -91,6 +105,12 @@ struct LogitsArgs {
 
 // what becomes of a tile of logits: maxima and sums; those and the logits themselves, of few rows; dz
 enum : int { STATISTICS = 0, KEPT = 1, GRADIENT = 2 };
+
+// exp(z - shift) grad, the same bits wherever it stands: the product is not fused with what is taken from it
+__device__ __forceinline__ float probability(float z, float shift, float grad) {
+#pragma clang fp contract(off)
+    return __builtin_amdgcn_exp2f((z - shift) * kLog2e) * grad;
+}
 
 template <typename T, typename S, bool DIRECT, int WHAT>
 __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
@@ -123,7 +143,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
             const int32_t row = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15), at = row < a.N ? row : a.N - 1;
             targets[j.value] = a.target[at];
             if constexpr (WHAT == GRADIENT) {
-                grads[j.value] = a.factor[at];
+                grads[j.value] = a.factor[at] * *a.common;
                 shifts[j.value] = a.lse[at];
             }
             each<kWords>([&](auto w) CFGZIP_INLINE { words[j.value][w.value] = ~0u; });
@@ -197,7 +217,7 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
                 each<S::FM>([&](auto i) CFGZIP_INLINE {
                     f32x4 d;
                     each<4>([&](auto r) CFGZIP_INLINE {
-                        d[r.value] = __builtin_amdgcn_exp2f((acc[i.value][j][r.value] - shift) * kLog2e) * grad;
+                        d[r.value] = probability(acc[i.value][j][r.value], shift, grad);
                     });
                     if (marked) {
                         each<4>([&](auto r) CFGZIP_INLINE {
@@ -206,6 +226,21 @@ __global__ __launch_bounds__(S::kThreads) void logits_kernel(LogitsArgs a) {
                     }
                     *reinterpret_cast<u32x2 *>(out + (i.value / 4) * (a.dz_rows * 64) + i.value % 4 * 16) = round4<Fp16>(d);
                 });
+                if constexpr (std::is_same_v<T, Fp16>) {
+                    if (marked) {  // the target's dz once more (among the elements it took the kernel 22 us of 150)
+                        float z = -kInf;
+                        each<S::FM * 4>([&](auto e) CFGZIP_INLINE {
+                            const bool here = mark == e.value / 4 * 16 + e.value % 4;
+                            z = here ? acc[e.value / 4][j][e.value % 4] : z;
+                        });
+                        const float d = probability(z, shift, grad) - grad;
+                        if (grad != 0.0f && z > -kInf) {
+                            a.rests.rest[row] = d - Fp16::value(Fp16::round(d));
+                            atomicMin(&a.rests.first[targets[j]], row);
+                            atomicAdd(&a.rests.count[targets[j]], 1);
+                        }
+                    }
+                }
             }
         });
     };
@@ -303,20 +338,16 @@ struct Rows {
 __device__ __forceinline__ int32_t exponent_of(float x) { return __builtin_amdgcn_frexp_expf(x) - 1; }
 
 // dz in fp16.  Its range holds a row's probabilities beside the row's own gradient, but not those of a row beside a gradient that
-// is 2^28 times as large, nor every gradient that there is.  So each row's dz has a factor of its own, 2^14 for any gradient, and the gradient,
-// digits * 2^(power + 14) with digits of 1 to 2, goes where it costs nothing: into the row of grad_hidden on its way out, and for grad_weight's
-// sum over the rows into the row's hidden states, as they become fp16 with a common power of two.  (With digits too: half the rounding of dz's
-// largest element, the target's, is none so.)  Where two numbers make up dz, and hidden states would be rounded more than it is, the digits
-// stay with dz.
+// is 2^28 times as large, nor every gradient that there is.  So a row's gradient is digits * 2^(power + 14) with digits of 1 to 2: dz has the
+// digits times 2^14, the power of two multiplies the row of grad_hidden on its way out and, for grad_weight's sum over the rows, the row's hidden
+// states as they become fp16 with a common power of two.
 struct RowFactors {
     float *dz;       // 0: the row has no gradient
-    float *digits;   // null: they stay with dz
     int32_t *power;
-    // [0] takes from the digits what they have in common, so that the same gradient for all rows, as that of a mean, costs no rounding;
-    // [1] its inverse.  null like the digits.
+    // [0] takes from the digits what they have in common, so that where all rows have the same gradient, as that of a mean, a row that is
+    // certain and wrong has dz without a rounding; [1] its inverse.  null where two numbers make up dz.
     float *common;
 };
-
 // dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
 // leave, the rest 0.  A thread has four tokens.
 template <typename T>
@@ -422,8 +453,14 @@ __device__ __forceinline__ int32_t largest_of(int32_t x, int32_t *shared) {
 constexpr int kRowsOfBlock = 16, kRowBlocks = 256;
 template <typename T>
 __global__ __launch_bounds__(kRowsOfBlock *kWave) void rows_kernel(Rows rows, const uint16_t *x, int64_t x_ld, int32_t D, uint16_t *y, int32_t y_ld,
-                                                                   RowFactors f, int32_t *largest) {
+                                                                   RowFactors f, Rests rests, int32_t *largest) {
     __shared__ int32_t shared[kRowsOfBlock];
+    if (rests.rest) {
+        for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows.V; i += (int64_t)gridDim.x * blockDim.x)
+            rests.first[i] = kNoRow, rests.count[i] = 0;
+        for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < rests.ld; i += gridDim.x * blockDim.x)
+            rests.sums[(int64_t)rows.N * rests.ld + i] = 0.0f;
+    }
     const int32_t blocks = gridDim.x - 1;
     if ((int32_t)blockIdx.x == blocks) {
         if (!f.common) return;
@@ -443,9 +480,9 @@ __global__ __launch_bounds__(kRowsOfBlock *kWave) void rows_kernel(Rows rows, co
         const int32_t e = finite ? exponent_of(grad) : 0, power = e - 14;
         const float digits = finite ? ldexpf(grad, -e) : grad;
         if (lane == 0) {
-            f.dz[row] = grad == 0.0f ? 0.0f : f.digits ? 0x1p14f : digits * 0x1p14f;
-            if (f.digits) f.digits[row] = digits;
+            f.dz[row] = digits * 0x1p14f;
             f.power[row] = power;
+            if (rests.rest) rests.rest[row] = 0.0f;
         }
         const uint16_t *const p = x + row * x_ld;
         uint16_t *const to = y + (int64_t)row * y_ld;
@@ -527,12 +564,12 @@ struct PowerOfTwo {
     }
 };
 
-// 16-bit rows as fp16, times a row's factors where there are some and the power of two that brings the largest of the `count` to 2^14
-// to 2^15 (with digits 2^12 to 2^15): bf16 weights within 2^31 of the largest keep their eight bits, what is smaller is 2^-39 of the
-// largest or less off (2^-37 with digits).  The rows `times` times over, y_ld elements each, zeros behind D and behind the last up to
-// `all`.  Leaves the power of two that takes that back in `back`.  A thread has four units of eight.
+// 16-bit rows as fp16, times a row's power of two where there is one and the one that brings the largest of the `count` to 2^14 to 2^15:
+// bf16 within 2^31 of the largest keeps its eight bits, what is smaller is 2^-39 of the largest or less off.  The rows `times` times over,
+// y_ld elements each, zeros behind D and behind the last up to `all`.  Leaves the power of two that takes that back in `back`.  A thread has
+// four units of eight.
 template <typename T>
-__global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, RowFactors f, const int32_t *largest, int32_t count, int32_t times,
+__global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, const int32_t *powers, const int32_t *largest, int32_t count, int32_t times,
                                                      uint16_t *y, int32_t y_ld, int32_t all, int32_t *back) {
     __shared__ int32_t shared[5];
     int32_t most = kNone;
@@ -541,10 +578,9 @@ __global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, RowFactors f, c
     if (threadIdx.x == 0) shared[4] = most;
     __syncthreads();
     most = shared[4];
-    const int32_t power = most == kNone ? 0 : (f.digits ? 13 : 14) - most;
+    const int32_t power = most == kNone ? 0 : 14 - most;
     if (blockIdx.x == 0 && threadIdx.x == 0) *back = -power;
     const int32_t units = y_ld / 8;
-    const float common = f.digits ? f.common[0] : 1.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t at = ((int64_t)blockIdx.x * 4 + i) * 256 + threadIdx.x;
@@ -552,7 +588,6 @@ __global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, RowFactors f, c
         const int32_t to = (int32_t)(at / units), c = (int32_t)(at % units) * 8, row = times == 2 && to >= x.rows ? to - x.rows : to;
         u32x4 v = {0, 0, 0, 0};
         int32_t e = power;
-        float factor = common;
         if (row < x.rows) {
             const uint16_t *const p = x.x + row * x.ld + c;
             if (c + 8 <= x.D) {
@@ -560,31 +595,54 @@ __global__ __launch_bounds__(256) void halves_kernel(Matrix16 x, RowFactors f, c
             } else {
                 for (int j = 0; c + j < x.D; ++j) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
             }
-            if (f.power) e += f.power[row];
-            if (f.digits) factor *= f.digits[row];
+            if (powers) e += powers[row];
         }
         const PowerOfTwo scale(e);
-        const float last = scale.b * factor;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            v[j] = Fp16::round2(T::value((uint16_t)v[j]) * scale.a * last, T::value((uint16_t)(v[j] >> 16)) * scale.a * last);
+            v[j] = Fp16::round2(T::value((uint16_t)v[j]) * scale.a * scale.b, T::value((uint16_t)(v[j] >> 16)) * scale.a * scale.b);
         *reinterpret_cast<u32x4 *>(y + (int64_t)to * y_ld + c) = v;
     }
+}
+
+// The sums of rest * hidden of the tokens v0 .. v0 + tokens - 1, in the order of their rows.  A workgroup has a row, and works if it is its
+// token's first, until it has met them all; most tokens have one.  A thread has four columns.
+__global__ __launch_bounds__(256) void rests_kernel(RowFactors f, Rests rests, const int32_t *target, int32_t N, int64_t v0, int32_t tokens,
+                                                    const uint16_t *hidden16) {
+    __shared__ uint64_t same[4];
+    const int32_t row = blockIdx.x, t = target[row], lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    if (f.dz[row] == 0.0f || t < v0 || t - v0 >= tokens || rests.first[t] != row) return;
+    const int32_t c = (blockIdx.y * 256 + threadIdx.x) * 4;
+    int32_t left = rests.count[t];
+    f32x4 sum = {0, 0, 0, 0};
+    for (int32_t first = row; left > 0 && first < N; first += 256) {
+        const int32_t j = first + threadIdx.x;
+        const uint64_t here = __builtin_amdgcn_ballot_w64(j < N && target[j] == t && f.dz[j] != 0.0f);
+        __syncthreads();
+        if (lane == 0) same[wave] = here;
+        __syncthreads();
+        for (int w = 0; w < 4; ++w) {
+            for (uint64_t more = same[w]; more; more &= more - 1, --left) {
+                const int32_t k = first + w * kWave + __builtin_ctzll(more);
+                if (c >= rests.ld) continue;
+                const float rest = rests.rest[k];
+                const u32x2 h = *reinterpret_cast<const u32x2 *>(hidden16 + (int64_t)k * rests.ld + c);
+                sum += rest * f32x4{Fp16::value((uint16_t)h[0]), Fp16::value((uint16_t)(h[0] >> 16)), Fp16::value((uint16_t)h[1]),
+                                    Fp16::value((uint16_t)(h[1] >> 16))};
+            }
+        }
+    }
+    if (c < rests.ld) *reinterpret_cast<f32x4 *>(rests.sums + (int64_t)row * rests.ld + c) = sum;
 }
 
 // What a result takes back of the factors of dz and of the product's other operand, each null where there is none.
 struct Factors {
     const float *all;      // of all results
-    const float *digits;   // of a row
     const int32_t *power;  // of a row
     const int32_t *back;   // of all results
-    __device__ __forceinline__ f32x2 of_all() const {
-        const PowerOfTwo scale(back ? *back : 0);
-        return f32x2{scale.a, scale.b * (all ? *all : 1.0f)};
-    }
     __device__ __forceinline__ f32x2 of(int32_t row) const {
         const PowerOfTwo scale((power ? power[row] : 0) + (back ? *back : 0));
-        return f32x2{scale.a, scale.b * (all ? *all : 1.0f) * (digits ? digits[row] : 1.0f)};
+        return f32x2{scale.a, scale.b * (all ? *all : 1.0f)};
     }
 };
 
@@ -599,11 +657,15 @@ struct GradArgs {
     float *sums;  // [splits][n][sums_ld], sums_ld = D rounded up to 4; null: the result goes to `out` at once
     int32_t sums_ld;
     int32_t add;  // to what is in `sums`
+    const int32_t *first;  // grad_weight in fp16: the tokens' rows with rests; or null
+    const float *rests;
+    int32_t rests_ld, rests_rows;
 };
 
 // grad_hidden: A = weight by columns, B = dz by rows.  grad_weight: A = hidden, B = dz, both by columns.
 // T: the operands' type, O: the results'.
-template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS>
+// RESTS: of grad_weight, what dz's rounding left is added.
+template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS, bool RESTS>
 __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
     // (weights end where the vocabulary does; hidden states and dz go on with zeros)
     using TileA = Tile<S::BM, S::kThreads, true, DIRECT, B_COLUMNS ? PADDED : ZERO>;
@@ -628,30 +690,44 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
         int32_t tm = 0, tn = 0, split = 0;
         place(i, tm, tn, split);
         f32x2 factor = {1.0f, 1.0f};
-        if (B_COLUMNS) factor = a.factors.of_all();  // (asked for once: 32,000 x 2,048 with 64 rows 69 us for 79)
+        if (B_COLUMNS) factor = a.factors.of(0);  // (asked for once: 32,000 x 2,048 with 64 rows 69 us for 79)
         each<S::FN>([&](auto j) CFGZIP_INLINE {
             const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
             if (n >= a.n) return;
             if (!B_COLUMNS && !a.sums) factor = a.factors.of(n);
-            each<S::FM>([&](auto i) CFGZIP_INLINE {
-                const int32_t c = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
-                if (c >= a.D) return;
-                if (a.sums) {
-                    f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
-                    *p = a.add ? *p + acc[i.value][j.value] : acc[i.value][j.value];
-                } else {
-                    store4<O>(a.out + n * a.out_ld, c, a.D, acc[i.value][j.value] * factor[0] * factor[1]);
-                }
-            });
+            auto store_some = [&](auto with, const float *rests) CFGZIP_INLINE {
+                each<S::FM>([&](auto i) CFGZIP_INLINE {
+                    const int32_t c = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
+                    if (c >= a.D) return;
+                    f32x4 x = acc[i.value][j.value];
+                    if constexpr (with.value) x += *reinterpret_cast<const f32x4 *>(rests + c);
+                    if (!RESTS && a.sums) {
+                        f32x4 *p = reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + c);
+                        *p = a.add ? *p + x : x;
+                    } else {
+                        store4<O>(a.out + n * a.out_ld, c, a.D, x * factor[0] * factor[1]);
+                    }
+                });
+            };
+            if constexpr (RESTS) {
+                // whose sum of rests belongs to the token; the last one's is 0
+                const int32_t row = a.first[n];
+                if (__builtin_amdgcn_ballot_w64(row != kNoRow) != 0)  // (few tokens are a row's target)
+                    store_some(std::true_type{}, a.rests + (int64_t)(row != kNoRow ? row : a.rests_rows) * a.rests_ld);
+                else store_some(std::false_type{}, nullptr);
+            } else {
+                store_some(std::false_type{}, nullptr);
+            }
         });
     };
     multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
 }
 
-// Joins grad_hidden's shares of the sum (and the two numbers of few rows' dz).
+// Joins grad_hidden's shares of the sum (and the two numbers of few rows' dz, or what is left of dz in one).
 template <typename T>
 __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t count, int32_t n, int32_t D, int32_t sums_ld,
-                                                         Factors factors, uint16_t *out, int64_t out_ld) {
+                                                         Factors factors, const float *rest, const int32_t *target, const uint16_t *weight,
+                                                         int64_t weight_ld, uint16_t *out, int64_t out_ld) {
     const int32_t units = sums_ld / 4;
     const int64_t k = (int64_t)blockIdx.x * kWave + threadIdx.x;
     if (k >= (int64_t)n * units) return;
@@ -666,6 +742,12 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_
         for (int i = 0; i < 16; ++i) y[i] = s + i < count ? *reinterpret_cast<const f32x4 *>(p + (s + i) * step) : f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 16; ++i) x += y[i];
+    }
+    if (rest && rest[row] != 0.0f) {
+        const uint16_t *const w = weight + target[row] * weight_ld + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < D) x[i] += rest[row] * T::value(w[i]);
     }
     store4<T>(out + row * out_ld, c, D, x * factor[0] * factor[1]);
 }
@@ -699,7 +781,7 @@ struct Plan {
     bool direct_out;    // grad_hidden in one go
 };
 
-// halves: weights are written in fp16, a piece at a time
+// halves: bf16 weights are written in fp16, a piece at a time
 Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows, bool halves) {
     Plan p{};
     p.parts = N <= few_rows ? 2 : 1;
@@ -709,11 +791,13 @@ Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows, bool halves) {
     // (tiles of logits leave zeros behind N as well, and grad_weight's sum goes over whole steps of rows)
     // A piece is a whole number of rounds of 256 tiles of logits, one to a compute unit, and one round at the least.
     const int64_t bytes = (pad(rows_dz, 256) + (halves && p.parts == 1 ? pad(D, 8) : 0)) * 2;  // of a token
+    const int64_t rests = halves ? 0 : (int64_t)N * p.d_pad * 4 + (int64_t)V * 8;
+    const int64_t there = std::max(kPieceBytes - rests, kPieceBytes / 2);
     const int64_t round = std::max<int64_t>(slots<Shape256>() / ceil_div(N, p.logits_rows), 1) * Shape256::BM;
-    const int64_t fit = std::min(kPieceBytes / (pad(rows_dz, 256) * 2), 3 * kPieceBytes / bytes) / round;
+    const int64_t fit = std::min(there / (pad(rows_dz, 256) * 2), 3 * there / bytes) / round;
     const int64_t products = std::min((int64_t)std::min(kPieceProducts / N / D / (double)round + 0.5, 1e9), fit);
     const int64_t least = std::max<int64_t>(ceil_div(kPieceLeast, round), 1);
-    const int64_t rounds = std::max(std::max(kPieceBytes / bytes / round, products), least);
+    const int64_t rounds = std::max(std::max(there / bytes / round, products), least);
     const int64_t pieces = p.parts == 2 ? 1 : ceil_div(V, rounds * round);
     p.piece = (int32_t)(pieces == 1 ? pad(V, 256) : ceil_div(ceil_div(V, round), pieces) * round);
     // grad_hidden's sum runs over the vocabulary: it is split so that its tiles fill the chip, which costs a pass over the shares
@@ -745,7 +829,7 @@ Plan plan_of(int32_t N, int32_t V, int32_t D, int32_t few_rows, bool halves) {
     p.rows_pad = (int32_t)pad(rows_dz, std::max(std::max(p.rows, p.logits_rows), (int)kStepK));
     p.splits = (int32_t)ceil_div(first, best_split);  // of the first piece; later ones add to them
     p.sums_ld = (int32_t)pad(D, 4);
-    p.direct_out = pieces == 1 && p.splits == 1 && p.parts == 1;
+    p.direct_out = halves && pieces == 1 && p.splits == 1 && p.parts == 1;  // (fp16 rows: the rests are added behind it)
     return p;
 }
 
@@ -819,13 +903,13 @@ int launch_logits(int rows, LogitsArgs a, int32_t tokens, bool direct, hipStream
     }
 }
 
-template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS>
+template <typename T, typename O, typename S, bool DIRECT, bool B_COLUMNS, bool RESTS = false>
 int launch_grad_of(GradArgs a, hipStream_t stream) {
     a.tiles_m = (int32_t)ceil_div(a.D, S::BM);
     a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
     const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = work < slots<S>() ? work : slots<S>();
     if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
-    hipLaunchKernelGGL((grad_kernel<T, O, S, DIRECT, B_COLUMNS>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
+    hipLaunchKernelGGL((grad_kernel<T, O, S, DIRECT, B_COLUMNS, RESTS>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a);
     return check_launch();
 }
 
@@ -839,14 +923,20 @@ int launch_grad_hidden(int rows, const GradArgs &a, hipStream_t stream) {
     }
 }
 
-template <typename T, typename O>
-int launch_grad_weight(const GradArgs &a, hipStream_t stream) {
+template <typename T, typename O, bool RESTS>
+int launch_grad_weight_of(const GradArgs &a, hipStream_t stream) {
     const int32_t steps = (int32_t)ceil_div(a.k, kStepK);
     const double large = time_of<Shape256>(a.D, a.n, steps), middle = time_of<Shape128>(a.D, a.n, steps),
                  flat = time_of<ShapeFlat>(a.D, a.n, steps), small = time_of<Shape64>(a.D, a.n, steps);
-    if (large <= middle && large <= flat && large <= small) return launch_grad_of<T, O, Shape256, true, true>(a, stream);
-    if (flat <= middle && flat <= small) return launch_grad_of<T, O, ShapeFlat, true, true>(a, stream);
-    return middle <= small ? launch_grad_of<T, O, Shape128, true, true>(a, stream) : launch_grad_of<T, O, Shape64, true, true>(a, stream);
+    if (large <= middle && large <= flat && large <= small) return launch_grad_of<T, O, Shape256, true, true, RESTS>(a, stream);
+    if (flat <= middle && flat <= small) return launch_grad_of<T, O, ShapeFlat, true, true, RESTS>(a, stream);
+    return middle <= small ? launch_grad_of<T, O, Shape128, true, true, RESTS>(a, stream) : launch_grad_of<T, O, Shape64, true, true, RESTS>(a, stream);
+}
+template <typename T, typename O>
+int launch_grad_weight(const GradArgs &a, hipStream_t stream) {
+    if constexpr (std::is_same_v<O, Fp16>)
+        if (a.first) return launch_grad_weight_of<T, O, true>(a, stream);
+    return launch_grad_weight_of<T, O, false>(a, stream);
 }
 
 int copy_rows(const LossCall &c, int32_t times, int32_t all, bool whole, const Rows &rows, uint16_t *y, int32_t y_ld,
@@ -903,8 +993,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     CFGZIP_TRY(masks_of(c, ws, stream, masks, launch));
     const bool few = p.parts == 2;
     // Of many rows dz is one fp16 number, whose eleven bits leave bf16 gradients as near to the truth as their own rounding does (in bf16
-    // dz's largest element, the target's, was off by as much as all of that) and fp16 ones up to 1.4 times as far off.  The products'
-    // other sides, where they are bf16, become fp16 too.
+    // dz's largest element, the target's, was off by as much as all of that); of fp16 ones the target's element is kept whole.  The
+    // products' other sides, where they are bf16, become fp16 too.
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
     const bool halves = kBf16 && !few, fp16_dz = !kBf16 || !few;
     const int32_t rows_dz = c.N * p.parts, count = part_count(p.logits_rows, c.V);
@@ -912,12 +1002,17 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     RowFactors of_rows{};                // of dz in fp16
     int32_t *back = ws.take<int32_t>(2);  // of weights in fp16; of hidden states times their rows' factors
     int32_t *largest_w = ws.take<int32_t>(kWeightBlocks), *largest_h = ws.take<int32_t>(kRowBlocks);
+    Rests rests{};                       // of dz in one number for fp16
     if (fp16_dz) {
         of_rows.dz = ws.take<float>(c.N);
         of_rows.power = ws.take<int32_t>(c.N);
-        if (!few) {
-            of_rows.digits = ws.take<float>(c.N);
-            of_rows.common = ws.take<float>(2);
+        if (!few) of_rows.common = ws.take<float>(2);
+        if (!few && !kBf16) {
+            rests.rest = ws.take<float>(c.N);
+            rests.first = ws.take<int32_t>(c.V);
+            rests.count = ws.take<int32_t>(c.V);
+            rests.ld = p.d_pad;
+            rests.sums = ws.take<float>((size_t)(c.N + 1) * p.d_pad);
         }
     }
     const int32_t copy_rows_pad = (int32_t)pad(rows_dz, kStepK), w_pad = (int32_t)pad(c.D, 8);
@@ -931,19 +1026,19 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     f32x2 *parts = few ? ws.take<f32x2>((size_t)count * c.N) : nullptr, *whole = few ? ws.take<f32x2>(c.N) : nullptr;
     if (!launch) return CFGZIP_OK;
     const Rows rows{grad_loss, c.target, c.N, c.V, masks};
-    auto to_halves = [&](const Matrix16 &x, const RowFactors &f, const int32_t *most, int32_t many, int32_t times, uint16_t *y, int32_t y_ld,
+    auto to_halves = [&](const Matrix16 &x, const int32_t *powers, const int32_t *most, int32_t many, int32_t times, uint16_t *y, int32_t y_ld,
                          int32_t all, int32_t *to) {
-        hipLaunchKernelGGL(halves_kernel<T>, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, f, most,
-                           many, times, y, y_ld, all, to);
+        hipLaunchKernelGGL(halves_kernel<T>, dim3((uint32_t)ceil_div((int64_t)all * (y_ld / 8), 1024)), dim3(256), 0, stream, x, powers,
+                           most, many, times, y, y_ld, all, to);
         return check_launch();
     };
     if (fp16_dz) {
         const int32_t blocks = std::min((int32_t)ceil_div(c.N, kRowsOfBlock), kRowBlocks);
         hipLaunchKernelGGL(rows_kernel<T>, dim3(blocks + 1), dim3(kRowsOfBlock * kWave), 0, stream, rows,
-                           static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.D, copy, p.d_pad, of_rows, largest_h);
+                           static_cast<const uint16_t *>(c.hidden), c.hidden_stride, c.D, copy, p.d_pad, of_rows, rests, largest_h);
         CFGZIP_TRY(check_launch());
         if (grad_weight)
-            CFGZIP_TRY(to_halves(Matrix16{copy, p.d_pad, c.N, c.D}, of_rows, largest_h, blocks, p.parts, copy16, p.d_pad, copy_rows_pad,
+            CFGZIP_TRY(to_halves(Matrix16{copy, p.d_pad, c.N, c.D}, of_rows.power, largest_h, blocks, p.parts, copy16, p.d_pad, copy_rows_pad,
                                  back + 1));
     } else {
         CFGZIP_TRY(copy_rows(c, p.parts, copy_rows_pad, false, rows, copy, p.d_pad, stream));
@@ -953,10 +1048,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
                            Matrix16{static_cast<const uint16_t *>(c.weight), c.weight_stride, c.V, c.D}, largest_w);
         CFGZIP_TRY(check_launch());
     }
-    const Factors factors_h = fp16_dz ? Factors{nullptr, of_rows.digits, of_rows.power, halves ? back : nullptr}
-                                      : Factors{unscale, nullptr, nullptr, nullptr};
-    const Factors factors_w = fp16_dz ? Factors{few ? nullptr : of_rows.common + 1, nullptr, nullptr, back + 1}
-                                      : Factors{unscale, nullptr, nullptr, nullptr};
+    const float *const all = !fp16_dz ? unscale : few ? nullptr : of_rows.common + 1;
+    const Factors factors_h{all, of_rows.power, halves ? back : nullptr}, factors_w{all, nullptr, fp16_dz ? back + 1 : nullptr};
     const uint16_t *weight = static_cast<const uint16_t *>(c.weight);
     const bool direct = whole_units(c.weight, c.weight_stride, c.D);
     for (int64_t v0 = 0; v0 < c.V; v0 += p.piece) {
@@ -973,6 +1066,8 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
         a.target = c.target;
         a.lse = lse;
         a.factor = of_rows.dz;
+        a.common = of_rows.common;
+        a.rests = rests;
         a.dz = dz;
         a.dz_rows = p.rows_pad;
         a.parts = parts;
@@ -1005,7 +1100,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.splits = (int32_t)ceil_div(tokens, g.k_split);
             if (halves) {
                 const Matrix16 w{first, c.weight_stride, tokens, c.D};
-                CFGZIP_TRY(to_halves(w, RowFactors{}, largest_w, kWeightBlocks, 1, weight16, w_pad, tokens, back));
+                CFGZIP_TRY(to_halves(w, nullptr, largest_w, kWeightBlocks, 1, weight16, w_pad, tokens, back));
                 CFGZIP_TRY((launch_grad_hidden<Fp16, T, true>(p.rows, g, stream)));
             } else {
                 CFGZIP_TRY(direct ? (launch_grad_hidden<T, T, true>(p.rows, g, stream))
@@ -1022,6 +1117,15 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
             g.k_split = (int32_t)pad(rows_dz, kStepK);
             g.splits = 1;
             g.factors = factors_w;
+            if (rests.rest) {
+                hipLaunchKernelGGL(rests_kernel, dim3(c.N, (uint32_t)ceil_div(p.d_pad, 1024)), dim3(256), 0, stream, of_rows, rests, c.target,
+                                   c.N, v0, tokens, copy16);
+                CFGZIP_TRY(check_launch());
+                g.first = rests.first + v0;
+                g.rests = rests.sums;
+                g.rests_ld = rests.ld;
+                g.rests_rows = c.N;
+            }
             g.out = grad_weight + v0 * gw_stride;
             g.out_ld = gw_stride;
             CFGZIP_TRY(halves ? (launch_grad_weight<Fp16, T>(g, stream)) : (launch_grad_weight<T, T>(g, stream)));
@@ -1030,7 +1134,7 @@ int backward(const LossCall &c, const float *lse, const float *grad_loss, uint16
     if (grad_hidden && !p.direct_out) {
         const int64_t units = (int64_t)c.N * (p.sums_ld / 4);
         hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, sums, p.splits * p.parts, c.N,
-                           c.D, p.sums_ld, factors_h, grad_hidden, gh_stride);
+                           c.D, p.sums_ld, factors_h, rests.rest, c.target, weight, c.weight_stride, grad_hidden, gh_stride);
         CFGZIP_TRY(check_launch());
     }
     return CFGZIP_OK;

@@ -44,19 +44,19 @@ def gradients(h, w, target, allowed, g, lse, dtype, few):
         form = 2.0 ** -16 * np.abs(dz)
     elif few:  # a row's factor makes its gradient 2^14 to 2^15
         form = 2.0 ** -22 * np.abs(dz) + 2.0 ** -39 * size_g
-    else:  # 2^14
-        form = 2.0 ** -11 * np.abs(dz) + 2.0 ** -39 * size_g
+    else:  # 2^13 to 2^15
+        form = 2.0 ** -11 * np.abs(dz) + 2.0 ** -38 * size_g
+        if dtype == "f16":  # of the target's element nothing is lost
+            form[rows[live], at[live]] = 2 * F32 * np.abs(dz)[rows[live], at[live]]
     dz_err = np.where(here, form * 1.01 + size_g * (p * p_rel + 2 * F32), 0.0)
     w_err = np.zeros_like(w)
     if dtype == "bf16" and not few:
         most = np.max(np.abs(w))
         w_err = np.where((w != 0) & (np.abs(w) < 2.0 ** -31 * most), 2.0 ** -39 * most, 0.0)
-    h_err = np.zeros_like(h)  # of g h, divided by g
+    h_err = np.zeros_like(h)  # of g h, divided by g: the largest becomes 2^14 at the least
     if dtype == "f16" or not few:
-        share = np.max(np.abs(h) * size_g, initial=0.0) * 2.0 ** -37
+        share = np.max(np.abs(h) * size_g, initial=0.0) * 2.0 ** -39
         h_err = np.where(live[:, None], share / np.where(live, np.abs(g), 1.0)[:, None], 0.0)
-        if not few:
-            h_err = h_err + np.abs(h) * (2.0 ** -11 + 4 * F32) * 1.01
     u, floor = HALF_STEP[dtype], SMALLEST_HALF_STEP[dtype]
     gh, gw = dz @ w, dz.T @ h
     return {

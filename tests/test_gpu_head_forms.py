@@ -86,3 +86,19 @@ def test_several_pieces(lib):  # noqa: F811
         bound = egw + wgw.abs() * 2.0 ** -8 * 1.01 + 1e-30
         assert ((gw[v:v + n].double() - wgw).abs() <= bound).all(), v
     assert ((gh.double() - wgh).abs() <= egh + wgh.abs() * 2.0 ** -8 * 1.01 + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("N,V,D", [(300, 16384, 1024), (260, 20000, 1000), (40, 16384, 1024), (2048, 6000, 1001), (1030, 4100, 2048)])
+def test_sizes_of_the_largest_tiles(lib, N, V, D, dtype):  # noqa: F811
+    """Enough tiles of 256 x 256 for all compute units in one of the three products at least, several rows with one target, and tokens that
+    are nobody's"""
+    print(f"case {dtype} N={N} V={V} D={D}", flush=True)
+    rng = np.random.default_rng(N + V + D)
+    w = torch.from_numpy(rng.standard_normal((V, D)) * (2.0 / np.sqrt(D))).to(TYPES[dtype])
+    h = torch.from_numpy(rng.standard_normal((N, D))).to(TYPES[dtype])
+    target = rng.integers(0, V, size=N)
+    target[::3] = target[0]
+    target[-1], target[5] = -1, V
+    g = (rng.standard_normal(N) * 8).astype(np.float32)
+    _check(lib, h, w, target, np.ones((N, V), bool), g, dtype)

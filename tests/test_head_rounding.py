@@ -55,11 +55,14 @@ def test_the_forms_pass(N, V, D, dtype):
         kept = (hi + _round(x - hi, "f16")) * 2.0 ** (e - 14)
         gh, gw = kept @ w, kept.T @ h
     else:
-        kept = _round(dz * 2.0 ** 14, "f16") * 2.0 ** -14
-        common = digits[np.argmax(np.abs(g))]
-        top = 13 - np.max(np.floor(np.log2(np.abs(h))) + e)
-        h16 = _round(h * (digits / common) * 2.0 ** (e + top), "f16") * common * 2.0 ** -top
-        gh, gw = (kept @ w) * g[:, None], kept.T @ h16
+        common = np.abs(digits[np.argmax(np.abs(g))])
+        x = dz * digits / common * 2.0 ** 14
+        kept = _round(x, "f16")
+        if dtype == "f16":  # of the target's element nothing is lost
+            kept[np.arange(N), target] = x[np.arange(N), target]
+        top = 14 - np.max(np.floor(np.log2(np.abs(h))) + e)
+        h16 = _round(h * 2.0 ** (e + top), "f16") * 2.0 ** -top
+        gh, gw = (kept @ w) * common * 2.0 ** (e - 14), kept.T @ h16 * common * 2.0 ** -14
     assert _worst(r, gh, gw, dtype) < 1.0
 
 
@@ -96,3 +99,23 @@ def test_one_factor_for_all_rows_does_not(dtype):
     r = gradients(h, w, target, np.ones((N, V), bool), g, lse, dtype, False)
     kept = _round(dz * g[:, None] * 4, "f16") / 4
     assert _worst(r, kept @ w, kept.T @ h, dtype) > 1.0
+
+
+@pytest.mark.parametrize("N,V,D", [s for s in SIZES if s[0] > 256])
+def test_many_fp16_rows_without_the_targets_rest_do_not(N, V, D):
+    h, w, target, g, lse, dz = _case(N, V, D, "f16", N + V)
+    h, target = _round(h * 0.02, "f16"), np.arange(N) % V  # flat probabilities: the target's element is all that counts
+    z = h @ w.T
+    lse = np.log(np.exp(z).sum(1))
+    dz = np.exp(z - lse[:, None])
+    dz[np.arange(N), target] -= 1.0
+    g = g * 4096
+    r = gradients(h, w, target, np.ones((N, V), bool), g, lse, "f16", False)
+    most = np.abs(g).max()
+    x = dz * g[:, None] / most * 2.0 ** 14
+    whole = _round(x, "f16")
+    gh, gw = whole @ w * most * 2.0 ** -14, whole.T @ h * most * 2.0 ** -14
+    assert _worst(r, gh, gw, "f16") > 1.0
+    whole[np.arange(N), target] = x[np.arange(N), target]
+    gh, gw = whole @ w * most * 2.0 ** -14, whole.T @ h * most * 2.0 ** -14
+    assert _worst(r, gh, gw, "f16") < 1.0
