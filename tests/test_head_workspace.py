@@ -36,7 +36,7 @@ def test_pieces_do_not_grow_with_the_vocabulary(need):
     assert need(4096, 4_000_000, 4096) <= need(4096, 128256, 4096) + 8 * (4_000_000 - 128256) + MB
 
 
-@pytest.mark.parametrize("N", [1, 16, 128])
+@pytest.mark.parametrize("N", [1, 16, 128, 256])
 def test_few_rows_keep_their_logits(need, N):
     """Logits in 32 bits and dz in twice 16 of every token, and no copy of the weights."""
     V, D = 128256, 4096
