@@ -46,10 +46,10 @@ double time_of(int64_t m, int64_t n, int64_t steps) {
     return (double)ceil_div(ceil_div(m, S::BM) * ceil_div(n, S::BN), slots<S>()) * ((double)steps * kStepTime<S> + kEndsTime<S>);
 }
 
-// Of dz, and of bf16 weights in fp16 or fp16 rows' rests beside it, in memory at a time: seven eighths of the last-level cache, so that the products that read
-// them find them there.  But each piece adds to grad_hidden's sums anew and has ends of its own: where rows times hidden size are few,
-// as many tokens as make that little beside the products, if dz alone still fits there and both take up to three times as much (777
-// rows of 128,256 x 4,096 in eight pieces 4.36 ms, in two 4.00, in one 3.95).
+// Of dz, and of bf16 weights in fp16 or fp16 rows' rests beside it, in memory at a time: seven eighths of the last-level cache, so that the
+// products that read them find them there.  But each piece adds to grad_hidden's sums anew and has ends of its own: where rows times
+// hidden size are few, as many tokens as make that little beside the products, if dz alone still fits there and both take up to three
+// times as much (777 rows of 128,256 x 4,096 in eight pieces 4.36 ms, in two 4.00, in one 3.95).
 constexpr int64_t kPieceBytes = (int64_t)224 << 20;
 constexpr double kPieceProducts = 2e11;  // rows * hidden size * tokens
 // Up to so many rows dz is kept in two 16-bit numbers, and its probabilities come from the row's maximum and sum beside lse, which
@@ -337,10 +337,10 @@ struct Rows {
 // floor(log2 |x|) of a finite x other than 0
 __device__ __forceinline__ int32_t exponent_of(float x) { return __builtin_amdgcn_frexp_expf(x) - 1; }
 
-// dz in fp16.  Its range holds a row's probabilities beside the row's own gradient, but not those of a row beside a gradient that
-// is 2^28 times as large, nor every gradient that there is.  So a row's gradient is digits * 2^(power + 14) with digits of 1 to 2: dz has the
-// digits times 2^14, the power of two multiplies the row of grad_hidden on its way out and, for grad_weight's sum over the rows, the row's hidden
-// states as they become fp16 with a common power of two.
+// dz in fp16.  Its range holds a row's probabilities beside the row's own gradient, but not those of a row beside a gradient that is
+// 2^28 times as large, nor every gradient that there is.  So a row's gradient is digits * 2^(power + 14) with digits of 1 to 2: dz has
+// the digits times 2^14, the power of two multiplies the row of grad_hidden on its way out and, for grad_weight's sum over the rows,
+// the row's hidden states as they become fp16 with a common power of two.
 struct RowFactors {
     float *dz;       // 0: the row has no gradient
     int32_t *power;
@@ -348,6 +348,7 @@ struct RowFactors {
     // certain and wrong has dz without a rounding; [1] its inverse.  null where two numbers make up dz.
     float *common;
 };
+
 // dz of few rows from their logits, as the sum of two 16-bit numbers: rows 0 .. N - 1 of dz are the first ones, N .. 2 N - 1 what they
 // leave, the rest 0.  A thread has four tokens.
 template <typename T>
@@ -711,6 +712,8 @@ __global__ __launch_bounds__(S::kThreads) void grad_kernel(GradArgs a) {
             };
             if constexpr (RESTS) {
                 // whose sum of rests belongs to the token; the last one's is 0
+                // (the loop twice, behind a condition of the whole wave: one load that each lane's own condition guards took the kernel
+                // 263 us for 151, its loads' addresses out of the registers)
                 const int32_t row = a.first[n];
                 if (__builtin_amdgcn_ballot_w64(row != kNoRow) != 0)  // (few tokens are a row's target)
                     store_some(std::true_type{}, a.rests + (int64_t)(row != kNoRow ? row : a.rests_rows) * a.rests_ld);
