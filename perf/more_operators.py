@@ -3,8 +3,8 @@ read from its logits under a grammar's masks, each forwards and backwards.
 
 Four kinds, each through the public entry points of ``paper_2605_29986_amd``:
 
-  score   log probabilities of given tokens over the tokens that each row's mask admits, entropy, log-sum-exp, and the best
-          alternatives (``cfgzip_token_logprobs``)
+  score   log probabilities of given tokens over the tokens that each row's mask admits, entropy, what the gradient
+          needs of a row, and the best alternatives (``cfgzip_token_logprobs``)
   policy  the same with the gradient of the logits, of log probabilities and entropy (``cfgzip_token_logprobs``,
           ``cfgzip_token_logprobs_grad``)
   layer   matrix product with bias, activation and residual (``cfgzip_head_layer``)
@@ -12,8 +12,8 @@ Four kinds, each through the public entry points of ``paper_2605_29986_amd``:
 
 The definitions.  Row i admits token v if bit class_of_token[v] of bits[i] is set (every token without a mask) and its logit is
 not -inf.  z[i][v] = logits[i][v] / temperature.  lse[i] = log sum over admitted v of exp z[i][v], -inf if there are none.  For a given
-token t: logprob = z[i][t] - lse[i]; 0 if t lies outside [0, V), which makes it none; -inf if the row does not admit it.  With
-p = exp(z - lse): entropy[i] = -sum over admitted v of p log p, 0 if there are none.  Alternatives: the admitted tokens with the largest logits, largest
+token t: logprob = z[i][t] - lse[i]; 0 if t lies outside [0, V), which makes it none; -inf if the row does not admit it.  stats[i] is the largest
+admitted logit, and lse[i] less that one's z (both -inf if there are none).  With p = exp(z - lse): entropy[i] = -sum over admitted v of p log p, 0 if there are none.  Alternatives: the admitted tokens with the largest logits, largest
 first, of equal ones the lowest; token -1 with -inf where there are no more.  With gradients g of the log probabilities and e of the entropy, over
 admitted v:
 
@@ -235,7 +235,6 @@ def _plain_score(s):
     e = torch.exp(z - shift)
     total = e.sum(1, keepdim=True)
     log_total = torch.log(total)
-    lse = log_total + shift
     there = (t >= 0) & (t < V)
     at = t.clamp(0, V - 1)
     z_t = torch.gather(z, 1, at)
@@ -244,7 +243,7 @@ def _plain_score(s):
     p = torch.where(total > 0, e / total, torch.zeros_like(e))
     log_p = torch.where(p > 0, (z - shift) - log_total, torch.zeros_like(z))
     entropy = -(p * log_p).sum(1)
-    out = {"logprob": logprob, "entropy": entropy, "lse": lse[:, 0]}
+    out = {"logprob": logprob, "entropy": entropy, "stats": torch.cat([x.amax(1, keepdim=True), log_total], 1)}
     if case["top"]:
         # one whole number for value and place: larger for larger logits, and of equal ones for the lower token
         b = (x + 0.0).view(torch.int32).long()
@@ -320,12 +319,12 @@ def run(s):
         how = {"temperature": case["temperature"]}
         if s["bits"] is not None:
             how.update(bits=s["bits"], class_of_token=s["c"], C=case["C"])
-        logprob, entropy, lse, top_tokens, top_logprobs = cfgzip.cfgzip_token_logprobs(s["logits"], s["tokens"], top=case["top"], **how)
-        out = {"logprob": logprob, "entropy": entropy, "lse": lse}
+        logprob, entropy, stats, top_tokens, top_logprobs = cfgzip.cfgzip_token_logprobs(s["logits"], s["tokens"], top=case["top"], **how)
+        out = {"logprob": logprob, "entropy": entropy, "stats": stats}
         if case["top"]:
             out.update(top_tokens=top_tokens, top_logprobs=top_logprobs)
         if kind == "policy":
-            out["grad_logits"] = cfgzip.cfgzip_token_logprobs_grad(s["logits"], s["tokens"], logprob, lse, s["grad_logprob"], entropy=entropy,
+            out["grad_logits"] = cfgzip.cfgzip_token_logprobs_grad(s["logits"], s["tokens"], logprob, stats, s["grad_logprob"], entropy=entropy,
                                                                    grad_entropy=s["grad_entropy"], **how)
         return out
     act = None if case["act"] == "none" else case["act"]
@@ -381,7 +380,9 @@ def _exact_rows(s, lo, hi):
     log_p = torch.where(z == NINF, NINF, z - lse[:, None])
     p = torch.exp(log_p)
     entropy = -torch.special.xlogy(p, p).sum(1)
-    out = {"logprob": logprob, "entropy": entropy, "lse": lse}
+    most = raw.max(1).values
+    log_sum = torch.where(most == NINF, NINF, lse - most / case["temperature"])
+    out = {"logprob": logprob, "entropy": entropy, "stats": torch.stack([most, log_sum], 1)}
     if case["top"]:
         value, token = torch.sort(raw, dim=1, descending=True, stable=True)
         value, token = value[:, :case["top"]], token[:, :case["top"]]
