@@ -519,6 +519,53 @@ int cfgzip_mx4_logits(const void *hidden, int32_t hidden_dtype, int64_t hidden_s
                       void *logits, int32_t dtype, int64_t row_stride,
                       void *ws, size_t ws_bytes, void *stream);
 
+/*
+ * What is read from logits under the grammar's masks: log probabilities over the tokens that a row admits.  With
+ *     z[i][v] = logits[i][v] / temperature   for admitted v: its bit set in the mask, and its logit not -infinity (so logits that
+ *                                            cfgzip_apply_mask or cfgzip_mx4_logits masked need no mask here)
+ *     p[i][v] = exp(z[i][v]) / sum over admitted u of exp z[i][u]
+ * cfgzip_token_logprobs:
+ *     logprob[i][j] = log p[i][tokens[i][j]]; a token outside [0, V) is none: 0; one that the row does not admit: -inf
+ *     entropy[i]    = -sum over admitted v of p log p (0 if the row admits none)
+ *     stats[i]      = (the largest admitted logit, log sum over admitted v of exp(z[i][v] - that one's z)), (-inf, -inf) if there are none;
+ *                     stats[i][0] / temperature + stats[i][1] is the log-sum-exp
+ *     top_tokens[i], top_logprobs[i]: the `top` admitted tokens with the largest logits, the largest first, of equal ones the lowest; token -1
+ *                     with -inf where there are no more
+ *   logits   [N] rows of V elements, row_stride ELEMENTS apart (>= V), F32, BF16 or F16, any alignment to whole elements.  Admitted ones
+ *            have to be finite: a row with a NaN or +infinity among them has results that are NaN or infinite, and any tokens for its best.
+ *            Others may be anything.
+ *   tokens   int32 [N][n], n <= CFGZIP_MAX_TOKENS; NULL if n = 0.  A token may come more than once
+ *   temperature  2^-20 .. 2^20
+ *   masks    as for cfgzip_head_loss
+ *   logprob  out, float [N][n] (NULL if n = 0);  entropy  out, float [N];  stats  out, float [N][2]: each of these two may be NULL
+ *   top      0 .. CFGZIP_MAX_TOP;  top_tokens  out, int32 [N][top];  top_logprobs  out, float [N][top]
+ *   ws       cfgzip_token_logprobs_workspace_bytes(N, V, top) bytes, 256-byte aligned; NULL where that is 0
+ * cfgzip_token_logprobs_grad: with the logprob and stats (and entropy) of the call above, grad_logprob float [N][n] and grad_entropy float [N],
+ *     grad_logits[i][v] = (sum_j g[i][j] [v = tokens[i][j]] - p[i][v] (G + grad_entropy[i] (log p[i][v] + entropy[i]))) / temperature
+ * for admitted v, else 0; g = grad_logprob of tokens that are there and admitted (logprob not -inf), else 0; G their sum over j.  Rows that admit
+ * nothing, and rows whose g and grad_entropy are all 0, have zeros whatever their logits hold.
+ *   entropy, grad_entropy   both NULL: the entropy has no gradient
+ *   grad_logits   out, [N] rows of V elements of the logits' type, grad_stride ELEMENTS apart (>= V); may be `logits` itself with
+ *                 their stride, else it must not overlap them
+ * Sums are fp32, in an order that does not change from call to call; the gradient is rounded once.  N = 0 enqueues nothing.  At most 2^22 rows, and for
+ * the gradient fewer than 2^24 workgroups (rows times pieces of 16,384 tokens).
+ */
+#define CFGZIP_MAX_TOP 64
+#define CFGZIP_MAX_TOKENS 4096
+size_t cfgzip_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t top);
+int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t row_stride,
+                          const int32_t *tokens, int32_t n, double temperature,
+                          const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token, int32_t C,
+                          float *logprob, float *entropy, float *stats,
+                          int32_t top, int32_t *top_tokens, float *top_logprobs,
+                          void *ws, size_t ws_bytes, void *stream);
+int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t row_stride,
+                               const int32_t *tokens, int32_t n, double temperature,
+                               const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token, int32_t C,
+                               const float *logprob, const float *stats, const float *grad_logprob,
+                               const float *entropy, const float *grad_entropy,
+                               void *grad_logits, int64_t grad_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,8 @@ from .binding import (  # noqa: F401
     cfgzip_signatures_static,
     cfgzip_stack_adjacency,
     cfgzip_state_masks,
+    cfgzip_token_logprobs,
+    cfgzip_token_logprobs_grad,
     cfgzip_version,
     library_path,
     load_library,

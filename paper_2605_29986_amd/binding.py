@@ -177,6 +177,13 @@ def load_library() -> ctypes.CDLL:
     lib.cfgzip_mx4_logits_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
     lib.cfgzip_mx4_logits.restype = ctypes.c_int
     lib.cfgzip_mx4_logits.argtypes = [vp, i32, i64, vp, vp, vp, i32, i32, i32, vp, i32, vp, i32, vp, i32, i64, vp, sz, vp]
+    f64 = ctypes.c_double
+    lib.cfgzip_token_logprobs_workspace_bytes.restype = sz
+    lib.cfgzip_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.cfgzip_token_logprobs.restype = ctypes.c_int
+    lib.cfgzip_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, f64, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.cfgzip_token_logprobs_grad.restype = ctypes.c_int
+    lib.cfgzip_token_logprobs_grad.argtypes = [vp, i32, i32, i32, i64, vp, i32, f64, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp]
     _decode_step, _engine_step, _signatures, _build_classes, _displacements, _nfa_signatures = _load_stepcall(lib)
     _lib = lib
     return lib
@@ -930,3 +937,110 @@ def cfgzip_mx4_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.T
         workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("cfgzip_mx4_logits", rc)
     return logits
+
+
+# ---------------------------------------------------------------- log probabilities
+
+MAX_TOP = 64
+MAX_TOKENS = 4096
+
+
+def _tokens(logits, tokens, bits, class_of_token, C):
+    """The arguments that cfgzip_token_logprobs and cfgzip_token_logprobs_grad share, but for the temperature"""
+    p, stride = _rows(logits, "logits", tuple(_DTYPE))
+    N, V = logits.shape
+    _same_device(logits.device, tokens=tokens, bits=bits, class_of_token=class_of_token)
+    n = 0
+    if tokens is not None:
+        if tokens.dim() not in (1, 2) or tokens.shape[0] != N:
+            raise ValueError("tokens must be [rows] or [rows, n]")
+        n = 1 if tokens.dim() == 1 else tokens.shape[1]
+        _dev(tokens, torch.int32, "tokens")
+    masks = _masks(bits, class_of_token, C, N, V)
+    return (p, _DTYPE[logits.dtype], N, V, stride, tokens.data_ptr() if n else None, n), masks
+
+
+def _like_tokens(t, tokens, name: str):
+    if t.shape != tokens.shape:
+        raise ValueError(f"{name} must have the shape of tokens")
+    return _dev(t, torch.float32, name)
+
+
+def cfgzip_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, top: int = 0, temperature: float = 1.0,
+                          bits: Optional[torch.Tensor] = None, class_of_token: Optional[torch.Tensor] = None, C: int = 0,
+                          logprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                          stats: Optional[torch.Tensor] = None, top_tokens: Optional[torch.Tensor] = None,
+                          top_logprobs: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(logprob, entropy, stats, top_tokens, top_logprobs) of logits [N, V] (float32, bfloat16 or float16, rows any stride apart) over the tokens
+    that `bits` admits (as for cfgzip_head_loss) and whose logit is not -inf.
+
+    logprob float32, of the shape of tokens (int32 [N] or [N, n]; None without): 0 for a token outside [0, V), -inf for one that is not
+    admitted.  entropy float32 [N].  stats float32 [N, 2]: the largest admitted logit, and the log of the sum of exponentials against it,
+    for cfgzip_token_logprobs_grad; stats[:, 0] / temperature + stats[:, 1] is the log-sum-exp.  top_tokens int32 and top_logprobs float32
+    [N, top] (None for top = 0, at most MAX_TOP): the admitted tokens with the largest logits, of equal ones the lowest first, -1 and -inf
+    where there are no more.  Autograd knows nothing of it."""
+    lib = _lib or load_library()
+    args, masks = _tokens(logits, tokens, bits, class_of_token, C)
+    N, V, n = args[2], args[3], args[6]
+    dev = logits.device
+    top = int(top)
+    if tokens is None:
+        logprob = None
+    elif logprob is None:
+        logprob = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
+    if entropy is None:
+        entropy = torch.empty((N,), dtype=torch.float32, device=dev)
+    if stats is None:
+        stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
+    if top <= 0:
+        top_tokens = top_logprobs = None
+    else:
+        if top_tokens is None:
+            top_tokens = torch.empty((N, top), dtype=torch.int32, device=dev)
+        if top_logprobs is None:
+            top_logprobs = torch.empty((N, top), dtype=torch.float32, device=dev)
+    if workspace is None:
+        need = lib.cfgzip_token_logprobs_workspace_bytes(N, V, top)
+        workspace = _workspace(need, dev, stream) if need else None
+    _same_device(dev, logprob=logprob, entropy=entropy, stats=stats, top_tokens=top_tokens, top_logprobs=top_logprobs, workspace=workspace)
+    rc = lib.cfgzip_token_logprobs(
+        *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
+        _vector(entropy, torch.float32, N, "entropy"), _vector(stats, torch.float32, 2 * N, "stats"), top,
+        _vector(top_tokens, torch.int32, N * top, "top_tokens") if top > 0 else None,
+        _vector(top_logprobs, torch.float32, N * top, "top_logprobs") if top > 0 else None,
+        _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
+        workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("cfgzip_token_logprobs", rc)
+    return logprob, entropy, stats, top_tokens, top_logprobs
+
+
+def cfgzip_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], logprob: Optional[torch.Tensor], stats: torch.Tensor,
+                               grad_logprob: Optional[torch.Tensor], *, entropy: Optional[torch.Tensor] = None,
+                               grad_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                               bits: Optional[torch.Tensor] = None, class_of_token: Optional[torch.Tensor] = None, C: int = 0,
+                               grad_logits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """grad_logits [N, V] in the logits' type for grad_logprob (float32, of the shape of tokens) and grad_entropy float32 [N] (None: the entropy
+    has no gradient), with logprob, stats and entropy of cfgzip_token_logprobs on the same inputs.  grad_logits may be the logits
+    themselves.  Tokens that are none or not admitted, and all others of a row that admits nothing, have no gradient."""
+    lib = _lib or load_library()
+    args, masks = _tokens(logits, tokens, bits, class_of_token, C)
+    N, V, n = args[2], args[3], args[6]
+    dev = logits.device
+    if (entropy is None) != (grad_entropy is None) and grad_entropy is not None:
+        raise ValueError("grad_entropy goes with entropy")
+    if n and (logprob is None or grad_logprob is None):
+        raise ValueError("logprob and grad_logprob go with tokens")
+    if grad_logits is None:
+        grad_logits = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    p, stride = _rows(grad_logits, "grad_logits", (logits.dtype,), V)
+    if grad_logits.shape[0] != N:
+        raise ValueError(f"grad_logits must have {N} rows")
+    _same_device(dev, logprob=logprob, stats=stats, grad_logprob=grad_logprob, entropy=entropy, grad_entropy=grad_entropy,
+                 grad_logits=grad_logits)
+    rc = lib.cfgzip_token_logprobs_grad(
+        *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
+        _vector(stats, torch.float32, 2 * N, "stats"), _like_tokens(grad_logprob, tokens, "grad_logprob") if n else None,
+        _vector(entropy, torch.float32, N, "entropy") if grad_entropy is not None else None,
+        _vector(grad_entropy, torch.float32, N, "grad_entropy") if grad_entropy is not None else None, p, stride, _stream(stream))
+    _check("cfgzip_token_logprobs_grad", rc)
+    return grad_logits

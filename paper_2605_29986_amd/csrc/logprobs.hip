@@ -1,0 +1,685 @@
+// Log probabilities of given tokens over the tokens that a grammar's mask admits, with the row's entropy and best alternatives, and
+// the gradient of the logits.
+//
+//     z[v] = logits[v] / temperature for admitted v (its mask's bit set, its logit not -inf),   lse = log sum exp z[v]
+//     logprob[j] = z[t[j]] - lse,   p = exp(z - lse),   entropy = -sum p log p
+//     grad[v] = (sum_j g[j] [v = t[j]] - p[v] (G + e (log p[v] + entropy))) / temperature,   G = sum of g[j] of admitted t[j]
+//
+// Forward: one pass over the logits.  A thread keeps, of its units of eight logits, the largest, m, and with c = log2(e) / temperature the sum S of
+// 2^(c (x - m)) and the sum T of (x - m) 2^(c (x - m)); a larger m brings both to its own.  Then lse = m / temperature + log S and
+// entropy = log S - T / (S temperature), in which nothing large is taken from something as large.  What the gradient needs of a row are m
+// and log S, two numbers: lse in one rounds large logits' to few digits behind the point.
+//
+// Alternatives cost the pass nothing: the k-th largest of 64 threads' (or groups of threads') maxima is a bound that k logits at the least reach,
+// so only threads whose maximum reaches it can have had one of the k best.  Their few units are read again (from a cache), what reaches
+// the bound is put together and sorted.  A logit is compared by (value, lower token first) as one 64-bit number.
+#include <algorithm>
+
+#include "gemm16.hpp"
+
+namespace cfgzip {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
+constexpr float kInf = __builtin_inff();
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr double kLog2eD = 1.44269504088896340736;
+constexpr float kLog2e = (float)kLog2eD;
+constexpr float kNoMore = -200.0f;  // 2^y is 0 from here on
+constexpr int kMaxTop = CFGZIP_MAX_TOP;
+constexpr int kCandidates = 1024;
+constexpr int32_t kMaskWords = 8192;  // of a mask over classes in LDS; larger ones are read where they lie
+constexpr int32_t kMaxTokens = CFGZIP_MAX_TOKENS, kMaxRows = 1 << 22;  // (a launch has fewer than 2^32 threads)
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+
+// where a mask comes from
+enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3 };
+
+struct Logits {
+    const void *p;
+    int64_t ld;
+    int32_t N, V;
+    const int32_t *bits;
+    int64_t words;
+    const int32_t *class_of_token;
+};
+
+// eight logits next to each other as they lie, -inf behind the row's end
+template <int DTYPE>
+struct Unit {
+    u32x4 w[DTYPE == CFGZIP_DTYPE_F32 ? 2 : 1];
+
+    __device__ __forceinline__ void read(const Logits &l, int64_t row, int32_t unit) {
+        const int32_t left = l.V - unit * 8;
+        const int64_t at = row * l.ld + (int64_t)unit * 8;
+        if constexpr (DTYPE == CFGZIP_DTYPE_F32) {
+            const uint32_t *const p = static_cast<const uint32_t *>(l.p) + at;
+            if (left >= 8) {
+                w[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const i32x4_any *>(p));
+                w[1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const i32x4_any *>(p + 4));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j / 4][j % 4] = j < left ? p[j] : 0xFF800000u;
+            }
+        } else {
+            const uint16_t *const p = static_cast<const uint16_t *>(l.p) + at;
+            constexpr uint32_t none = DTYPE == CFGZIP_DTYPE_BF16 ? 0xFF80u : 0xFC00u;
+            if (left >= 8) {
+                w[0] = *reinterpret_cast<const u32x4_any *>(p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[0][j] = (2 * j < left ? p[2 * j] : none) | (2 * j + 1 < left ? p[2 * j + 1] : none) << 16;
+            }
+        }
+    }
+    template <int J>
+    __device__ __forceinline__ float value() const {
+        if constexpr (DTYPE == CFGZIP_DTYPE_F32) {
+            const uint32_t x = w[J / 4][J % 4];
+            return __builtin_bit_cast(float, x);
+        } else if constexpr (DTYPE == CFGZIP_DTYPE_BF16) {
+            return __builtin_bit_cast(float, J % 2 ? w[0][J / 2] & 0xFFFF0000u : w[0][J / 2] << 16);
+        } else {
+            return Fp16::value((uint16_t)(w[0][J / 2] >> (J % 2 * 16)));
+        }
+    }
+};
+
+// Which of a unit's tokens the row admits, a bit each: ids(unit) asks memory, bits() uses what came.
+template <int MASK>
+struct Admitted {
+    i32x4_any id[2];
+    uint32_t byte;
+    __device__ __forceinline__ void ask(const Logits &l, int64_t row, int32_t unit) {
+        if constexpr (MASK == TOKENS) {
+            byte = reinterpret_cast<const uint8_t *>(l.bits + row * l.words)[unit];
+        } else if constexpr (MASK >= CLASSES) {
+            const int32_t *const p = l.class_of_token + (int64_t)unit * 8;
+            const int32_t left = l.V - unit * 8;
+            if (left >= 8) {
+                id[0] = reinterpret_cast<const i32x4_any *>(p)[0];
+                id[1] = reinterpret_cast<const i32x4_any *>(p)[1];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) id[j / 4][j % 4] = j < left ? p[j] : 0;
+            }
+        }
+    }
+    __device__ __forceinline__ uint32_t bits(const Logits &l, int64_t row, const uint32_t *lds) const {
+        if constexpr (MASK == ALL) return 255;
+        if constexpr (MASK == TOKENS) return byte;
+        uint32_t ok = 0;
+        if constexpr (MASK >= CLASSES) {
+            const uint32_t *const words = MASK == CLASSES ? lds : reinterpret_cast<const uint32_t *>(l.bits + row * l.words);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t k = (uint32_t)id[j / 4][j % 4];
+                ok |= (words[k >> 5] >> (k & 31) & 1) << j;
+            }
+        }
+        return ok;
+    }
+};
+
+// the row's mask over classes to LDS
+template <int MASK>
+__device__ __forceinline__ void mask_to_lds(const Logits &l, int64_t row, uint32_t *lds) {
+    if constexpr (MASK == CLASSES) {
+        for (int32_t i = threadIdx.x; i < (int32_t)l.words; i += blockDim.x) lds[i] = (uint32_t)l.bits[row * l.words + i];
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ float logit_of(const Logits &l, int32_t dtype, int64_t row, int32_t v) {
+    const int64_t at = row * l.ld + v;
+    if (dtype == CFGZIP_DTYPE_F32) return static_cast<const float *>(l.p)[at];
+    const uint16_t x = static_cast<const uint16_t *>(l.p)[at];
+    return dtype == CFGZIP_DTYPE_BF16 ? Bf16::value(x) : Fp16::value(x);
+}
+
+// ---------------------------------------------------------------- the k best
+
+// larger for larger x (+0 and -0 alike), and of equal ones for the lower place; 0: none
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+    return __builtin_bit_cast(float, order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t place) { return (uint64_t)order_of(x) << 32 | (uint32_t)~place; }
+
+__device__ __forceinline__ uint64_t exchanged(uint64_t key, int distance, bool keep_larger) {
+    const uint64_t other = __shfl_xor((unsigned long long)key, distance);
+    return (key > other) == keep_larger ? key : other;
+}
+// a wave's 64 keys, the largest first
+__device__ __forceinline__ uint64_t sorted(uint64_t key, int lane) {
+#pragma unroll
+    for (int size = 2; size <= kWave; size *= 2)
+#pragma unroll
+        for (int d = size / 2; d > 0; d /= 2) key = exchanged(key, d, ((lane & d) == 0) == ((lane & size) == 0));
+    return key;
+}
+// the 64 largest of two sorted lists, sorted
+__device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, int lane) {
+    const uint64_t other = __shfl((unsigned long long)b, kWave - 1 - lane);
+    a = a > other ? a : other;
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2) a = exchanged(a, d, (lane & d) == 0);
+    return a;
+}
+
+// ---------------------------------------------------------------- forward
+
+// the largest x = m, the sums of 2^(c (x - m)) and of (x - m) 2^(c (x - m)); m is 0 where there is nothing yet
+struct Sums {
+    float m, s, t;
+    // brought to `to`, which is no less than m
+    __device__ __forceinline__ void raise(float to, float c) {
+        const float d = m - to, f = __builtin_amdgcn_exp2f(d * c);
+        t = s == 0.0f || f == 0.0f ? 0.0f : f * (t + s * d);
+        s = s == 0.0f ? 0.0f : s * f;
+        m = to;
+    }
+    __device__ __forceinline__ void add(const Sums &o) { s += o.s, t += o.t; }
+};
+
+struct ScoreArgs {
+    Logits l;
+    int32_t dtype;
+    float c, per_temperature;  // log2(e) / temperature
+    const int32_t *tokens;     // [N][n]
+    int32_t n, top;
+    int32_t splits, per;  // of a row's units, `per` to a workgroup
+    float *logprob, *entropy;
+    f32x2_any *stats;
+    int32_t *top_tokens;
+    float *top_logprobs;
+    f32x4 *parts;         // [N][splits]: m (-inf where nothing is admitted), S, T
+    uint64_t *part_keys;  // [N][splits][top]
+};
+
+// What belongs to a row, from its sums and its best keys (lane i of wave 0 has the i-th).  For all threads of a workgroup.
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const Sums &sums, uint64_t key) {
+    const float log_s = __builtin_amdgcn_logf(sums.s);  // log2; -inf where nothing is admitted
+    if (threadIdx.x == 0) {
+        if (a.stats) a.stats[row] = f32x2_any{sums.s == 0.0f ? -kInf : sums.m, kLn2 * log_s};
+        if (a.entropy) {
+            const float h = kLn2 * log_s - sums.t / sums.s * a.per_temperature;
+            a.entropy[row] = sums.s == 0.0f || h < 0.0f ? 0.0f : h;
+        }
+    }
+    for (int32_t j = threadIdx.x; j < a.n; j += blockDim.x) {
+        const int32_t t = a.tokens[row * a.n + j];
+        float out = 0.0f;
+        if (t >= 0 && t < a.l.V) {
+            bool ok = true;
+            if (a.l.bits) {
+                const int32_t k = a.l.class_of_token ? a.l.class_of_token[t] : t;
+                ok = a.l.bits[row * a.l.words + (k >> 5)] >> (k & 31) & 1;
+            }
+            const float x = ok ? logit_of(a.l, a.dtype, row, t) : -kInf;
+            out = x == -kInf ? -kInf : (x - sums.m) * a.per_temperature - kLn2 * log_s;
+        }
+        a.logprob[row * a.n + j] = out;
+    }
+    if (threadIdx.x < (uint32_t)a.top) {
+        const bool there = key != 0;
+        a.top_tokens[row * a.top + threadIdx.x] = there ? (int32_t)~(uint32_t)key : -1;
+        a.top_logprobs[row * a.top + threadIdx.x] =
+            there ? (value_of((uint32_t)(key >> 32)) - sums.m) * a.per_temperature - kLn2 * log_s : -kInf;
+    }
+}
+
+// Units of a thread on their way at a time: 64 bytes of logits.
+template <int DTYPE>
+constexpr int kAhead = DTYPE == CFGZIP_DTYPE_F32 ? 2 : 4;
+
+template <int DTYPE, int MASK, bool TOP>
+__global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
+    extern __shared__ uint32_t mask[];
+    __shared__ Sums shared_sums[kWaves];
+    __shared__ float shared_most[kWaves];
+    __shared__ uint64_t keys[TOP ? kThreads : 1], candidates[TOP ? kCandidates : 1];
+    __shared__ uint16_t again[TOP ? kThreads : 1];
+    __shared__ int32_t count[2];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t row = blockIdx.x / a.splits;
+    const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
+    const int32_t u0 = split * a.per, u1 = units - u0 < a.per ? units : u0 + a.per;
+    mask_to_lds<MASK>(a.l, row, mask);
+
+    const float no_more = kNoMore / a.c;
+    float most = -kInf;
+    int32_t at = 0;  // the first unit with it
+    Sums sums{0.0f, 0.0f, 0.0f};
+    constexpr int kUnits = kAhead<DTYPE>;
+    for (int32_t u = u0 + threadIdx.x; u < u1; u += kThreads * kUnits) {
+        Unit<DTYPE> x[kUnits];
+        Admitted<MASK> ok[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u + i * kThreads < u1) {
+                x[i].read(a.l, row, u + i * kThreads);
+                ok[i].ask(a.l, row, u + i * kThreads);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u + i * kThreads >= u1) break;
+            const uint32_t bits = ok[i].bits(a.l, row, mask);
+            float v[8];
+            float here = -kInf;
+            each<8>([&](auto j) CFGZIP_INLINE {
+                const float z = x[i].template value<j.value>();
+                v[j.value] = MASK == ALL || (bits >> j.value & 1) ? z : -kInf;
+                here = fmaxf(here, v[j.value]);
+            });
+            if (here > most) {
+                most = here;
+                at = u + i * kThreads;
+                sums.raise(here, a.c);
+            }
+            each<8>([&](auto j) CFGZIP_INLINE {
+                const float d = v[j.value] - sums.m, e = __builtin_amdgcn_exp2f(d * a.c);
+                sums.s += e;
+                sums.t = __builtin_fmaf(e, fmaxf(d, no_more), sums.t);
+            });
+        }
+    }
+
+    // the workgroup's sums
+    if (TOP) keys[threadIdx.x] = most > -kInf ? key_of(most, at) : 0;
+    float all = most;
+    for (int d = 1; d < kWave; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+    if (lane == 0) shared_most[wave] = all;
+    if (threadIdx.x < 2) count[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) all = fmaxf(all, shared_most[i]);
+    if (all > -kInf) sums.raise(all, a.c);
+    for (int d = 1; d < kWave; d *= 2) sums.s += __shfl_xor(sums.s, d), sums.t += __shfl_xor(sums.t, d);
+    if (lane == 0) shared_sums[wave] = sums;
+    __syncthreads();
+    sums = shared_sums[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) sums.add(shared_sums[i]);
+
+    uint64_t best = 0;
+    if constexpr (TOP) {
+        // every wave works out the bound, from the largest of the threads of each lane
+        uint64_t key = keys[lane];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) key = keys[lane + i * kWave] > key ? keys[lane + i * kWave] : key;
+        const uint64_t bound = __shfl((unsigned long long)sorted(key, lane), a.top - 1);
+        const uint64_t mine = keys[threadIdx.x];
+        if (mine != 0 && mine >= bound) again[atomicAdd(&count[0], 1)] = (uint16_t)threadIdx.x;
+        __syncthreads();
+        const uint32_t bound_value = (uint32_t)(bound >> 32), bound_unit = ~(uint32_t)bound;
+        const int32_t rounds = (u1 - u0 + kThreads - 1) / kThreads, items = count[0] * rounds;
+        // f(key) of the unit's logits that reach the bound
+        auto look_again = [&](int32_t item, auto &&f) CFGZIP_INLINE {
+            const int32_t u = item < items ? u0 + again[item / rounds] + item % rounds * kThreads : u1;
+            Unit<DTYPE> x;
+            Admitted<MASK> ok;
+            uint32_t bits = 0;
+            if (u < u1) {
+                x.read(a.l, row, u);
+                ok.ask(a.l, row, u);
+                bits = ok.bits(a.l, row, mask);
+            }
+            each<8>([&](auto j) CFGZIP_INLINE {
+                uint64_t k = 0;
+                if (bits >> j.value & 1) {
+                    const float z = x.template value<j.value>();
+                    const uint32_t order = order_of(z);
+                    if (z != -kInf && (order > bound_value || (order == bound_value && (uint32_t)u <= bound_unit)))
+                        k = key_of(z, (uint32_t)u * 8 + j.value);
+                }
+                f(k);
+            });
+        };
+        for (int32_t i = threadIdx.x; i < items; i += kThreads)
+            look_again(i, [&](uint64_t k) CFGZIP_INLINE {
+                if (k == 0) return;
+                const int32_t to = atomicAdd(&count[1], 1);
+                if (to < kCandidates) candidates[to] = k;
+            });
+        __syncthreads();
+        if (wave == 0) {
+            const int32_t found = count[1];
+            if (found <= kCandidates) {
+                for (int32_t i = 0; i < found; i += kWave) {
+                    const uint64_t k = sorted(i + lane < found ? candidates[i + lane] : 0, lane);
+                    best = i == 0 ? k : merged(best, k, lane);
+                }
+            } else {  // (rows whose large logits lie in a few threads' units)
+                for (int32_t i = 0; i < items; i += kWave)
+                    look_again(i + lane, [&](uint64_t k) CFGZIP_INLINE {
+                        const uint64_t least = __shfl((unsigned long long)best, a.top - 1);
+                        if (__builtin_amdgcn_ballot_w64(k > least) != 0) best = merged(best, sorted(k, lane), lane);
+                    });
+            }
+        }
+    }
+    if (a.splits == 1) {
+        write_row(a, row, sums, best);
+        return;
+    }
+    const int64_t part = row * a.splits + split;
+    if (threadIdx.x == 0) a.parts[part] = f32x4{all, sums.s, sums.t, 0.0f};
+    if (TOP && threadIdx.x < (uint32_t)a.top) a.part_keys[part * a.top + threadIdx.x] = best;
+}
+
+// Joins a row's parts.
+__global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a) {
+    __shared__ uint64_t lists[kWaves][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t row = blockIdx.x, first = row * a.splits;
+    const f32x4 part = lane < a.splits ? a.parts[first + lane] : f32x4{-kInf, 0.0f, 0.0f, 0.0f};
+    Sums sums{part[0] > -kInf ? part[0] : 0.0f, part[1], part[2]};
+    float all = part[0];
+    for (int d = 1; d < kWave; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+    if (all > -kInf) sums.raise(all, a.c);
+    for (int d = 1; d < kWave; d *= 2) sums.s += __shfl_xor(sums.s, d), sums.t += __shfl_xor(sums.t, d);
+    uint64_t best = 0;
+    if (a.top) {
+        for (int32_t p = wave; p < a.splits; p += kWaves) {
+            const uint64_t k = lane < a.top ? a.part_keys[(first + p) * a.top + lane] : 0;
+            best = p == wave ? k : merged(best, k, lane);
+        }
+        lists[wave][lane] = best;
+        for (int half = kWaves / 2; half > 0; half /= 2) {
+            __syncthreads();
+            if (wave < half) lists[wave][lane] = best = merged(best, lists[wave + half][lane], lane);
+        }
+    }
+    write_row(a, row, sums, best);
+}
+
+// ---------------------------------------------------------------- backward
+
+constexpr int kGradThreads = 256;
+constexpr int32_t kGradUnits = 2048;  // of a workgroup at the most
+
+struct GradArgs {
+    Logits l;
+    float c, per_temperature;
+    const int32_t *tokens;
+    int32_t n;
+    const float *logprob, *stats, *grad_logprob, *entropy, *grad_entropy;
+    void *out;
+    int64_t out_ld;
+    int32_t splits, per;
+};
+
+// eight results as they lie
+template <int DTYPE>
+__device__ __forceinline__ void write_unit(void *out, int64_t at, int32_t left, const float (&v)[8]) {
+    if constexpr (DTYPE == CFGZIP_DTYPE_F32) {
+        float *const p = static_cast<float *>(out) + at;
+        if (left >= 8) {
+            *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4_any *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) p[j] = v[j];
+        }
+    } else {
+        using T = std::conditional_t<DTYPE == CFGZIP_DTYPE_BF16, Bf16, Fp16>;
+        uint16_t *const p = static_cast<uint16_t *>(out) + at;
+        if (left >= 8) {
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = T::round2(v[2 * j], v[2 * j + 1]);
+            *reinterpret_cast<u32x4_any *>(p) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) p[j] = T::round(v[j]);
+        }
+    }
+}
+
+// A workgroup has a piece of a row.  With e = 2^y, y = c (x - m), and S of the row's statistics p is e / S, and a logit's gradient
+// e (A + B y) with constants of the row.  Tokens that are given are marked in LDS, a bit each; a thread that meets one adds up its gradients
+// in their order.  May write where it reads.
+template <int DTYPE, int MASK>
+__global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
+    extern __shared__ uint32_t mask[];
+    __shared__ uint32_t marks[kGradUnits / 4];
+    const int lane = threadIdx.x % kWave;
+    const int64_t row = blockIdx.x / a.splits;
+    const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
+    const int32_t u0 = split * a.per, u1 = units - u0 < a.per ? units : u0 + a.per;
+    const int32_t *const tokens = a.tokens + row * a.n;
+    const float *const logprob = a.logprob + row * a.n, *const grads = a.grad_logprob + row * a.n;
+    auto grad_of = [&](int32_t j) { return tokens[j] >= 0 && tokens[j] < a.l.V && logprob[j] != -kInf ? grads[j] : 0.0f; };
+
+    for (int32_t i = threadIdx.x; i < kGradUnits / 4; i += kGradThreads) marks[i] = 0;
+    __syncthreads();
+    float g = 0.0f;
+    bool any = false;
+    for (int32_t j = lane; j < a.n; j += kWave) {
+        const float x = grad_of(j);
+        g += x;
+        any |= x != 0.0f;
+        const int32_t v = tokens[j] - u0 * 8;
+        if (x != 0.0f && v >= 0 && v < (u1 - u0) * 8 && threadIdx.x < kWave) atomicOr(&marks[v >> 5], 1u << (v & 31));
+    }
+    for (int d = 1; d < kWave; d *= 2) g += __shfl_xor(g, d);
+    const float bonus = a.grad_entropy ? a.grad_entropy[row] : 0.0f, m = a.stats[2 * row], log_s = a.stats[2 * row + 1];
+    const bool live = m != -kInf && (__builtin_amdgcn_ballot_w64(any) != 0 || bonus != 0.0f);
+    __syncthreads();
+    if (!live) {
+        const float zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int32_t u = u0 + threadIdx.x; u < u1; u += kGradThreads)
+            write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)u * 8, a.l.V - u * 8, zeros);
+        return;
+    }
+    mask_to_lds<MASK>(a.l, row, mask);
+
+    const float scale = -a.per_temperature * __builtin_amdgcn_exp2f(-log_s * kLog2e);
+    const float B = bonus != 0.0f ? bonus * kLn2 * scale : 0.0f;
+    const float A = (bonus != 0.0f ? g + bonus * (a.entropy[row] - log_s) : g) * scale;
+    constexpr int kUnits = kAhead<DTYPE>;
+    for (int32_t u = u0 + threadIdx.x; u < u1; u += kGradThreads * kUnits) {
+        Unit<DTYPE> x[kUnits];
+        Admitted<MASK> ok[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u + i * kGradThreads < u1) {
+                x[i].read(a.l, row, u + i * kGradThreads);
+                ok[i].ask(a.l, row, u + i * kGradThreads);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int32_t unit = u + i * kGradThreads;
+            if (unit >= u1) break;
+            const uint32_t bits = ok[i].bits(a.l, row, mask);
+            float d[8];
+            each<8>([&](auto j) CFGZIP_INLINE {
+                const float z = x[i].template value<j.value>();
+                const float y = (z - m) * a.c;
+                const float f = __builtin_amdgcn_exp2f(y) * __builtin_fmaf(B, fmaxf(y, kNoMore), A);
+                d[j.value] = MASK == ALL || (bits >> j.value & 1) ? f : 0.0f;
+            });
+            const uint32_t marked = marks[(unit - u0) >> 2] >> ((unit - u0) & 3) * 8 & 255;
+            if (marked) {
+                each<8>([&](auto j) CFGZIP_INLINE {
+                    if (marked >> j.value & 1) {
+                        float sum = 0.0f;
+                        for (int32_t q = 0; q < a.n; ++q)
+                            if (tokens[q] == unit * 8 + j.value) sum += grad_of(q);
+                        d[j.value] += sum * a.per_temperature;
+                    }
+                });
+            }
+            write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)unit * 8, a.l.V - unit * 8, d);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+// Workgroups of a row: as many as fill the chip, of one round of units to a thread at the least.
+constexpr int32_t kWorkgroups = 512;
+int32_t splits_of(int32_t N, int32_t V) {
+    const int64_t most = std::min<int64_t>(ceil_div(V, kThreads * 8), kWave);
+    return (int32_t)std::max<int64_t>(std::min<int64_t>(kWorkgroups / std::max(N, 1), most), 1);
+}
+
+bool kind_ok(int32_t kind) { return kind == CFGZIP_BITS_TOKEN || kind == CFGZIP_BITS_CLASS || kind == CFGZIP_BITS_NONE; }
+
+struct Call {
+    const void *logits;
+    int32_t dtype, N, V;
+    int64_t row_stride;
+    const int32_t *tokens;
+    int32_t n;
+    double temperature;
+    const int32_t *bits;
+    int32_t bits_kind;
+    const int32_t *class_of_token;
+    int32_t C;
+};
+
+size_t size_of(int32_t dtype) { return dtype == CFGZIP_DTYPE_F32 ? 4 : 2; }
+
+int check_call(const Call &c) {
+    if (c.N < 0 || c.V <= 0 || c.n < 0 || c.row_stride < c.V || !kind_ok(c.bits_kind)) return CFGZIP_E_INVALID;
+    if (c.dtype != CFGZIP_DTYPE_F32 && c.dtype != CFGZIP_DTYPE_BF16 && c.dtype != CFGZIP_DTYPE_F16) return CFGZIP_E_INVALID;
+    if (!(c.temperature >= 0x1p-20 && c.temperature <= 0x1p20)) return CFGZIP_E_INVALID;
+    if (c.N > 0) {
+        if (!c.logits || !aligned_to(c.logits, size_of(c.dtype))) return CFGZIP_E_INVALID;
+        if (c.n > 0 && (!c.tokens || !aligned_to(c.tokens, 4))) return CFGZIP_E_INVALID;
+        if (c.bits_kind != CFGZIP_BITS_NONE && (!c.bits || !aligned_to(c.bits, 4))) return CFGZIP_E_INVALID;
+        if (c.bits_kind == CFGZIP_BITS_CLASS && (!c.class_of_token || c.C <= 0 || !aligned_to(c.class_of_token, 4)))
+            return CFGZIP_E_INVALID;
+    }
+    if (c.V > 0x7FFFFC00 || c.n > kMaxTokens || c.N > kMaxRows) return CFGZIP_E_TOO_LARGE;
+    return CFGZIP_OK;
+}
+
+Logits logits_of(const Call &c) {
+    const bool classes = c.bits_kind == CFGZIP_BITS_CLASS;
+    return Logits{c.logits, c.row_stride, c.N, c.V, c.bits_kind == CFGZIP_BITS_NONE ? nullptr : c.bits, words_for(classes ? c.C : c.V),
+                  classes ? c.class_of_token : nullptr};
+}
+
+int mask_of(const Call &c) {
+    if (c.bits_kind == CFGZIP_BITS_NONE) return ALL;
+    if (c.bits_kind == CFGZIP_BITS_TOKEN) return TOKENS;
+    return words_for(c.C) <= kMaskWords ? CLASSES : CLASSES_FAR;
+}
+
+// f(type, mask) with both as constants
+template <typename F>
+int with(int32_t dtype, int mask, F &&f) {
+    auto masked = [&](auto type) {
+        switch (mask) {
+            case ALL: return f(type, std::integral_constant<int, ALL>{});
+            case TOKENS: return f(type, std::integral_constant<int, TOKENS>{});
+            case CLASSES: return f(type, std::integral_constant<int, CLASSES>{});
+            default: return f(type, std::integral_constant<int, CLASSES_FAR>{});
+        }
+    };
+    if (dtype == CFGZIP_DTYPE_F32) return masked(std::integral_constant<int, CFGZIP_DTYPE_F32>{});
+    if (dtype == CFGZIP_DTYPE_BF16) return masked(std::integral_constant<int, CFGZIP_DTYPE_BF16>{});
+    return masked(std::integral_constant<int, CFGZIP_DTYPE_F16>{});
+}
+
+}  // namespace
+}  // namespace cfgzip
+
+using namespace cfgzip;
+
+extern "C" size_t cfgzip_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t top) {
+    if (N <= 0 || V <= 0 || top < 0 || top > kMaxTop || N > kMaxRows || V > 0x7FFFFC00) return 0;
+    const int64_t splits = splits_of(N, V);
+    if (splits == 1) return 0;
+    Carver ws(nullptr);
+    ws.take<f32x4>((size_t)N * splits);
+    ws.take<uint64_t>((size_t)N * splits * top);
+    return ws.used;
+}
+
+extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t row_stride, const int32_t *tokens,
+                                     int32_t n, double temperature, const int32_t *bits, int32_t bits_kind, const int32_t *class_of_token,
+                                     int32_t C, float *logprob, float *entropy, float *stats, int32_t top, int32_t *top_tokens,
+                                     float *top_logprobs, void *ws, size_t ws_bytes, void *stream) {
+    const Call c{logits, dtype, N, V, row_stride, tokens, n, temperature, bits, bits_kind, class_of_token, C};
+    CFGZIP_TRY(check_call(c));
+    if (top < 0 || !aligned_to(entropy, 4) || !aligned_to(stats, 4)) return CFGZIP_E_INVALID;
+    if (top > kMaxTop) return CFGZIP_E_TOO_LARGE;
+    if (N == 0) return CFGZIP_OK;
+    if (n > 0 && (!logprob || !aligned_to(logprob, 4))) return CFGZIP_E_INVALID;
+    if (top > 0 && (!top_tokens || !top_logprobs || !aligned_to(top_tokens, 4) || !aligned_to(top_logprobs, 4))) return CFGZIP_E_INVALID;
+    const size_t need = cfgzip_token_logprobs_workspace_bytes(N, V, top);
+    if (need && (!ws || !aligned_to(ws, 256) || ws_bytes < need)) return CFGZIP_E_WORKSPACE;
+    ScoreArgs a{};
+    a.l = logits_of(c);
+    a.dtype = dtype;
+    a.c = (float)(kLog2eD / temperature), a.per_temperature = (float)(1.0 / temperature);
+    a.tokens = tokens, a.n = n, a.top = top;
+    a.splits = splits_of(N, V);
+    a.per = (int32_t)ceil_div(ceil_div(V, 8), a.splits);
+    a.splits = (int32_t)ceil_div(ceil_div(V, 8), a.per);
+    a.logprob = logprob, a.entropy = entropy, a.stats = reinterpret_cast<f32x2_any *>(stats), a.top_tokens = top_tokens, a.top_logprobs = top_logprobs;
+    Carver carve(ws);
+    if (a.splits > 1) {
+        a.parts = carve.take<f32x4>((size_t)N * a.splits);
+        a.part_keys = carve.take<uint64_t>((size_t)N * a.splits * top);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int mask = mask_of(c);
+    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : 0;
+    CFGZIP_TRY(with(dtype, mask, [&](auto type, auto kind) {
+        const dim3 grid((uint32_t)N * a.splits);
+        if (top) hipLaunchKernelGGL((score_kernel<type.value, kind.value, true>), grid, dim3(kThreads), lds, s, a);
+        else hipLaunchKernelGGL((score_kernel<type.value, kind.value, false>), grid, dim3(kThreads), lds, s, a);
+        return check_launch();
+    }));
+    if (a.splits == 1) return CFGZIP_OK;
+    hipLaunchKernelGGL(score_join_kernel, dim3(N), dim3(kThreads), 0, s, a);
+    return check_launch();
+}
+
+extern "C" int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t row_stride, const int32_t *tokens,
+                                          int32_t n, double temperature, const int32_t *bits, int32_t bits_kind,
+                                          const int32_t *class_of_token, int32_t C, const float *logprob, const float *stats,
+                                          const float *grad_logprob, const float *entropy, const float *grad_entropy, void *grad_logits,
+                                          int64_t grad_stride, void *stream) {
+    const Call c{logits, dtype, N, V, row_stride, tokens, n, temperature, bits, bits_kind, class_of_token, C};
+    CFGZIP_TRY(check_call(c));
+    if (grad_stride < V) return CFGZIP_E_INVALID;
+    if (N == 0) return CFGZIP_OK;
+    if (!stats || !aligned_to(stats, 4) || !grad_logits || !aligned_to(grad_logits, size_of(dtype))) return CFGZIP_E_INVALID;
+    if (n > 0 && (!logprob || !grad_logprob || !aligned_to(logprob, 4) || !aligned_to(grad_logprob, 4))) return CFGZIP_E_INVALID;
+    if (grad_entropy && (!entropy || !aligned_to(entropy, 4) || !aligned_to(grad_entropy, 4))) return CFGZIP_E_INVALID;
+    if (grad_logits == logits && grad_stride != row_stride) return CFGZIP_E_INVALID;
+    GradArgs a{};
+    a.l = logits_of(c);
+    a.c = (float)(kLog2eD / temperature);
+    a.per_temperature = (float)(1.0 / temperature);
+    a.tokens = tokens, a.n = n;
+    a.logprob = logprob, a.stats = stats, a.grad_logprob = grad_logprob, a.entropy = entropy, a.grad_entropy = grad_entropy;
+    a.out = grad_logits, a.out_ld = grad_stride;
+    a.per = kGradUnits;
+    a.splits = (int32_t)ceil_div(ceil_div(V, 8), a.per);
+    if ((int64_t)N * a.splits > 0xFFFFFFFF / kGradThreads) return CFGZIP_E_TOO_LARGE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int mask = mask_of(c);
+    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : 0;
+    return with(dtype, mask, [&](auto type, auto kind) {
+        hipLaunchKernelGGL((grad_kernel<type.value, kind.value>), dim3((uint32_t)N * a.splits), dim3(kGradThreads), lds, s, a);
+        return check_launch();
+    });
+}
