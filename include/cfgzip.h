@@ -566,6 +566,51 @@ int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int32_t N, int
                                const float *entropy, const float *grad_entropy,
                                void *grad_logits, int64_t grad_stride, void *stream);
 
+/*
+ * The layer in front of the vocabulary projection (a head's transform, a drafting head's residual block), or the projection itself with its
+ * weights in 16 bits: a matrix product with bias, activation and residual in its epilogue.
+ *     z[i][m] = sum_d hidden[i][d] * weight[m][d] + bias[m],     out[i][m] = act(z[i][m]) + residual[i][m]
+ * with act one of
+ *     CFGZIP_ACT_NONE z,  CFGZIP_ACT_RELU max(z, 0),  CFGZIP_ACT_GELU z (1 + erf(z / sqrt 2)) / 2,
+ *     CFGZIP_ACT_GELU_TANH z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2,  CFGZIP_ACT_SILU z / (1 + exp(-z))
+ *   hidden, weight   [N] and [M] rows of D elements, BF16 or F16 alike, strides in ELEMENTS (>= D); any alignment to whole elements, fastest
+ *                    at multiples of 16 bytes and D, strides multiples of 8; finite
+ *   bias       [M] of the inputs' type, or NULL
+ *   residual   [N] rows of M elements of the inputs' type, residual_stride apart, or NULL; may be `out` itself with its stride and type
+ *   out        [N] rows of M elements, out_stride apart, of the inputs' type or F32; must not overlap the other inputs
+ *   slope      out, int16 [N] rows of M elements, slope_stride apart, or NULL: act'(z), all that the gradient needs of z, as q = sign *
+ *              round(2^14 sqrt |act'|), which stands for q |q| / 2^28 (off by 2^-14 sqrt |act'| at the most; 0 and 1 are exact)
+ *   ws         cfgzip_head_layer_workspace_bytes(N, M, D) bytes, 256-byte aligned; NULL where that is 0
+ * cfgzip_head_layer_grad: with dz[i][m] = grad_out[i][m] * slope[i][m],
+ *     grad_hidden[i] = sum_m dz[i][m] * weight[m],   grad_weight[m] = sum_i dz[i][m] * hidden[i],   grad_bias[m] = sum_i dz[i][m]
+ * (the residual's gradient is grad_out).
+ *   grad_out   [N] rows of M elements of the inputs' type or F32, finite;  slope  of the call above, or NULL where act is CFGZIP_ACT_NONE
+ *   grad_hidden, grad_weight, grad_bias   out, [N] and [M] rows of D elements and [M], of the inputs' type; any of them may be NULL
+ *   ws         cfgzip_head_layer_grad_workspace_bytes(N, M, D) bytes, 256-byte aligned
+ * dz is rounded to the inputs' type (not for grad_bias, and not where slope is NULL and grad_out of that type); in F16 it is brought into range by a
+ * power of two first, so grad_out may be of any size: what is less than 2^-38 of its largest counts as multiples of that.
+ * All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight and grad_bias
+ * are set to 0).
+ */
+#define CFGZIP_ACT_NONE 0
+#define CFGZIP_ACT_RELU 1
+#define CFGZIP_ACT_GELU 2
+#define CFGZIP_ACT_GELU_TANH 3
+#define CFGZIP_ACT_SILU 4
+size_t cfgzip_head_layer_workspace_bytes(int32_t N, int32_t M, int32_t D);
+int cfgzip_head_layer(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                      int32_t dtype, int32_t N, int32_t M, int32_t D, const void *bias, int32_t activation,
+                      const void *residual, int64_t residual_stride,
+                      void *out, int32_t out_dtype, int64_t out_stride, void *slope, int64_t slope_stride,
+                      void *ws, size_t ws_bytes, void *stream);
+size_t cfgzip_head_layer_grad_workspace_bytes(int32_t N, int32_t M, int32_t D);
+int cfgzip_head_layer_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                           int32_t dtype, int32_t N, int32_t M, int32_t D,
+                           const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride,
+                           const void *slope, int64_t slope_stride,
+                           void *grad_hidden, int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride,
+                           void *grad_bias, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

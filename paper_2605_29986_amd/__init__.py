@@ -23,6 +23,8 @@ from .binding import (  # noqa: F401
     cfgzip_displacements,
     cfgzip_engine_step,
     cfgzip_expand_mask,
+    cfgzip_head_layer,
+    cfgzip_head_layer_grad,
     cfgzip_head_loss,
     cfgzip_head_loss_grad,
     cfgzip_map_to_rep,

@@ -184,6 +184,14 @@ def load_library() -> ctypes.CDLL:
     lib.cfgzip_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, f64, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.cfgzip_token_logprobs_grad.restype = ctypes.c_int
     lib.cfgzip_token_logprobs_grad.argtypes = [vp, i32, i32, i32, i64, vp, i32, f64, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.cfgzip_head_layer_workspace_bytes.restype = sz
+    lib.cfgzip_head_layer_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.cfgzip_head_layer.restype = ctypes.c_int
+    lib.cfgzip_head_layer.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, vp, i64, vp, i32, i64, vp, i64, vp, sz, vp]
+    lib.cfgzip_head_layer_grad_workspace_bytes.restype = sz
+    lib.cfgzip_head_layer_grad_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.cfgzip_head_layer_grad.restype = ctypes.c_int
+    lib.cfgzip_head_layer_grad.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, i64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
     _decode_step, _engine_step, _signatures, _build_classes, _displacements, _nfa_signatures = _load_stepcall(lib)
     _lib = lib
     return lib
@@ -1044,3 +1052,92 @@ def cfgzip_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tens
         _vector(grad_entropy, torch.float32, N, "grad_entropy") if grad_entropy is not None else None, p, stride, _stream(stream))
     _check("cfgzip_token_logprobs_grad", rc)
     return grad_logits
+
+
+# ---------------------------------------------------------------- the layer in front of the projection
+
+_ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _matrix(t, name: str, dtypes, rows: int, columns: int) -> Tuple[int, int]:
+    p, stride = _rows(t, name, dtypes, columns)
+    if t.shape[0] != rows:
+        raise ValueError(f"{name} must have {rows} rows")
+    return p, stride
+
+
+def _layer(hidden, weight):
+    """The arguments that cfgzip_head_layer and cfgzip_head_layer_grad share"""
+    w, w_stride = _rows(weight, "weight", (torch.bfloat16, torch.float16))
+    M, D = weight.shape
+    h, h_stride = _rows(hidden, "hidden", (weight.dtype,), D)
+    return (h, h_stride, w, w_stride, _DTYPE[weight.dtype], hidden.shape[0], M, D)
+
+
+def cfgzip_head_layer(hidden: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *, activation: Optional[str] = None,
+                      residual: Optional[torch.Tensor] = None, dtype=None, want_slope: bool = False, out: Optional[torch.Tensor] = None,
+                      slope: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                      ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(out, slope): out [N, M] = act(hidden weight^T + bias) + residual of hidden [N, D] and weight [M, D] (bfloat16 or float16, rows any
+    stride apart), bias [M] and residual [N, M] of their type, in that type or in float32 (`dtype`, or that of `out`).  activation: None, "relu",
+    "gelu", "gelu_tanh" or "silu".  slope int16 [N, M] (if it is wanted or given, else None): act' for cfgzip_head_layer_grad,
+    which q of it stands for as q |q| / 2^28.  `out` may be `residual`.  Autograd knows nothing of it."""
+    lib = _lib or load_library()
+    args = _layer(hidden, weight)
+    N, M, D = args[5:]
+    dev = weight.device
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(str(a) for a in _ACTIVATIONS)}")
+    b = _vector(bias, weight.dtype, M, "bias") if bias is not None else None
+    r = _matrix(residual, "residual", (weight.dtype,), N, M) if residual is not None else (None, 0)
+    if out is None:
+        out = torch.empty((N, M), dtype=weight.dtype if dtype is None else dtype, device=dev)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out must have dtype {dtype}, got {out.dtype}")
+    o, o_stride = _matrix(out, "out", (weight.dtype, torch.float32), N, M)
+    if slope is None and want_slope:
+        slope = torch.empty((N, M), dtype=torch.int16, device=dev)
+    s = _matrix(slope, "slope", (torch.int16,), N, M) if slope is not None else (None, 0)
+    if workspace is None:
+        need = lib.cfgzip_head_layer_workspace_bytes(N, M, D)
+        workspace = _workspace(need, dev, stream) if need else None
+    _same_device(dev, hidden=hidden, bias=bias, residual=residual, out=out, slope=slope, workspace=workspace)
+    rc = lib.cfgzip_head_layer(*args, b, _ACTIVATIONS[activation], *r, o, _DTYPE[out.dtype], o_stride, *s,
+                               _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
+                               workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("cfgzip_head_layer", rc)
+    return out, slope
+
+
+def cfgzip_head_layer_grad(hidden: torch.Tensor, weight: torch.Tensor, grad_out: torch.Tensor, *, slope: Optional[torch.Tensor] = None,
+                           want_hidden: bool = True, want_weight: bool = True, want_bias: bool = False,
+                           grad_hidden: Optional[torch.Tensor] = None, grad_weight: Optional[torch.Tensor] = None,
+                           grad_bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                           ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(grad_hidden [N, D], grad_weight [M, D], grad_bias [M]) in the inputs' type, each None if it is not wanted, for grad_out [N, M] (that type or
+    float32), with the slope of cfgzip_head_layer on the same inputs (None where there is no activation).  The residual's gradient is grad_out."""
+    lib = _lib or load_library()
+    args = _layer(hidden, weight)
+    N, M, D = args[5:]
+    dev = weight.device
+    g, g_stride = _matrix(grad_out, "grad_out", (weight.dtype, torch.float32), N, M)
+    s = _matrix(slope, "slope", (torch.int16,), N, M) if slope is not None else (None, 0)
+    if not (want_hidden or want_weight or want_bias):
+        raise ValueError("one of the gradients must be wanted")
+    if want_hidden and grad_hidden is None:
+        grad_hidden = torch.empty((N, D), dtype=weight.dtype, device=dev)
+    if want_weight and grad_weight is None:
+        grad_weight = torch.empty((M, D), dtype=weight.dtype, device=dev)
+    if want_bias and grad_bias is None:
+        grad_bias = torch.empty((M,), dtype=weight.dtype, device=dev)
+    gh = _matrix(grad_hidden, "grad_hidden", (weight.dtype,), N, D) if want_hidden else (None, 0)
+    gw = _matrix(grad_weight, "grad_weight", (weight.dtype,), M, D) if want_weight else (None, 0)
+    gb = _vector(grad_bias, weight.dtype, M, "grad_bias") if want_bias else None
+    if workspace is None:
+        workspace = _workspace(lib.cfgzip_head_layer_grad_workspace_bytes(N, M, D), dev, stream)
+    _same_device(dev, hidden=hidden, grad_out=grad_out, slope=slope, grad_hidden=grad_hidden, grad_weight=grad_weight, grad_bias=grad_bias,
+                 workspace=workspace)
+    rc = lib.cfgzip_head_layer_grad(*args, g, _DTYPE[grad_out.dtype], g_stride, *s, *gh, *gw, gb, _dev(workspace, torch.uint8, "workspace"),
+                                    workspace.numel(), _stream(stream))
+    _check("cfgzip_head_layer_grad", rc)
+    return grad_hidden if want_hidden else None, grad_weight if want_weight else None, grad_bias if want_bias else None

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libcfgzip.so")
 SOURCES = ["mask.hip", "walk.hip", "classes.hip", "engine.hip", "displacement.hip", "nfa.hip", "head.hip", "mx4.hip",
-           "logprobs.hip"]
+           "logprobs.hip", "layer.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

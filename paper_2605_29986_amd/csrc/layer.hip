@@ -1,0 +1,700 @@
+// The layer in front of the vocabulary projection, or the projection itself in 16 bits: a matrix product with bias, activation and residual in
+// its epilogue, and its gradients.
+//
+//     z[i][m] = sum_d hidden[i][d] weight[m][d] + bias[m],   out = act(z) + residual,   slope = act'(z)
+//     dz = grad_out slope,   grad_hidden = dz weight,   grad_weight = dz^T hidden,   grad_bias[m] = sum_i dz[i][m]
+//
+// All three products are made in tiles on the matrix cores (gemm16.hpp); the tile's sums become results in the accumulators.  Where
+// the tiles are too few to fill the chip their sum over k is split, the shares are added up by a kernel that ends with the same epilogue.
+// Up to 16 rows it is reading the weights that counts: a workgroup's 16 waves split the k of 16 rows of weights, each with loads of its own
+// straight to registers, and join through LDS.
+#include <algorithm>
+
+#include "gemm16.hpp"
+
+namespace cfgzip {
+namespace {
+
+using Shape64 = Shape<128, 64, 4, 1, 3>;
+using Shape128 = Shape<256, 128, 4, 2, 3>;
+using Shape256 = Shape<256, 256, 2, 2, 2>;
+
+constexpr int32_t kFewRows = 16;
+constexpr int32_t kMaxRows = 1 << 22;
+constexpr float kLog2e = 1.44269504088896340736f;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// ---------------------------------------------------------------- epilogues
+
+// A slope in 16 bits: the root of its size in steps of 2^-14, with its sign.  It is off by 2^-14 of that root at the most, 2^-15 rms near 1, an eighth
+// of what fp16 is off there (whose error was as large as dz's own rounding: gradients of 777 fp16 rows 1.8 times as far from 64 bits as their
+// own rounding makes them), and 0 and 1 are exact.
+__device__ __forceinline__ uint32_t slope_code(float s) {
+    const float root = __builtin_amdgcn_sqrtf(fabsf(s)) * 0x1p14f;
+    return (uint32_t)(int32_t)__builtin_rintf(__builtin_copysignf(root, s)) & 0xFFFFu;
+}
+__device__ __forceinline__ float slope_value(uint32_t code) {
+    const float root = (float)(int16_t)code * 0x1p-14f;
+    return root * fabsf(root);
+}
+
+// act(z) = z q(z): q = 1 / (1 + exp(-z (a + b z^2))) is silu's for a = 1, b = 0, and gelu_tanh's, whose (1 + tanh u) / 2 is the logistic
+// function of 2 u, for a = 2 sqrt(2 / pi), b = 0.044715 a.
+struct Activation {
+    int32_t kind;
+    float a, b;
+
+    __device__ __forceinline__ float of(float z, float &slope) const {
+        if (kind == CFGZIP_ACT_NONE) {
+            slope = 1.0f;
+            return z;
+        }
+        if (kind == CFGZIP_ACT_RELU) {
+            slope = z > 0.0f ? 1.0f : 0.0f;
+            return z < 0.0f ? 0.0f : z;
+        }
+        if (kind == CFGZIP_ACT_GELU) {
+            const float q = 0.5f * erfcf(z * -0.70710678118654752440f);
+            slope = __builtin_fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e)), q);
+            return z * q;
+        }
+        const float zz = z * z, u = z * __builtin_fmaf(b, zz, a);
+        const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -kLog2e));
+        slope = __builtin_fmaf(z * q * (1.0f - q), __builtin_fmaf(3.0f * b, zz, a), q);
+        return z * q;
+    }
+};
+
+struct Forward {
+    const uint16_t *bias;      // or null
+    const uint16_t *residual;  // or null
+    int64_t residual_ld;
+    Activation act;
+    void *out;
+    int64_t out_ld;
+    int32_t f32;
+    uint16_t *slope;  // or null
+    int64_t slope_ld;
+    int32_t M;
+
+    // results m .. m + 3 (as many as there are) of row n
+    template <typename T>
+    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z) const {
+        const int32_t left = M - m;
+        u32x2 b = {0, 0}, r = {0, 0};
+        auto read4 = [&](const uint16_t *p) CFGZIP_INLINE {
+            if (left >= 4) return u32x2(*reinterpret_cast<const u32x2_any *>(p));
+            u32x2 v = {0, 0};
+            for (int i = 0; i < left; ++i) v[i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
+            return v;
+        };
+        if (bias) b = read4(bias + m);
+        if (residual) r = read4(residual + n * residual_ld + m);
+        f32x4 y, s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float slope_i;
+            const float zi = z[i] + T::value((uint16_t)(b[i / 2] >> (i % 2 * 16)));
+            y[i] = act.of(zi, slope_i) + T::value((uint16_t)(r[i / 2] >> (i % 2 * 16)));
+            s[i] = slope_i;
+        }
+        auto write4 = [&](uint16_t *p, u32x2 v) CFGZIP_INLINE {
+            if (left >= 4) {
+                *reinterpret_cast<u32x2_any *>(p) = v;
+            } else {
+                for (int i = 0; i < left; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+            }
+        };
+        if (slope)
+            write4(slope + n * slope_ld + m, u32x2{slope_code(s[0]) | slope_code(s[1]) << 16, slope_code(s[2]) | slope_code(s[3]) << 16});
+        if (f32) {
+            float *const p = static_cast<float *>(out) + n * out_ld + m;
+            if (left >= 4) {
+                *reinterpret_cast<f32x4_any *>(p) = y;
+            } else {
+                for (int i = 0; i < left; ++i) p[i] = y[i];
+            }
+        } else {
+            write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y));
+        }
+    }
+};
+
+struct Gradient {
+    const float *unscale;  // what dz was multiplied with is taken back; or null
+    uint16_t *out;
+    int64_t out_ld;
+    int32_t M;  // columns
+
+    template <typename T>
+    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z) const {
+        if (unscale) z *= *unscale;
+        uint16_t *const p = out + n * out_ld + m;
+        const u32x2 v = round4<T>(z);
+        if (m + 4 <= M) {
+            *reinterpret_cast<u32x2_any *>(p) = v;
+        } else {
+            for (int i = 0; m + i < M; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+        }
+    }
+};
+
+// ---------------------------------------------------------------- products
+
+struct ProductArgs {
+    Operand A, B;
+    int32_t m, n, k;  // extents; the result is [n][m]
+    int32_t k_split, splits;
+    int32_t tiles_m, tiles_n;
+    float *sums;  // [splits][n][sums_ld]; null: results are written at once
+    int32_t sums_ld;
+};
+
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool DIRECT, typename E>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E end) {
+    // (B goes on with zeros to the end of a step, so what A has there only has to be finite; hidden states by columns go on with zeros too: with
+    // ANY the largest tile's addresses are out of the registers, 122 of them)
+    using TileA = Tile<S::BM, S::kThreads, A_COLUMNS, DIRECT, A_COLUMNS && B_COLUMNS ? PADDED : ANY>;
+    using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true, PADDED>;
+    CFGZIP_STAGES(S, lds);
+    auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
+        const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = blockIdx.x + i * gridDim.x;
+        if (t >= total) return false;
+        tile_of(t, total, a.tiles_m, a.tiles_n * a.splits, tm, tn);
+        split = tn / a.tiles_n;
+        tn -= split * a.tiles_n;
+        return true;
+    };
+    auto work = [&](int32_t i, Work &w) CFGZIP_INLINE {
+        int32_t tm, tn, split;
+        if (!place(i, tm, tn, split)) return false;
+        const int32_t k0 = split * a.k_split;
+        w = Work{tm * S::BM, tn * S::BN, k0 / kStepK, a.k - k0 < a.k_split ? a.k - k0 : a.k_split};
+        return true;
+    };
+    auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
+        int32_t tm = 0, tn = 0, split = 0;
+        place(i, tm, tn, split);
+        each<S::FN>([&](auto j) CFGZIP_INLINE {
+            const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
+            if (n >= a.n) return;
+            each<S::FM>([&](auto i) CFGZIP_INLINE {
+                const int32_t m = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
+                if (m >= a.m) return;
+                if (a.sums) *reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + m) = acc[i.value][j.value];
+                else end.template store<T>(n, m, acc[i.value][j.value]);
+            });
+        });
+    };
+    multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
+}
+
+// Adds up the shares of a sum that was split.
+template <typename T, typename E>
+__global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_t splits, int32_t n, int32_t sums_ld, E end) {
+    const int32_t units = sums_ld / 4;
+    const int64_t at = (int64_t)blockIdx.x * kWave + threadIdx.x;
+    if (at >= (int64_t)n * units) return;
+    const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 4;
+    const float *const p = sums + (int64_t)row * sums_ld + c;
+    const int64_t step = (int64_t)n * sums_ld;
+    f32x4 x = {0, 0, 0, 0};
+    for (int32_t s = 0; s < splits; s += 8) {
+        f32x4 y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = s + i < splits ? *reinterpret_cast<const f32x4 *>(p + (s + i) * step) : f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += y[i];
+    }
+    end.template store<T>(row, c, x);
+}
+
+// ---------------------------------------------------------------- few rows
+
+struct FewArgs {
+    const uint16_t *x, *w;
+    int64_t x_ld, w_ld;
+    int32_t N, M, D;
+};
+constexpr int kFewWaves = 16, kFewThreads = kFewWaves * kWave;
+constexpr int kFewAhead = 4;  // steps of 64 on their way at a time
+
+// eight elements of a row of which `left` are there, at any alignment
+__device__ __forceinline__ u32x4 eight(const uint16_t *p, int32_t left) {
+    if (left >= 8) return *reinterpret_cast<const u32x4_any *>(p);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < left) v[j / 2] |= (uint32_t)p[j] << (j % 2 * 16);
+    return v;
+}
+
+// Lane l has row l & 15 of both sides and of every 64 elements those of 16 (l >> 4) on, which two products take as if they were apart: a sum has
+// no order of its own, and a row's 128 bytes come in one line.
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a, Forward end) {
+    __shared__ f32x4 shared[kFewWaves][kWave];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int r = lane & 15, g = lane >> 4;
+    const int32_t m0 = blockIdx.x * 16, steps = (a.D + 63) / 64;
+    const int32_t s0 = (int32_t)((int64_t)steps * wave / kFewWaves), s1 = (int32_t)((int64_t)steps * (wave + 1) / kFewWaves);
+    const uint16_t *const w = a.w + (m0 + r < a.M ? m0 + r : a.M - 1) * a.w_ld;
+    const uint16_t *const x = a.x + (r < a.N ? r : a.N - 1) * a.x_ld;
+    f32x4 acc = {0, 0, 0, 0};
+    for (int32_t s = s0; s < s1; s += kFewAhead) {
+        u32x4 p[kFewAhead][2], q[kFewAhead][2];
+        if (s + kFewAhead <= s1 && (s + kFewAhead) * 64 <= a.D) {
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) p[i][h] = *reinterpret_cast<const u32x4_any *>(w + (s + i) * 64 + g * 16 + h * 8);
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) q[i][h] = *reinterpret_cast<const u32x4_any *>(x + (s + i) * 64 + g * 16 + h * 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int32_t c = (s + i) * 64 + g * 16 + h * 8, left = s + i < s1 ? a.D - c : 0;
+                    p[i][h] = eight(w + c, left);
+                    q[i][h] = eight(x + c, left);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc = T::mma(p[i][h], q[i][h], acc);
+    }
+    shared[wave][lane] = acc;
+    __syncthreads();
+    if (threadIdx.x >= kWave) return;
+#pragma unroll
+    for (int i = 1; i < kFewWaves; ++i) acc += shared[i][lane];
+    const int32_t m = m0 + 4 * g;
+    if (r < a.N && m < a.M) end.template store<T>(r, m, acc);
+}
+
+// ---------------------------------------------------------------- dz and the gradient of the bias
+
+// `all` rows of y_ld elements, zeros behind D and N
+__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, uint16_t *y, int32_t y_ld,
+                                                        int32_t all) {
+    const int32_t units = y_ld / 8;
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (k >= (int64_t)all * units) return;
+    const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
+    *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = eight(x + row * x_ld + c, row < N ? D - c : 0);
+}
+
+struct DzArgs {
+    const void *grad_out;
+    int64_t grad_ld;
+    const uint16_t *slope;  // or null: 1
+    int64_t slope_ld;
+    int32_t N, M;
+    int32_t rows;           // of a workgroup
+    uint16_t *dz;           // [N in whole steps][dz_ld], zeros where there is nothing; or null
+    int32_t dz_ld;
+    const float *largest;   // of |grad_out|, [kLargestBlocks]; or null: dz is not scaled
+    float *unscale;
+    float *sums;            // [row blocks][dz_ld]: of the columns; or null
+};
+constexpr int kLargestBlocks = 256;
+
+// eight of grad_out's values from column c on
+template <typename T, bool F32>
+__device__ __forceinline__ void read8(const void *row, int32_t c, int32_t left, float (&v)[8]) {
+    if constexpr (F32) {
+        const float *const p = static_cast<const float *>(row) + c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (left >= 8) {
+            const f32x4 lo = *reinterpret_cast<const f32x4_any *>(p), hi = *reinterpret_cast<const f32x4_any *>(p + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) v[j] = p[j];
+        }
+    } else {
+        const u32x4 x = eight(static_cast<const uint16_t *>(row) + c, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = T::value((uint16_t)(x[j / 2] >> (j % 2 * 16)));
+    }
+}
+
+// The largest finite |grad_out|: of fp16, whose range dz has to be brought into.
+template <typename T, bool F32>
+__global__ __launch_bounds__(256) void largest_kernel(const void *grad_out, int64_t grad_ld, int32_t N, int32_t M, float *largest) {
+    __shared__ float shared[4];
+    const int32_t units = (M + 7) / 8;
+    float most = 0.0f;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < (int64_t)N * units; k += kLargestBlocks * 256) {
+        const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
+        float v[8];
+        read8<T, F32>(static_cast<const char *>(grad_out) + row * grad_ld * (F32 ? 4 : 2), c, M - c, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = fabsf(v[j]);
+            most = x < __builtin_inff() && x > most ? x : most;
+        }
+    }
+    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) largest[blockIdx.x] = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
+}
+
+// A workgroup has 512 columns of `rows` rows, a wave every fourth of them, a thread eight columns.
+template <typename T, bool F32>
+__global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
+    __shared__ float shared[4][kWave][9];
+    __shared__ float most_of[4];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    float factor = 1.0f;
+    if (a.largest) {
+        float most = a.largest[threadIdx.x];
+        for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        if (lane == 0) most_of[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+        // the power of two that makes it 2^13 to 2^14, and slopes reach 1.13; a power that is no fp32 number itself is not needed
+        int32_t e = most > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+        e = e > 126 ? 126 : e < -126 ? -126 : e;
+        factor = __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.unscale = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+    }
+    const int32_t c = (blockIdx.x * kWave + lane) * 8, r0 = blockIdx.y * a.rows;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (c < a.dz_ld) {
+#pragma unroll 4
+        for (int32_t i = wave; i < a.rows; i += 4) {
+            const int32_t row = r0 + i;
+            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (row < a.N) {
+                read8<T, F32>(static_cast<const char *>(a.grad_out) + row * a.grad_ld * (F32 ? 4 : 2), c, a.M - c, v);
+                if (a.slope) {
+                    const u32x4 s = eight(a.slope + row * a.slope_ld + c, a.M - c);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= slope_value(s[j / 2] >> (j % 2 * 16));
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += v[j];
+            }
+            if (a.dz) {
+                u32x4 d;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[j] = T::round2(v[2 * j] * factor, v[2 * j + 1] * factor);
+                *reinterpret_cast<u32x4 *>(a.dz + (int64_t)row * a.dz_ld + c) = d;
+            }
+        }
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) shared[wave][lane][j] = sum[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kWave * 8; i += 256) {
+        const int32_t at = blockIdx.x * kWave * 8 + i;
+        if (at < a.dz_ld)
+            a.sums[(int64_t)blockIdx.y * a.dz_ld + at] = (shared[0][i / 8][i % 8] + shared[1][i / 8][i % 8]) +
+                                                         (shared[2][i / 8][i % 8] + shared[3][i / 8][i % 8]);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kWave) void bias_kernel(const float *sums, int32_t blocks, int32_t ld, int32_t M, uint16_t *out) {
+    const int32_t c = blockIdx.x * kWave + threadIdx.x;
+    if (c >= M) return;
+    float x = 0.0f;
+    for (int32_t b = 0; b < blocks; b += 8) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = b + i < blocks ? sums[(int64_t)(b + i) * ld + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += y[i];
+    }
+    out[c] = T::round(x);
+}
+
+__global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x)
+        for (int32_t c = threadIdx.x; c < D; c += 256) out[row * out_ld + c] = 0;
+}
+
+// ---------------------------------------------------------------- host
+
+int64_t pad(int64_t x, int64_t to) { return ceil_div(x, to) * to; }
+bool whole_units(const void *p, int64_t stride, int32_t D) { return aligned_to(p, 16) && stride % 8 == 0 && D % 8 == 0; }
+
+// workgroups that are at work at a time: as many to a compute unit as its LDS holds
+template <typename S>
+constexpr int64_t slots() {
+    return 256 * (160 * 1024 / (S::kStages * S::kLds));
+}
+// What a product's tiles take, in microseconds: rounds of as many as are at work at a time, of so many steps each and a beginning and an end.
+template <typename S>
+constexpr double kStepTime = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : 0.6;
+template <typename S>
+constexpr double kEndsTime = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.0 : 4.0;
+
+struct Plan {
+    int shape;  // 64, 128, 256: its extent in n
+    int32_t k_split, splits;
+};
+
+// A product [n][m] over k.  large: the largest tile is there too (it is not for weights at odd addresses).
+Plan plan_of(int64_t m, int64_t n, int64_t k, bool large) {
+    Plan p{};
+    double best = 0;
+    auto look = [&](auto shape) {
+        using S = decltype(shape);
+        const int64_t tiles = ceil_div(m, S::BM) * ceil_div(n, S::BN), steps = ceil_div(k, kStepK);
+        for (int64_t s = 1; s <= 32 && (s == 1 || (s * 4 <= steps && tiles * s <= slots<S>())); ++s) {
+            const int64_t per = ceil_div(steps, s);
+            const double shares = s > 1 ? 4.0 + (double)s * n * pad(m, 4) * 8.0 / 4e6 : 0.0;
+            const double time = (double)ceil_div(tiles * s, slots<S>()) * ((double)per * kStepTime<S> + kEndsTime<S>) + shares;
+            if (best == 0 || time < best) {
+                best = time;
+                p = Plan{S::BN, (int32_t)(per * kStepK), (int32_t)ceil_div(steps, per)};
+            }
+        }
+    };
+    look(Shape64{});
+    look(Shape128{});
+    if (large) look(Shape256{});
+    return p;
+}
+
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool DIRECT, typename E>
+int launch_product_of(ProductArgs a, const E &end, hipStream_t stream) {
+    a.tiles_m = (int32_t)ceil_div(a.m, S::BM);
+    a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = std::min(work, slots<S>());
+    if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
+    hipLaunchKernelGGL((product_kernel<T, S, A_COLUMNS, B_COLUMNS, DIRECT, E>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a, end);
+    return check_launch();
+}
+
+// ws: room for the shares of a sum that is split; taken, or with `launch` used
+template <typename T, bool A_COLUMNS, bool B_COLUMNS, typename E>
+int product(ProductArgs a, const E &end, bool direct, Carver &ws, hipStream_t stream, bool launch) {
+    const Plan p = plan_of(a.m, a.n, a.k, direct);
+    a.k_split = p.k_split, a.splits = p.splits;
+    a.sums_ld = (int32_t)pad(a.m, 4);
+    if (p.splits > 1) a.sums = ws.take<float>((size_t)p.splits * a.n * a.sums_ld);
+    if (!launch) return CFGZIP_OK;
+    if constexpr (!(A_COLUMNS && B_COLUMNS)) {
+        if (!direct) {
+            if (p.shape == 64) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
+            else CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
+        }
+    }
+    if (direct) {
+        if (p.shape == 64) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+        else if (p.shape == 128) CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+        else CFGZIP_TRY((launch_product_of<T, Shape256, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+    }
+    if (p.splits == 1) return CFGZIP_OK;
+    const int64_t units = (int64_t)a.n * (a.sums_ld / 4);
+    hipLaunchKernelGGL((finish_kernel<T, E>), dim3((uint32_t)ceil_div(units, kWave)), dim3(kWave), 0, stream, a.sums, p.splits, a.n, a.sums_ld,
+                       end);
+    return check_launch();
+}
+
+struct Call {
+    const void *hidden;
+    int64_t hidden_stride;
+    const void *weight;
+    int64_t weight_stride;
+    int32_t dtype, N, M, D;
+    const uint16_t *x() const { return static_cast<const uint16_t *>(hidden); }
+    const uint16_t *w() const { return static_cast<const uint16_t *>(weight); }
+};
+
+int check_call(const Call &c) {
+    if (c.N < 0 || c.M <= 0 || c.D <= 0) return CFGZIP_E_INVALID;
+    if (c.dtype != CFGZIP_DTYPE_BF16 && c.dtype != CFGZIP_DTYPE_F16) return CFGZIP_E_INVALID;
+    if (c.N > 0 && (!c.weight || !aligned_to(c.weight, 2) || c.weight_stride < c.D)) return CFGZIP_E_INVALID;
+    if (c.N > 0 && (!c.hidden || !aligned_to(c.hidden, 2) || c.hidden_stride < c.D)) return CFGZIP_E_INVALID;
+    if (c.N > kMaxRows || c.D >= kMaxStride - 64 || c.M >= kMaxStride - 64 || c.weight_stride >= kMaxStride) return CFGZIP_E_TOO_LARGE;
+    return CFGZIP_OK;
+}
+
+int copy_rows(const Call &c, uint16_t *y, int32_t y_ld, int32_t all, hipStream_t stream) {
+    const int64_t units = (int64_t)all * (y_ld / 8);
+    hipLaunchKernelGGL(copy_rows_kernel, dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream, c.x(), c.hidden_stride, c.N, c.D, y, y_ld,
+                       all);
+    return check_launch();
+}
+
+template <typename T>
+int forward(const Call &c, const Forward &end, bool direct, Carver &ws, hipStream_t stream, bool launch) {
+    if (c.N <= kFewRows) {
+        if (!launch) return CFGZIP_OK;
+        const FewArgs a{c.x(), c.w(), c.hidden_stride, c.weight_stride, c.N, c.M, c.D};
+        hipLaunchKernelGGL(few_rows_kernel<T>, dim3((uint32_t)ceil_div(c.M, 16)), dim3(kFewThreads), 0, stream, a, end);
+        return check_launch();
+    }
+    const int32_t d_pad = (int32_t)pad(c.D, kStepK);
+    uint16_t *copy = ws.take<uint16_t>((size_t)c.N * d_pad);
+    const bool as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.D % kStepK == 0 && c.hidden_stride < kMaxStride;
+    if (launch && !as_it_is) CFGZIP_TRY(copy_rows(c, copy, d_pad, c.N, stream));
+    ProductArgs a{};
+    a.A = by_rows(c.w(), c.weight_stride, c.M);
+    a.B = as_it_is ? by_rows(c.x(), c.hidden_stride, c.N) : by_rows(copy, d_pad, c.N);
+    a.m = c.M, a.n = c.N, a.k = c.D;
+    return product<T, false, false>(a, end, direct, ws, stream, launch);
+}
+
+struct Grads {
+    const void *grad_out;
+    int64_t grad_out_stride;
+    int32_t f32;
+    const uint16_t *slope;
+    int64_t slope_stride;
+    uint16_t *hidden, *weight, *bias;
+    int64_t hidden_stride, weight_stride;
+};
+
+template <typename T>
+int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t stream, bool launch) {
+    const int32_t m_pad = (int32_t)pad(c.M, kStepK), n_pad = (int32_t)pad(c.N, kStepK), d_units = (int32_t)pad(c.D, 8);
+    const int32_t rows = c.N <= 1024 ? 16 : 64, blocks = n_pad / rows;
+    float *unscale = ws.take<float>(1), *largest = ws.take<float>(kLargestBlocks), *sums = ws.take<float>((size_t)blocks * m_pad);
+    uint16_t *dz = ws.take<uint16_t>((size_t)n_pad * m_pad), *copy = ws.take<uint16_t>((size_t)n_pad * d_units);
+    // grad_out is dz where nothing has to be done to it
+    const bool as_it_is = !g.slope && !g.f32 && whole_units(g.grad_out, g.grad_out_stride, c.M) && c.M % kStepK == 0 && c.N % kStepK == 0 &&
+                          g.grad_out_stride < kMaxStride;
+    const bool scaled = std::is_same_v<T, Fp16> && !as_it_is;
+    if (launch && (!as_it_is || g.bias)) {
+        if (scaled) {
+            if (g.f32) hipLaunchKernelGGL((largest_kernel<T, true>), dim3(kLargestBlocks), dim3(256), 0, stream, g.grad_out, g.grad_out_stride, c.N, c.M, largest);
+            else hipLaunchKernelGGL((largest_kernel<T, false>), dim3(kLargestBlocks), dim3(256), 0, stream, g.grad_out, g.grad_out_stride, c.N, c.M, largest);
+            CFGZIP_TRY(check_launch());
+        }
+        const bool needed = !as_it_is && (g.hidden || g.weight);
+        const DzArgs a{g.grad_out, g.grad_out_stride, g.slope, g.slope_stride, c.N, c.M, rows, needed ? dz : nullptr, m_pad,
+                       scaled ? largest : nullptr, unscale, g.bias ? sums : nullptr};
+        const dim3 grid((uint32_t)ceil_div(m_pad, kWave * 8), (uint32_t)blocks);
+        if (g.f32) hipLaunchKernelGGL((dz_kernel<T, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((dz_kernel<T, false>), grid, dim3(256), 0, stream, a);
+        CFGZIP_TRY(check_launch());
+        if (g.bias) {
+            hipLaunchKernelGGL(bias_kernel<T>, dim3((uint32_t)ceil_div(c.M, kWave)), dim3(kWave), 0, stream, sums, blocks, m_pad, c.M, g.bias);
+            CFGZIP_TRY(check_launch());
+        }
+    }
+    const uint16_t *const d = as_it_is ? static_cast<const uint16_t *>(g.grad_out) : dz;
+    const int64_t d_ld = as_it_is ? g.grad_out_stride : m_pad;
+    if (g.hidden || !launch) {
+        ProductArgs a{};
+        a.A = by_columns(c.w(), c.weight_stride, c.D);
+        a.B = by_rows(d, d_ld, c.N);
+        a.m = c.D, a.n = c.N, a.k = c.M;
+        Carver own = ws;
+        const Gradient end{scaled ? unscale : nullptr, g.hidden, g.hidden_stride, c.D};
+        CFGZIP_TRY((product<T, true, false>(a, end, direct, own, stream, launch)));
+        if (!launch) ws.used = std::max(ws.used, own.used);
+    }
+    if (g.weight || !launch) {
+        const bool x_as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.N % kStepK == 0 && c.hidden_stride < kMaxStride;
+        if (launch && !x_as_it_is) CFGZIP_TRY(copy_rows(c, copy, d_units, n_pad, stream));
+        ProductArgs a{};
+        a.A = x_as_it_is ? by_columns(c.x(), c.hidden_stride, c.D) : by_columns(copy, d_units, d_units);
+        a.B = by_columns(d, d_ld, m_pad);
+        a.m = c.D, a.n = c.M, a.k = c.N;
+        const Gradient end{scaled ? unscale : nullptr, g.weight, g.weight_stride, c.D};
+        CFGZIP_TRY((product<T, true, true>(a, end, true, ws, stream, launch)));
+    }
+    return CFGZIP_OK;
+}
+
+bool size_ok(int32_t N, int32_t M, int32_t D) {
+    return N > 0 && M > 0 && D > 0 && N <= kMaxRows && M < kMaxStride - 64 && D < kMaxStride - 64;
+}
+
+}  // namespace
+}  // namespace cfgzip
+
+using namespace cfgzip;
+
+extern "C" size_t cfgzip_head_layer_workspace_bytes(int32_t N, int32_t M, int32_t D) {
+    if (!size_ok(N, M, D)) return 0;
+    Call c{};
+    c.N = N, c.M = M, c.D = D;
+    Carver a(nullptr), b(nullptr);  // (weights at odd addresses have other tiles: the larger)
+    forward<Bf16>(c, Forward{}, true, a, nullptr, false);
+    forward<Bf16>(c, Forward{}, false, b, nullptr, false);
+    return std::max(a.used, b.used);
+}
+
+extern "C" size_t cfgzip_head_layer_grad_workspace_bytes(int32_t N, int32_t M, int32_t D) {
+    if (!size_ok(N, M, D)) return 0;
+    Call c{};
+    c.N = N, c.M = M, c.D = D;
+    Carver a(nullptr), b(nullptr);
+    backward<Bf16>(c, Grads{}, true, a, nullptr, false);
+    backward<Bf16>(c, Grads{}, false, b, nullptr, false);
+    return std::max(a.used, b.used);
+}
+
+extern "C" int cfgzip_head_layer(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride, int32_t dtype, int32_t N,
+                                 int32_t M, int32_t D, const void *bias, int32_t activation, const void *residual, int64_t residual_stride,
+                                 void *out, int32_t out_dtype, int64_t out_stride, void *slope, int64_t slope_stride, void *ws, size_t ws_bytes,
+                                 void *stream) {
+    const Call c{hidden, hidden_stride, weight, weight_stride, dtype, N, M, D};
+    CFGZIP_TRY(check_call(c));
+    if (activation < CFGZIP_ACT_NONE || activation > CFGZIP_ACT_SILU) return CFGZIP_E_INVALID;
+    if (out_dtype != dtype && out_dtype != CFGZIP_DTYPE_F32) return CFGZIP_E_INVALID;
+    if (!aligned_to(bias, 2) || !aligned_to(residual, 2) || !aligned_to(slope, 2)) return CFGZIP_E_INVALID;
+    if ((residual && residual_stride < M) || (slope && slope_stride < M) || out_stride < M) return CFGZIP_E_INVALID;
+    if (N == 0) return CFGZIP_OK;
+    const bool f32 = out_dtype == CFGZIP_DTYPE_F32;
+    if (!out || !aligned_to(out, f32 ? 4 : 2)) return CFGZIP_E_INVALID;
+    const size_t need = cfgzip_head_layer_workspace_bytes(N, M, D);
+    if (need && (!ws || !aligned_to(ws, 256) || ws_bytes < need)) return CFGZIP_E_WORKSPACE;
+    const double a = 2.0 * 0.79788456080286535588;  // 2 sqrt(2 / pi)
+    const bool tanh = activation == CFGZIP_ACT_GELU_TANH;
+    const Activation act{activation, tanh ? (float)a : 1.0f, tanh ? (float)(0.044715 * a) : 0.0f};
+    const Forward end{static_cast<const uint16_t *>(bias), static_cast<const uint16_t *>(residual), residual_stride, act, out, out_stride, f32,
+                      static_cast<uint16_t *>(slope), slope_stride, M};
+    Carver carve(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool direct = whole_units(weight, weight_stride, D);
+    return dtype == CFGZIP_DTYPE_BF16 ? forward<Bf16>(c, end, direct, carve, s, true) : forward<Fp16>(c, end, direct, carve, s, true);
+}
+
+extern "C" int cfgzip_head_layer_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride, int32_t dtype,
+                                      int32_t N, int32_t M, int32_t D, const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride,
+                                      const void *slope, int64_t slope_stride, void *grad_hidden, int64_t grad_hidden_stride,
+                                      void *grad_weight, int64_t grad_weight_stride, void *grad_bias, void *ws, size_t ws_bytes,
+                                      void *stream) {
+    const Call c{hidden, hidden_stride, weight, weight_stride, dtype, N, M, D};
+    CFGZIP_TRY(check_call(c));
+    if (grad_out_dtype != dtype && grad_out_dtype != CFGZIP_DTYPE_F32) return CFGZIP_E_INVALID;
+    if (!grad_hidden && !grad_weight && !grad_bias) return CFGZIP_E_INVALID;
+    if (!aligned_to(slope, 2) || !aligned_to(grad_hidden, 2) || !aligned_to(grad_weight, 2) || !aligned_to(grad_bias, 2)) return CFGZIP_E_INVALID;
+    if ((slope && slope_stride < M) || (grad_hidden && grad_hidden_stride < D) || (grad_weight && grad_weight_stride < D)) return CFGZIP_E_INVALID;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (N == 0) {
+        if (grad_weight) {
+            hipLaunchKernelGGL(zero_rows_kernel, dim3(M < 4096 ? M : 4096), dim3(256), 0, s, static_cast<uint16_t *>(grad_weight),
+                               grad_weight_stride, M, D);
+            CFGZIP_TRY(check_launch());
+        }
+        if (!grad_bias) return CFGZIP_OK;
+        hipLaunchKernelGGL(zero_rows_kernel, dim3(1), dim3(256), 0, s, static_cast<uint16_t *>(grad_bias), (int64_t)M, 1, M);
+        return check_launch();
+    }
+    const bool f32 = grad_out_dtype == CFGZIP_DTYPE_F32;
+    if (!grad_out || !aligned_to(grad_out, f32 ? 4 : 2) || grad_out_stride < M) return CFGZIP_E_INVALID;
+    if (!ws || !aligned_to(ws, 256) || ws_bytes < cfgzip_head_layer_grad_workspace_bytes(N, M, D)) return CFGZIP_E_WORKSPACE;
+    const Grads g{grad_out, grad_out_stride, f32, static_cast<const uint16_t *>(slope), slope_stride, static_cast<uint16_t *>(grad_hidden),
+                  static_cast<uint16_t *>(grad_weight), static_cast<uint16_t *>(grad_bias), grad_hidden_stride, grad_weight_stride};
+    Carver carve(ws);
+    const bool direct = whole_units(weight, weight_stride, D);
+    return dtype == CFGZIP_DTYPE_BF16 ? backward<Bf16>(c, g, direct, carve, s, true) : backward<Fp16>(c, g, direct, carve, s, true);
+}
