@@ -36,6 +36,11 @@ _HEAD_CALLS = ("head_loss", "head_loss_grad", "mx4_quantize", "mx4_values", "mx4
 _HEAD_ENTRIES = ("head_loss_workspace_bytes", "head_loss", "head_loss_grad_workspace_bytes", "head_loss_grad", "mx4_quantize",
                  "mx4_values", "mx4_logits_workspace_bytes", "mx4_logits")
 _head_loss = _head_loss_grad = _mx4_quantize = _mx4_values = _mx4_logits = None
+# the same of what is read from logits and of the layer in front of the projection
+_LAYER_CALLS = ("token_logprobs", "token_logprobs_grad", "head_layer", "head_layer_grad")
+_LAYER_ENTRIES = ("token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_grad", "head_layer_workspace_bytes", "head_layer",
+                  "head_layer_grad_workspace_bytes", "head_layer_grad")
+_token_logprobs = _token_logprobs_grad = _head_layer = _head_layer_grad = None
 
 DEFAULT_HASH_SEED = 0x5EED_CF62_1234_ABCD
 
@@ -80,7 +85,9 @@ def _load_stepcall(lib: ctypes.CDLL):
     """The calls of the extension.  They save host time and nothing else: every call goes through ctypes as
     well, so an extension that is not there, or was built for another torch or Python, is done without."""
     global _head_loss, _head_loss_grad, _mx4_quantize, _mx4_values, _mx4_logits
+    global _token_logprobs, _token_logprobs_grad, _head_layer, _head_layer_grad
     _head_loss = _head_loss_grad = _mx4_quantize = _mx4_values = _mx4_logits = _by_ctypes
+    _token_logprobs = _token_logprobs_grad = _head_layer = _head_layer_grad = _by_ctypes
     try:
         loader = importlib.machinery.ExtensionFileLoader("cfgzip_stepcall", _STEPCALL_PATH)
         spec = importlib.util.spec_from_file_location("cfgzip_stepcall", _STEPCALL_PATH, loader=loader)
@@ -96,6 +103,8 @@ def _load_stepcall(lib: ctypes.CDLL):
     stepcall.connect(*(ctypes.cast(getattr(lib, "cfgzip_" + f), ctypes.c_void_p).value for f in _CALLS))
     stepcall.connect_head(*(ctypes.cast(getattr(lib, "cfgzip_" + f), ctypes.c_void_p).value for f in _HEAD_ENTRIES))
     _head_loss, _head_loss_grad, _mx4_quantize, _mx4_values, _mx4_logits = (getattr(stepcall, f) for f in _HEAD_CALLS)
+    stepcall.connect_layer(*(ctypes.cast(getattr(lib, "cfgzip_" + f), ctypes.c_void_p).value for f in _LAYER_ENTRIES))
+    _token_logprobs, _token_logprobs_grad, _head_layer, _head_layer_grad = (getattr(stepcall, f) for f in _LAYER_CALLS)
     return tuple(getattr(stepcall, f) for f in _CALLS)
 
 
@@ -953,6 +962,13 @@ MAX_TOP = 64
 MAX_TOKENS = 4096
 
 
+def _on(device):
+    """A call's own device as the current one, whose stream it takes and where it launches"""
+    if _current_device is not None and device.index == _current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
 def _tokens(logits, tokens, bits, class_of_token, C):
     """The arguments that cfgzip_token_logprobs and cfgzip_token_logprobs_grad share, but for the temperature"""
     p, stride = _rows(logits, "logits", tuple(_DTYPE))
@@ -988,6 +1004,13 @@ def cfgzip_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] =
     [N, top] (None for top = 0, at most MAX_TOP): the admitted tokens with the largest logits, of equal ones the lowest first, -1 and -inf
     where there are no more.  Autograd knows nothing of it."""
     lib = _lib or load_library()
+    if (logprob is None and entropy is None and stats is None and top_tokens is None and top_logprobs is None and workspace is None
+            and stream is None):
+        out = _token_logprobs(logits, tokens, top, temperature, bits, class_of_token, C)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_token_logprobs", out)
+            return out
     args, masks = _tokens(logits, tokens, bits, class_of_token, C)
     N, V, n = args[2], args[3], args[6]
     dev = logits.device
@@ -1011,13 +1034,14 @@ def cfgzip_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] =
         need = lib.cfgzip_token_logprobs_workspace_bytes(N, V, top)
         workspace = _workspace(need, dev, stream) if need else None
     _same_device(dev, logprob=logprob, entropy=entropy, stats=stats, top_tokens=top_tokens, top_logprobs=top_logprobs, workspace=workspace)
-    rc = lib.cfgzip_token_logprobs(
-        *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
-        _vector(entropy, torch.float32, N, "entropy"), _vector(stats, torch.float32, 2 * N, "stats"), top,
-        _vector(top_tokens, torch.int32, N * top, "top_tokens") if top > 0 else None,
-        _vector(top_logprobs, torch.float32, N * top, "top_logprobs") if top > 0 else None,
-        _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
-        workspace.numel() if workspace is not None else 0, _stream(stream))
+    with _on(dev):
+        rc = lib.cfgzip_token_logprobs(
+            *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
+            _vector(entropy, torch.float32, N, "entropy"), _vector(stats, torch.float32, 2 * N, "stats"), top,
+            _vector(top_tokens, torch.int32, N * top, "top_tokens") if top > 0 else None,
+            _vector(top_logprobs, torch.float32, N * top, "top_logprobs") if top > 0 else None,
+            _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
+            workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("cfgzip_token_logprobs", rc)
     return logprob, entropy, stats, top_tokens, top_logprobs
 
@@ -1031,6 +1055,12 @@ def cfgzip_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tens
     has no gradient), with logprob, stats and entropy of cfgzip_token_logprobs on the same inputs.  grad_logits may be the logits
     themselves.  Tokens that are none or not admitted, and all others of a row that admits nothing, have no gradient."""
     lib = _lib or load_library()
+    if grad_logits is None and stream is None:
+        out = _token_logprobs_grad(logits, tokens, logprob, stats, grad_logprob, entropy, grad_entropy, temperature, bits, class_of_token, C)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_token_logprobs_grad", out)
+            return out
     args, masks = _tokens(logits, tokens, bits, class_of_token, C)
     N, V, n = args[2], args[3], args[6]
     dev = logits.device
@@ -1045,11 +1075,12 @@ def cfgzip_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tens
         raise ValueError(f"grad_logits must have {N} rows")
     _same_device(dev, logprob=logprob, stats=stats, grad_logprob=grad_logprob, entropy=entropy, grad_entropy=grad_entropy,
                  grad_logits=grad_logits)
-    rc = lib.cfgzip_token_logprobs_grad(
-        *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
-        _vector(stats, torch.float32, 2 * N, "stats"), _like_tokens(grad_logprob, tokens, "grad_logprob") if n else None,
-        _vector(entropy, torch.float32, N, "entropy") if grad_entropy is not None else None,
-        _vector(grad_entropy, torch.float32, N, "grad_entropy") if grad_entropy is not None else None, p, stride, _stream(stream))
+    with _on(dev):
+        rc = lib.cfgzip_token_logprobs_grad(
+            *args, float(temperature), *masks, _like_tokens(logprob, tokens, "logprob") if n else None,
+            _vector(stats, torch.float32, 2 * N, "stats"), _like_tokens(grad_logprob, tokens, "grad_logprob") if n else None,
+            _vector(entropy, torch.float32, N, "entropy") if grad_entropy is not None else None,
+            _vector(grad_entropy, torch.float32, N, "grad_entropy") if grad_entropy is not None else None, p, stride, _stream(stream))
     _check("cfgzip_token_logprobs_grad", rc)
     return grad_logits
 
@@ -1083,6 +1114,13 @@ def cfgzip_head_layer(hidden: torch.Tensor, weight: torch.Tensor, bias: Optional
     "gelu", "gelu_tanh" or "silu".  slope int16 [N, M] (if it is wanted or given, else None): act' for cfgzip_head_layer_grad,
     which q of it stands for as q |q| / 2^28.  `out` may be `residual`.  Autograd knows nothing of it."""
     lib = _lib or load_library()
+    if out is None and slope is None and workspace is None and stream is None:
+        made = _head_layer(hidden, weight, bias, _ACTIVATIONS.get(activation, -1), residual, None if dtype is None else _DTYPE.get(dtype, -1),
+                           want_slope)
+        if made is not None:
+            if type(made) is int:
+                _check("cfgzip_head_layer", made)
+            return made
     args = _layer(hidden, weight)
     N, M, D = args[5:]
     dev = weight.device
@@ -1102,9 +1140,10 @@ def cfgzip_head_layer(hidden: torch.Tensor, weight: torch.Tensor, bias: Optional
         need = lib.cfgzip_head_layer_workspace_bytes(N, M, D)
         workspace = _workspace(need, dev, stream) if need else None
     _same_device(dev, hidden=hidden, bias=bias, residual=residual, out=out, slope=slope, workspace=workspace)
-    rc = lib.cfgzip_head_layer(*args, b, _ACTIVATIONS[activation], *r, o, _DTYPE[out.dtype], o_stride, *s,
-                               _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
-                               workspace.numel() if workspace is not None else 0, _stream(stream))
+    with _on(dev):
+        rc = lib.cfgzip_head_layer(*args, b, _ACTIVATIONS[activation], *r, o, _DTYPE[out.dtype], o_stride, *s,
+                                   _dev(workspace, torch.uint8, "workspace") if workspace is not None else None,
+                                   workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("cfgzip_head_layer", rc)
     return out, slope
 
@@ -1117,6 +1156,12 @@ def cfgzip_head_layer_grad(hidden: torch.Tensor, weight: torch.Tensor, grad_out:
     """(grad_hidden [N, D], grad_weight [M, D], grad_bias [M]) in the inputs' type, each None if it is not wanted, for grad_out [N, M] (that type or
     float32), with the slope of cfgzip_head_layer on the same inputs (None where there is no activation).  The residual's gradient is grad_out."""
     lib = _lib or load_library()
+    if grad_hidden is None and grad_weight is None and grad_bias is None and workspace is None and stream is None:
+        out = _head_layer_grad(hidden, weight, grad_out, slope, want_hidden, want_weight, want_bias)
+        if out is not None:
+            if type(out) is int:
+                _check("cfgzip_head_layer_grad", out)
+            return out
     args = _layer(hidden, weight)
     N, M, D = args[5:]
     dev = weight.device
@@ -1137,7 +1182,8 @@ def cfgzip_head_layer_grad(hidden: torch.Tensor, weight: torch.Tensor, grad_out:
         workspace = _workspace(lib.cfgzip_head_layer_grad_workspace_bytes(N, M, D), dev, stream)
     _same_device(dev, hidden=hidden, grad_out=grad_out, slope=slope, grad_hidden=grad_hidden, grad_weight=grad_weight, grad_bias=grad_bias,
                  workspace=workspace)
-    rc = lib.cfgzip_head_layer_grad(*args, g, _DTYPE[grad_out.dtype], g_stride, *s, *gh, *gw, gb, _dev(workspace, torch.uint8, "workspace"),
-                                    workspace.numel(), _stream(stream))
+    with _on(dev):
+        rc = lib.cfgzip_head_layer_grad(*args, g, _DTYPE[grad_out.dtype], g_stride, *s, *gh, *gw, gb, _dev(workspace, torch.uint8, "workspace"),
+                                        workspace.numel(), _stream(stream))
     _check("cfgzip_head_layer_grad", rc)
     return grad_hidden if want_hidden else None, grad_weight if want_weight else None, grad_bias if want_bias else None

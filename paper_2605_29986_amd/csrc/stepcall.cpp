@@ -3,7 +3,7 @@
 // and checks of tensors, the conversion of as many arguments for ctypes) took 5 us of the 8 that a step on small logits
 // takes, and the kernel 3; and of the 44 us of signatures and classes of 4,096 tokens, 157 of displacements and classes of
 // 32,000 and 165 of relations and classes of 32,000 it took 5, 6 and 4, as the GPU has nothing to do before the first launch.
-// The vocabulary projection's calls are here for the same reason, with results and workspace of their own only.
+// The calls of the vocabulary projection, of what is read from its logits and of the layer in front of it are here for the same reason, with results and workspace of their own only.
 //
 // Marshalling only, and only of the plain case: exact torch.Tensor objects in GPU memory of the types and layouts the
 // binding asks for, the current stream.  For anything else a function returns None and has done nothing; the binding then
@@ -15,6 +15,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -64,6 +65,24 @@ Mx4Quantize g_mx4_quantize = nullptr;
 Mx4Values g_mx4_values = nullptr;
 Mx4LogitsBytes g_mx4_logits_bytes = nullptr;
 Mx4Logits g_mx4_logits = nullptr;
+
+using TokenLogprobsBytes = size_t (*)(int32_t, int32_t, int32_t);
+using TokenLogprobs = int (*)(const void *, int32_t, int32_t, int32_t, int64_t, const int32_t *, int32_t, double, const int32_t *, int32_t,
+                              const int32_t *, int32_t, float *, float *, float *, int32_t, int32_t *, float *, void *, size_t, void *);
+using TokenLogprobsGrad = int (*)(const void *, int32_t, int32_t, int32_t, int64_t, const int32_t *, int32_t, double, const int32_t *, int32_t,
+                                  const int32_t *, int32_t, const float *, const float *, const float *, const float *, const float *, void *,
+                                  int64_t, void *);
+using HeadLayerBytes = size_t (*)(int32_t, int32_t, int32_t);
+using HeadLayer = int (*)(const void *, int64_t, const void *, int64_t, int32_t, int32_t, int32_t, int32_t, const void *, int32_t, const void *,
+                          int64_t, void *, int32_t, int64_t, void *, int64_t, void *, size_t, void *);
+using HeadLayerGrad = int (*)(const void *, int64_t, const void *, int64_t, int32_t, int32_t, int32_t, int32_t, const void *, int32_t, int64_t,
+                              const void *, int64_t, void *, int64_t, void *, int64_t, void *, void *, size_t, void *);
+TokenLogprobsBytes g_token_logprobs_bytes = nullptr;
+TokenLogprobs g_token_logprobs = nullptr;
+TokenLogprobsGrad g_token_logprobs_grad = nullptr;
+HeadLayerBytes g_head_layer_bytes = nullptr, g_head_layer_grad_bytes = nullptr;
+HeadLayer g_head_layer = nullptr;
+HeadLayerGrad g_head_layer_grad = nullptr;
 
 constexpr int64_t kMost = std::numeric_limits<int32_t>::max();
 
@@ -729,6 +748,255 @@ PyObject *connect_head(PyObject *, PyObject *const *args, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// ---------------------------------------------------------------- log probabilities, the layer in front of the projection
+
+// On the device whose current stream a call takes; others are left to the general way.
+bool here(const at::Tensor &t) { return t.device().index() == c10::hip::current_device(); }
+
+// (logits, tokens, .., temperature, bits, class_of_token, C): what log probabilities and their gradient share.  No rows are left to the general way.
+struct Score {
+    Matrix logits;
+    const at::Tensor *tokens = nullptr;  // none: null
+    int32_t n = 0;
+    double temperature = 0.0;
+    Masks masks;
+    const int32_t *ids() const { return tokens ? static_cast<const int32_t *>(tokens->data_ptr()) : nullptr; }
+};
+bool score_of(PyObject *logits, PyObject *tokens, PyObject *temperature, PyObject *const *masks, Score *out) {
+    if (!matrix_of(logits, &out->logits) || out->logits.rows < 1 || !here(*out->logits.t) || !PyFloat_CheckExact(temperature)) return false;
+    out->temperature = PyFloat_AS_DOUBLE(temperature);
+    if (tokens != Py_None) {
+        const at::Tensor *t = plain(tokens, at::kInt);
+        if (!t || (t->dim() != 1 && t->dim() != 2) || t->size(0) != out->logits.rows || t->device() != out->logits.t->device()) return false;
+        const int64_t n = t->dim() == 1 ? 1 : t->size(1);
+        if (n < 1 || n > kMost) return false;
+        out->tokens = t;
+        out->n = (int32_t)n;
+    }
+    return masks_of(masks[0], masks[1], masks[2], out->logits.rows, out->logits.columns, *out->logits.t, &out->masks);
+}
+// n values beside a tensor, or None
+bool vector_or_none(PyObject *o, int64_t n, const at::Tensor &beside, const float **out) {
+    *out = nullptr;
+    if (o == Py_None) return true;
+    *out = static_cast<const float *>(vector_of(o, at::kFloat, n, beside));
+    return *out != nullptr;
+}
+
+// (logits, tokens, top, temperature, bits, class_of_token, C)
+PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 7 || !g_token_logprobs || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Score s{};
+    float *logprob = nullptr, *entropy = nullptr, *stats = nullptr, *top_logprobs = nullptr;
+    int32_t *top_tokens = nullptr, top = 0;
+    void *ws = nullptr, *stream = nullptr;
+    size_t bytes = 0;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        if (!score_of(args[0], args[1], args[3], args + 4, &s) || !PyLong_CheckExact(args[2])) return leave_it();
+        const long k = PyLong_AsLong(args[2]);
+        if (k < 0 || k > 64) return leave_it();
+        top = (int32_t)k;
+        const auto floats = s.logits.t->options().dtype(at::kFloat), ints = s.logits.t->options().dtype(at::kInt);
+        const int64_t N = s.logits.rows;
+        at::Tensor made_logprob, made_tokens, made_top;
+        const at::Tensor made_entropy = at::empty({N}, floats), made_stats = at::empty({N, 2}, floats);
+        entropy = static_cast<float *>(made_entropy.data_ptr());
+        stats = static_cast<float *>(made_stats.data_ptr());
+        if (s.tokens) {
+            made_logprob = at::empty(s.tokens->sizes(), floats);
+            logprob = static_cast<float *>(made_logprob.data_ptr());
+        }
+        if (top) {
+            made_tokens = at::empty({N, top}, ints);
+            made_top = at::empty({N, top}, floats);
+            top_tokens = static_cast<int32_t *>(made_tokens.data_ptr());
+            top_logprobs = static_cast<float *>(made_top.data_ptr());
+        }
+        bytes = g_token_logprobs_bytes(s.logits.rows, s.logits.columns, top);
+        if (bytes) {
+            workspace = workspace_of(bytes, *s.logits.t);
+            ws = workspace.data_ptr();
+            bytes = (size_t)workspace.numel();
+        }
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(s.tokens ? THPVariable_Wrap(made_logprob) : Py_NewRef(Py_None)), b(THPVariable_Wrap(made_entropy)),
+            c(THPVariable_Wrap(made_stats)), d(top ? THPVariable_Wrap(made_tokens) : Py_NewRef(Py_None)),
+            e(top ? THPVariable_Wrap(made_top) : Py_NewRef(Py_None));
+        if (a.o && b.o && c.o && d.o && e.o) result = PyTuple_Pack(5, a.o, b.o, c.o, d.o, e.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_token_logprobs(s.logits.data, s.logits.type, s.logits.rows, s.logits.columns, s.logits.stride, s.ids(), s.n, s.temperature,
+                          s.masks.bits, s.masks.kind, s.masks.class_of_token, s.masks.C, logprob, entropy, stats, top, top_tokens, top_logprobs,
+                          ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// (logits, tokens, logprob, stats, grad_logprob, entropy, grad_entropy, temperature, bits, class_of_token, C)
+PyObject *token_logprobs_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 11 || !g_token_logprobs_grad || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Score s{};
+    const float *logprob = nullptr, *stats = nullptr, *grad_logprob = nullptr, *entropy = nullptr, *grad_entropy = nullptr;
+    void *out = nullptr, *stream = nullptr;
+    PyObject *result = nullptr;
+    try {
+        if (!score_of(args[0], args[1], args[7], args + 8, &s)) return leave_it();
+        const at::Tensor &beside = *s.logits.t;
+        const int64_t N = s.logits.rows;
+        stats = static_cast<const float *>(vector_of(args[3], at::kFloat, 2 * N, beside));
+        if (!stats || !vector_or_none(args[6], N, beside, &grad_entropy) ||
+            !vector_or_none(grad_entropy ? args[5] : Py_None, N, beside, &entropy) || (grad_entropy && !entropy))
+            return leave_it();
+        if (s.tokens) {
+            logprob = static_cast<const float *>(vector_of(args[2], at::kFloat, N * s.n, beside));
+            grad_logprob = static_cast<const float *>(vector_of(args[4], at::kFloat, N * s.n, beside));
+            if (!logprob || !grad_logprob || plain(args[2])->sizes() != s.tokens->sizes() || plain(args[4])->sizes() != s.tokens->sizes())
+                return leave_it();
+        }
+        const at::Tensor made = at::empty({N, s.logits.columns}, beside.options());
+        out = made.data_ptr();
+        stream = c10::hip::getCurrentHIPStream().stream();
+        result = THPVariable_Wrap(made);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_token_logprobs_grad(s.logits.data, s.logits.type, s.logits.rows, s.logits.columns, s.logits.stride, s.ids(), s.n, s.temperature,
+                               s.masks.bits, s.masks.kind, s.masks.class_of_token, s.masks.C, logprob, stats, grad_logprob, entropy,
+                               grad_entropy, out, s.logits.columns, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// rows x columns values of `type` beside a tensor, rows any distance apart; for None `data` is null
+struct Rows {
+    const void *data = nullptr;
+    int64_t stride = 0;
+};
+bool rows_of(PyObject *o, at::ScalarType type, int64_t rows, int64_t columns, const at::Tensor &beside, Rows *out) {
+    if (o == Py_None) return true;
+    const at::Tensor *t = plain(o);
+    if (!t || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != columns || (columns > 1 && t->stride(1) != 1) ||
+        t->device() != beside.device())
+        return false;
+    out->stride = rows > 1 || t->stride(0) > columns ? t->stride(0) : columns;
+    out->data = t->data_ptr();
+    return out->stride >= columns;
+}
+bool layer_of(PyObject *const *args, Matrix *hidden, Matrix *weight) {
+    return matrix_of(args[0], hidden) && matrix_of(args[1], weight) && weight->type != 0 && hidden->type == weight->type &&
+           hidden->columns == weight->columns && hidden->rows >= 1 && weight->rows >= 1 && hidden->t->device() == weight->t->device() &&
+           here(*weight->t);
+}
+
+// (hidden, weight, bias, activation's number, residual, the result's type, want_slope)
+PyObject *head_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 7 || !g_head_layer || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Matrix x{}, w{};
+    Rows residual;
+    const void *bias = nullptr;
+    int32_t activation = -1, type = -1;
+    bool want_slope = false;
+    void *out = nullptr, *slope = nullptr, *ws = nullptr, *stream = nullptr;
+    size_t bytes = 0;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        if (!layer_of(args, &x, &w) || !bool_of(args[6], &want_slope)) return leave_it();
+        activation = type_of(args[3], 4);
+        type = args[5] == Py_None ? w.type : type_of(args[5], 2);
+        if (activation < 0 || (type != 0 && type != w.type) || !rows_of(args[4], kTypes[w.type], x.rows, w.rows, *w.t, &residual)) return leave_it();
+        if (args[2] != Py_None && !(bias = vector_of(args[2], kTypes[w.type], w.rows, *w.t))) return leave_it();
+        const at::Tensor made = at::empty({x.rows, w.rows}, w.t->options().dtype(kTypes[type]));
+        out = made.data_ptr();
+        at::Tensor made_slope;
+        if (want_slope) {
+            made_slope = at::empty({x.rows, w.rows}, w.t->options().dtype(at::kShort));
+            slope = made_slope.data_ptr();
+        }
+        bytes = g_head_layer_bytes(x.rows, w.rows, w.columns);
+        if (bytes) {
+            workspace = workspace_of(bytes, *w.t);
+            ws = workspace.data_ptr();
+            bytes = (size_t)workspace.numel();
+        }
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(THPVariable_Wrap(made)), b(want_slope ? THPVariable_Wrap(made_slope) : Py_NewRef(Py_None));
+        if (a.o && b.o) result = PyTuple_Pack(2, a.o, b.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_head_layer(x.data, x.stride, w.data, w.stride, w.type, x.rows, w.rows, w.columns, bias, activation, residual.data, residual.stride,
+                      out, type, w.rows, slope, slope ? w.rows : 0, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// (hidden, weight, grad_out, slope, want_hidden, want_weight, want_bias)
+PyObject *head_layer_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 7 || !g_head_layer_grad || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
+    Matrix x{}, w{}, g{};
+    Rows slope;
+    bool want[3] = {false, false, false};
+    void *out[3] = {nullptr, nullptr, nullptr}, *ws = nullptr, *stream = nullptr;
+    at::Tensor workspace;
+    PyObject *result = nullptr;
+    try {
+        if (!layer_of(args, &x, &w) || !matrix_of(args[2], &g) || g.rows != x.rows || g.columns != w.rows || (g.type != 0 && g.type != w.type) ||
+            g.t->device() != w.t->device() || !rows_of(args[3], at::kShort, x.rows, w.rows, *w.t, &slope) || !bool_of(args[4], &want[0]) ||
+            !bool_of(args[5], &want[1]) || !bool_of(args[6], &want[2]) || !(want[0] || want[1] || want[2]))
+            return leave_it();
+        at::Tensor made[3];
+        if (want[0]) made[0] = at::empty({x.rows, w.columns}, w.t->options());
+        if (want[1]) made[1] = at::empty({w.rows, w.columns}, w.t->options());
+        if (want[2]) made[2] = at::empty({w.rows}, w.t->options());
+        for (int i = 0; i < 3; ++i) out[i] = want[i] ? made[i].data_ptr() : nullptr;
+        workspace = workspace_of(g_head_layer_grad_bytes(x.rows, w.rows, w.columns), *w.t);
+        ws = workspace.data_ptr();
+        stream = c10::hip::getCurrentHIPStream().stream();
+        const Held a(want[0] ? THPVariable_Wrap(made[0]) : Py_NewRef(Py_None)), b(want[1] ? THPVariable_Wrap(made[1]) : Py_NewRef(Py_None)),
+            c(want[2] ? THPVariable_Wrap(made[2]) : Py_NewRef(Py_None));
+        if (a.o && b.o && c.o) result = PyTuple_Pack(3, a.o, b.o, c.o);
+    } catch (...) {
+    }
+    if (!result) return leave_it();
+    int rc = 0;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_head_layer_grad(x.data, x.stride, w.data, w.stride, w.type, x.rows, w.rows, w.columns, g.data, g.type, g.stride, slope.data,
+                           slope.stride, out[0], out[0] ? w.columns : 0, out[1], out[1] ? w.columns : 0, out[2], ws,
+                           (size_t)workspace.numel(), stream);
+    Py_END_ALLOW_THREADS
+    return finish(rc, result);
+}
+
+// The addresses of cfgzip_token_logprobs_workspace_bytes, cfgzip_token_logprobs, cfgzip_token_logprobs_grad, cfgzip_head_layer_workspace_bytes,
+// cfgzip_head_layer, cfgzip_head_layer_grad_workspace_bytes and cfgzip_head_layer_grad
+PyObject *connect_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    void *at[7];
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "connect_layer takes seven addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 7; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+    if (PyErr_Occurred()) return nullptr;
+    g_token_logprobs_bytes = reinterpret_cast<TokenLogprobsBytes>(at[0]);
+    g_token_logprobs = reinterpret_cast<TokenLogprobs>(at[1]);
+    g_token_logprobs_grad = reinterpret_cast<TokenLogprobsGrad>(at[2]);
+    g_head_layer_bytes = reinterpret_cast<HeadLayerBytes>(at[3]);
+    g_head_layer = reinterpret_cast<HeadLayer>(at[4]);
+    g_head_layer_grad_bytes = reinterpret_cast<HeadLayerBytes>(at[5]);
+    g_head_layer_grad = reinterpret_cast<HeadLayerGrad>(at[6]);
+    Py_RETURN_NONE;
+}
+
 // The addresses of cfgzip_decode_step, cfgzip_engine_step, cfgzip_signatures, cfgzip_build_classes, cfgzip_displacements and
 // cfgzip_nfa_signatures, of the library that the binding has loaded
 PyObject *connect(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -765,6 +1033,11 @@ PyMethodDef g_methods[] = {{"decode_step", fast<decode_step>(), METH_FASTCALL, n
                            {"mx4_values", fast<mx4_values>(), METH_FASTCALL, nullptr},
                            {"mx4_logits", fast<mx4_logits>(), METH_FASTCALL, nullptr},
                            {"connect_head", fast<connect_head>(), METH_FASTCALL, nullptr},
+                           {"token_logprobs", fast<token_logprobs>(), METH_FASTCALL, nullptr},
+                           {"token_logprobs_grad", fast<token_logprobs_grad>(), METH_FASTCALL, nullptr},
+                           {"head_layer", fast<head_layer>(), METH_FASTCALL, nullptr},
+                           {"head_layer_grad", fast<head_layer_grad>(), METH_FASTCALL, nullptr},
+                           {"connect_layer", fast<connect_layer>(), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "cfgzip_stepcall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
