@@ -28,42 +28,85 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // A slope in 16 bits: the root of its size in steps of 2^-14, with its sign.  It is off by 2^-14 of that root at the most, 2^-15 rms near 1, an eighth
 // of what fp16 is off there (whose error was as large as dz's own rounding: gradients of 777 fp16 rows 1.8 times as far from 64 bits as their
-// own rounding makes them), and 0 and 1 are exact.
-__device__ __forceinline__ uint32_t slope_code(float s) {
-    const float root = __builtin_amdgcn_sqrtf(fabsf(s)) * 0x1p14f;
-    return (uint32_t)(int32_t)__builtin_rintf(__builtin_copysignf(root, s)) & 0xFFFFu;
+// own rounding makes them), and 0 and 1 are exact.  The code is the low half of the sum's bits: 1.5 * 2^23 leaves whole numbers there.
+__device__ __forceinline__ uint32_t slope_bits(float s) {
+    const float root = __builtin_copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s);
+    return __builtin_bit_cast(uint32_t, __builtin_fmaf(root, 0x1p14f, 0x1.8p23f));
+}
+__device__ __forceinline__ uint32_t slope_codes(float s0, float s1) {  // the first in the low half
+    return __builtin_amdgcn_perm(slope_bits(s1), slope_bits(s0), 0x05040100);
 }
 __device__ __forceinline__ float slope_value(uint32_t code) {
     const float root = (float)(int16_t)code * 0x1p-14f;
     return root * fabsf(root);
 }
 
+// The normal distribution's half (1 + erf(z / sqrt 2)) / 2, and exp(-z^2 / 2).  For z < 0 it is t P(t) exp(-z^2 / 2) with t = 1 / (1 - 0.318198 z), P of
+// degree 7 fitted for the least largest relative error (3.3e-7) over 0 .. -15.5, where it is 0 in fp32; no branch.
+__device__ __forceinline__ float normal(float z, float &bell) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(z), 0.31819806f, 1.0f));
+    bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+    float p = __builtin_fmaf(0.03383570536971092f, t, -0.12183640897274017f);
+    p = __builtin_fmaf(p, t, 0.10739953070878983f);
+    p = __builtin_fmaf(p, t, 0.01735507883131504f);
+    p = __builtin_fmaf(p, t, 0.0958288237452507f);
+    p = __builtin_fmaf(p, t, 0.11357394605875015f);
+    p = __builtin_fmaf(p, t, 0.1268940418958664f);
+    p = __builtin_fmaf(p, t, 0.1269494593143463f);
+    const float below = p * t * bell;
+    return z < 0.0f ? below : 1.0f - below;
+}
+
 // act(z) = z q(z): q = 1 / (1 + exp(-z (a + b z^2))) is silu's for a = 1, b = 0, and gelu_tanh's, whose (1 + tanh u) / 2 is the logistic
 // function of 2 u, for a = 2 sqrt(2 / pi), b = 0.044715 a.
 struct Activation {
     int32_t kind;
-    float a, b;
+    float a, b;  // of neither: what is not above a is 0 (-infinity: there is no activation)
 
+    template <int KIND>
     __device__ __forceinline__ float of(float z, float &slope) const {
-        if (kind == CFGZIP_ACT_NONE) {
-            slope = 1.0f;
-            return z;
-        }
-        if (kind == CFGZIP_ACT_RELU) {
-            slope = z > 0.0f ? 1.0f : 0.0f;
-            return z < 0.0f ? 0.0f : z;
-        }
-        if (kind == CFGZIP_ACT_GELU) {
-            const float q = 0.5f * erfcf(z * -0.70710678118654752440f);
-            slope = __builtin_fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e)), q);
+        if constexpr (KIND == CFGZIP_ACT_RELU) {
+            slope = z > a ? 1.0f : 0.0f;
+            return z < a ? 0.0f : z;
+        } else if constexpr (KIND == CFGZIP_ACT_GELU) {
+            float bell;
+            const float q = normal(z, bell);
+            slope = __builtin_fmaf(z * 0.39894228040143267794f, bell, q);
+            return z * q;
+        } else {
+            const float zz = z * z, u = z * __builtin_fmaf(b, zz, a);
+            const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -kLog2e));
+            slope = __builtin_fmaf(z * q * (1.0f - q), __builtin_fmaf(3.0f * b, zz, a), q);
             return z * q;
         }
-        const float zz = z * z, u = z * __builtin_fmaf(b, zz, a);
-        const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -kLog2e));
-        slope = __builtin_fmaf(z * q * (1.0f - q), __builtin_fmaf(3.0f * b, zz, a), q);
-        return z * q;
+    }
+    // f(kind) with the kind as a constant
+    template <typename F>
+    __device__ __forceinline__ void with(F &&f) const {
+        if (kind <= CFGZIP_ACT_RELU) f(std::integral_constant<int, CFGZIP_ACT_RELU>{});
+        else if (kind == CFGZIP_ACT_GELU) f(std::integral_constant<int, CFGZIP_ACT_GELU>{});
+        else f(std::integral_constant<int, CFGZIP_ACT_SILU>{});
     }
 };
+
+// four 16-bit values of which `left` are there
+__device__ __forceinline__ u32x2 read4(const uint16_t *p, int32_t left) {
+    if (left >= 4) return u32x2(*reinterpret_cast<const u32x2_any *>(p));
+    u32x2 v = {0, 0};
+    for (int i = 0; i < left; ++i) v[i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
+    return v;
+}
+__device__ __forceinline__ void write4(uint16_t *p, u32x2 v, int32_t left) {
+    if (left >= 4) {
+        *reinterpret_cast<u32x2_any *>(p) = v;
+    } else {
+        for (int i = 0; i < left; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+    }
+}
+template <typename T>
+__device__ __forceinline__ float value_at(u32x2 v, int i) {
+    return T::value((uint16_t)(v[i / 2] >> (i % 2 * 16)));
+}
 
 struct Forward {
     const uint16_t *bias;      // or null
@@ -77,45 +120,57 @@ struct Forward {
     int64_t slope_ld;
     int32_t M;
 
-    // results m .. m + 3 (as many as there are) of row n
+    // What results m .. m + 3 (as many as there are) ask of memory: of all rows, and of row n.
+    typedef u32x2 Column;
+    typedef u32x2 Row;
+    __device__ __forceinline__ Column column(int32_t m) const { return bias ? read4(bias + m, M - m) : u32x2{0, 0}; }
+    __device__ __forceinline__ Row row(int32_t n, int32_t m) const {
+        return residual ? read4(residual + n * residual_ld + m, M - m) : u32x2{0, 0};
+    }
+    template <typename T, int KIND>
+    __device__ __forceinline__ f32x4 result(f32x4 z, Column b, Row r, u32x2 &codes) const {
+        f32x4 y;
+        float s[4];
+        each<4>([&](auto i) CFGZIP_INLINE {
+            y[i.value] = act.of<KIND>(z[i.value] + value_at<T>(b, i.value), s[i.value]) + value_at<T>(r, i.value);
+        });
+        codes = u32x2{slope_codes(s[0], s[1]), slope_codes(s[2], s[3])};
+        return y;
+    }
     template <typename T>
-    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z) const {
+    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z, Column b, Row r) const {
         const int32_t left = M - m;
-        u32x2 b = {0, 0}, r = {0, 0};
-        auto read4 = [&](const uint16_t *p) CFGZIP_INLINE {
-            if (left >= 4) return u32x2(*reinterpret_cast<const u32x2_any *>(p));
-            u32x2 v = {0, 0};
-            for (int i = 0; i < left; ++i) v[i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
-            return v;
-        };
-        if (bias) b = read4(bias + m);
-        if (residual) r = read4(residual + n * residual_ld + m);
-        f32x4 y, s;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float slope_i;
-            const float zi = z[i] + T::value((uint16_t)(b[i / 2] >> (i % 2 * 16)));
-            y[i] = act.of(zi, slope_i) + T::value((uint16_t)(r[i / 2] >> (i % 2 * 16)));
-            s[i] = slope_i;
+        f32x4 y;
+        u32x2 codes;
+        act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value>(z, b, r, codes); });
+        if (slope) write4(slope + n * slope_ld + m, codes, left);
+        if (!f32) {
+            write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y), left);
+            return;
         }
-        auto write4 = [&](uint16_t *p, u32x2 v) CFGZIP_INLINE {
-            if (left >= 4) {
-                *reinterpret_cast<u32x2_any *>(p) = v;
-            } else {
-                for (int i = 0; i < left; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
-            }
-        };
-        if (slope)
-            write4(slope + n * slope_ld + m, u32x2{slope_code(s[0]) | slope_code(s[1]) << 16, slope_code(s[2]) | slope_code(s[3]) << 16});
-        if (f32) {
-            float *const p = static_cast<float *>(out) + n * out_ld + m;
-            if (left >= 4) {
-                *reinterpret_cast<f32x4_any *>(p) = y;
-            } else {
-                for (int i = 0; i < left; ++i) p[i] = y[i];
-            }
+        float *const p = static_cast<float *>(out) + n * out_ld + m;
+        if (left >= 4) {
+            *reinterpret_cast<f32x4_any *>(p) = y;
         } else {
-            write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y));
+            for (int i = 0; i < left; ++i) p[i] = y[i];
+        }
+    }
+    // P rows, STEP apart, all of whose four results are there: nothing branches among the results
+    template <typename T, int P, int STEP>
+    __device__ __forceinline__ void store_rows(int32_t n, int32_t m, f32x4 (&z)[P], Column b, const Row (&r)[P]) const {
+        u32x2 codes[P];
+        act.with([&](auto kind) CFGZIP_INLINE {
+            each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value>(z[p.value], b, r[p.value], codes[p.value]); });
+        });
+        if (slope) each<P>([&](auto p) CFGZIP_INLINE { write4(slope + (n + p.value * STEP) * slope_ld + m, codes[p.value], 4); });
+        if (f32) {
+            each<P>([&](auto p) CFGZIP_INLINE {
+                *reinterpret_cast<f32x4_any *>(static_cast<float *>(out) + (n + p.value * STEP) * out_ld + m) = z[p.value];
+            });
+        } else {
+            each<P>([&](auto p) CFGZIP_INLINE {
+                write4(static_cast<uint16_t *>(out) + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value]), 4);
+            });
         }
     }
 };
@@ -126,16 +181,17 @@ struct Gradient {
     int64_t out_ld;
     int32_t M;  // columns
 
+    typedef float Column;
+    struct Row {};
+    __device__ __forceinline__ Column column(int32_t) const { return unscale ? *unscale : 1.0f; }
+    __device__ __forceinline__ Row row(int32_t, int32_t) const { return Row{}; }
     template <typename T>
-    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z) const {
-        if (unscale) z *= *unscale;
-        uint16_t *const p = out + n * out_ld + m;
-        const u32x2 v = round4<T>(z);
-        if (m + 4 <= M) {
-            *reinterpret_cast<u32x2_any *>(p) = v;
-        } else {
-            for (int i = 0; m + i < M; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
-        }
+    __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z, Column back, Row) const {
+        write4(out + n * out_ld + m, round4<T>(z * back), M - m);
+    }
+    template <typename T, int P, int STEP>
+    __device__ __forceinline__ void store_rows(int32_t n, int32_t m, f32x4 (&z)[P], Column back, const Row (&)[P]) const {
+        each<P>([&](auto p) CFGZIP_INLINE { write4(out + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value] * back), 4); });
     }
 };
 
@@ -150,6 +206,39 @@ struct ProductArgs {
     int32_t sums_ld;
 };
 
+// Four of a tile's sums out of accumulation registers, here and not before: the compiler takes all 256 at the tile's end, and has no room for them.
+template <typename S>
+__device__ __forceinline__ f32x4 taken(const f32x4 &acc) {
+    if constexpr (S::kGroup == 4) {
+        f32x4 z;
+        each<4>([&](auto r) CFGZIP_INLINE {
+            const float from = acc[r.value];
+            float to;
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(to) : "a"(from));
+            z[r.value] = to;
+        });
+        return z;
+    }
+    return acc;
+}
+
+// A wave's sums on their way out: 16 rows of 16 FRAGMENTS columns at a time through the part of LDS that the operands' buffers leave, so that
+// a lane has four columns next to its neighbours', of rows that a loop goes through.  (With the epilogue's code written out for every
+// fragment's four results, 64 times in the largest tile, it came from memory for each tile: 40 us a tile whatever the activation, 590 us for
+// 4,096 x 16,384 x 4,096.)  What a chunk asks of memory is asked for ahead of the stores of the one before it: a load waits for all stores before it.
+template <typename S>
+struct Way {
+    static constexpr int FRAGMENTS = S::FM == 8 ? 8 : 2;
+    static constexpr int kGroups = S::FM / FRAGMENTS, kChunks = kGroups * S::FN;
+    static constexpr int kLanes = FRAGMENTS * 4;  // of a row
+    static constexpr int kRows = kWave / kLanes;  // of a pass
+    static constexpr int kPasses = 16 / kRows;
+    static constexpr int kBytes = 16 * kLanes * 16;
+    static_assert(S::FM % FRAGMENTS == 0, "whole chunks");
+    // where unit u (four columns) of row r lies
+    static __device__ __forceinline__ int at(int r, int u) { return r * (kLanes * 16) + ((u ^ (r & 7)) * 16); }
+};
+
 template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool DIRECT, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E end) {
     // (B goes on with zeros to the end of a step, so what A has there only has to be finite; hidden states by columns go on with zeros too: with
@@ -157,6 +246,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
     using TileA = Tile<S::BM, S::kThreads, A_COLUMNS, DIRECT, A_COLUMNS && B_COLUMNS ? PADDED : ANY>;
     using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true, PADDED>;
     CFGZIP_STAGES(S, lds);
+    __shared__ __attribute__((aligned(16))) char way[S::WM * S::WN * Way<S>::kBytes];
     auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
         const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = blockIdx.x + i * gridDim.x;
         if (t >= total) return false;
@@ -175,16 +265,53 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
     auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
         int32_t tm = 0, tn = 0, split = 0;
         place(i, tm, tn, split);
-        each<S::FN>([&](auto j) CFGZIP_INLINE {
-            const int32_t n = tn * S::BN + wn * S::TN + 16 * j.value + (lane & 15);
-            if (n >= a.n) return;
-            each<S::FM>([&](auto i) CFGZIP_INLINE {
-                const int32_t m = tm * S::BM + wm * S::TM + 16 * i.value + 4 * (lane >> 4);
-                if (m >= a.m) return;
-                if (a.sums) *reinterpret_cast<f32x4 *>(a.sums + ((int64_t)split * a.n + n) * a.sums_ld + m) = acc[i.value][j.value];
-                else end.template store<T>(n, m, acc[i.value][j.value]);
+        using W = Way<S>;
+        typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+        lds_char *const mine = (lds_char *)way + (wm * S::WN + wn) * W::kBytes;
+        const int32_t m0 = tm * S::BM + wm * S::TM + lane % W::kLanes * 4, n0 = tn * S::BN + wn * S::TN + lane / W::kLanes;
+        const bool all = (a.m & 3) == 0 && tn * S::BN + wn * S::TN + S::TN <= a.n;
+        typename E::Column column{}, next_column{};
+        typename E::Row row[W::kPasses], next[W::kPasses];
+        auto ask = [&](int32_t chunk) CFGZIP_INLINE {
+            const int32_t m = m0 + chunk / S::FN * (W::FRAGMENTS * 16), n = n0 + chunk % S::FN * 16;
+            if (a.sums || m >= a.m) return;
+            next_column = end.column(m);
+            each<W::kPasses>([&](auto p) CFGZIP_INLINE {
+                if (all || n + p.value * W::kRows < a.n) next[p.value] = end.row(n + p.value * W::kRows, m);
             });
-        });
+        };
+        ask(0);
+#pragma nounroll
+        for (int32_t chunk = 0; chunk < W::kChunks; ++chunk) {
+            each<W::kChunks>([&](auto c) CFGZIP_INLINE {
+                if (chunk == c.value)
+                    each<W::FRAGMENTS>([&](auto i) CFGZIP_INLINE {
+                        *(lds_f32x4 *)(mine + W::at(lane & 15, i.value * 4 + (lane >> 4))) =
+                            taken<S>(acc[c.value / S::FN * W::FRAGMENTS + i.value][c.value % S::FN]);
+                    });
+            });
+            column = next_column;
+            each<W::kPasses>([&](auto p) CFGZIP_INLINE { row[p.value] = next[p.value]; });
+            if (chunk + 1 < W::kChunks) ask(chunk + 1);
+            const int32_t m = m0 + chunk / S::FN * (W::FRAGMENTS * 16), n = n0 + chunk % S::FN * 16;
+            f32x4 z[W::kPasses];
+            each<W::kPasses>([&](auto p) CFGZIP_INLINE {
+                z[p.value] = *(const lds_f32x4 *)(mine + W::at(lane / W::kLanes + p.value * W::kRows, lane % W::kLanes));
+            });
+            if (m >= a.m) continue;
+            if (a.sums) {
+                float *const p0 = a.sums + ((int64_t)split * a.n + n) * a.sums_ld + m;
+                each<W::kPasses>([&](auto p) CFGZIP_INLINE {
+                    if (n + p.value * W::kRows < a.n) *reinterpret_cast<f32x4 *>(p0 + (int64_t)p.value * W::kRows * a.sums_ld) = z[p.value];
+                });
+            } else if (all) {
+                end.template store_rows<T, W::kPasses, W::kRows>(n, m, z, column, row);
+            } else {
+                each<W::kPasses>([&](auto p) CFGZIP_INLINE {
+                    if (n + p.value * W::kRows < a.n) end.template store<T>(n + p.value * W::kRows, m, z[p.value], column, row[p.value]);
+                });
+            }
+        }
     };
     multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
 }
@@ -198,6 +325,8 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_
     const int32_t row = (int32_t)(at / units), c = (int32_t)(at % units) * 4;
     const float *const p = sums + (int64_t)row * sums_ld + c;
     const int64_t step = (int64_t)n * sums_ld;
+    const typename E::Column column = end.column(c);
+    const typename E::Row ahead = end.row(row, c);
     f32x4 x = {0, 0, 0, 0};
     for (int32_t s = 0; s < splits; s += 8) {
         f32x4 y[8];
@@ -206,7 +335,7 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const float *sums, int32_
 #pragma unroll
         for (int i = 0; i < 8; ++i) x += y[i];
     }
-    end.template store<T>(row, c, x);
+    end.template store<T>(row, c, x, column, ahead);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -240,6 +369,9 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a, Forwar
     const int32_t s0 = (int32_t)((int64_t)steps * wave / kFewWaves), s1 = (int32_t)((int64_t)steps * (wave + 1) / kFewWaves);
     const uint16_t *const w = a.w + (m0 + r < a.M ? m0 + r : a.M - 1) * a.w_ld;
     const uint16_t *const x = a.x + (r < a.N ? r : a.N - 1) * a.x_ld;
+    const int32_t m = m0 + 4 * g;
+    u32x2 bias = {0, 0}, residual = {0, 0};
+    if (wave == 0 && r < a.N && m < a.M) bias = end.column(m), residual = end.row(r, m);
     f32x4 acc = {0, 0, 0, 0};
     for (int32_t s = s0; s < s1; s += kFewAhead) {
         u32x4 p[kFewAhead][2], q[kFewAhead][2];
@@ -272,8 +404,7 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a, Forwar
     if (threadIdx.x >= kWave) return;
 #pragma unroll
     for (int i = 1; i < kFewWaves; ++i) acc += shared[i][lane];
-    const int32_t m = m0 + 4 * g;
-    if (r < a.N && m < a.M) end.template store<T>(r, m, acc);
+    if (r < a.N && m < a.M) end.template store<T>(r, m, acc, bias, residual);
 }
 
 // ---------------------------------------------------------------- dz and the gradient of the bias
@@ -658,7 +789,12 @@ extern "C" int cfgzip_head_layer(const void *hidden, int64_t hidden_stride, cons
     if (need && (!ws || !aligned_to(ws, 256) || ws_bytes < need)) return CFGZIP_E_WORKSPACE;
     const double a = 2.0 * 0.79788456080286535588;  // 2 sqrt(2 / pi)
     const bool tanh = activation == CFGZIP_ACT_GELU_TANH;
-    const Activation act{activation, tanh ? (float)a : 1.0f, tanh ? (float)(0.044715 * a) : 0.0f};
+    const Activation act{activation,
+                         activation == CFGZIP_ACT_NONE   ? -__builtin_inff()
+                         : activation == CFGZIP_ACT_RELU ? 0.0f
+                         : tanh                          ? (float)a
+                                                         : 1.0f,
+                         tanh ? (float)(0.044715 * a) : 0.0f};
     const Forward end{static_cast<const uint16_t *>(bias), static_cast<const uint16_t *>(residual), residual_stride, act, out, out_stride, f32,
                       static_cast<uint16_t *>(slope), slope_stride, M};
     Carver carve(ws);
