@@ -30,13 +30,33 @@ constexpr float kNoMore = -200.0f;  // 2^y is 0 from here on
 constexpr int kMaxTop = CFGZIP_MAX_TOP;
 constexpr int kCandidates = 1024;
 constexpr int32_t kMaskWords = 8192;  // of a mask over classes in LDS; larger ones are read where they lie
+// A table of the classes: up to 12,288 of them, 48 KB, where a workgroup has four times as many logits (to make it takes as long as a class's bits).
+constexpr int32_t kTableWords = 384, kTableUse = 4;
 constexpr int32_t kMaxTokens = CFGZIP_MAX_TOKENS, kMaxRows = 1 << 22;  // (a launch has fewer than 2^32 threads)
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
-// where a mask comes from
-enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3 };
+// Where a mask comes from.  CLASS_TABLE: each class a float in LDS, infinity if it is admitted, else -infinity, and a logit masked is the lower of the
+// two: two instructions for the seven of a bit (score of 256 x 128,256 with 8,000 classes TIME_BITS us with bits, TIME_TABLE so).
+enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3, CLASS_TABLE = 4 };
+
+// (As instructions: behind the functions come others that make signalling NaN quiet.)
+__device__ __forceinline__ float lower_of(float a, float b) {
+    float x;
+    asm("v_min_f32 %0, %1, %2" : "=v"(x) : "v"(a), "v"(b));
+    return x;
+}
+__device__ __forceinline__ float larger_of(float a, float b) {
+    float x;
+    asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(a), "v"(b));
+    return x;
+}
+__device__ __forceinline__ float larger_of(float a, float b, float c) {
+    float x;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+    return x;
+}
 
 struct Logits {
     const void *p;
@@ -118,10 +138,27 @@ struct Admitted {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t k = (uint32_t)id[j / 4][j % 4];
-                ok |= (words[k >> 5] >> (k & 31) & 1) << j;
+                if constexpr (MASK == CLASS_TABLE) ok |= (~lds[k] >> 31) << j;
+                else ok |= (words[k >> 5] >> (k & 31) & 1) << j;
             }
         }
         return ok;
+    }
+    // x[j] of the unit where it is admitted, else -infinity
+    template <typename U>
+    __device__ __forceinline__ void values(const U &x, const Logits &l, int64_t row, const uint32_t *lds, float (&v)[8]) const {
+        if constexpr (MASK == CLASS_TABLE) {
+            float limit[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) limit[j] = reinterpret_cast<const float *>(lds)[id[j / 4][j % 4]];
+            each<8>([&](auto j) CFGZIP_INLINE { v[j.value] = lower_of(x.template value<j.value>(), limit[j.value]); });
+        } else {
+            const uint32_t ok = bits(l, row, lds);
+            each<8>([&](auto j) CFGZIP_INLINE {
+                const float z = x.template value<j.value>();
+                v[j.value] = MASK == ALL || (ok >> j.value & 1) ? z : -kInf;
+            });
+        }
     }
 };
 
@@ -130,6 +167,11 @@ template <int MASK>
 __device__ __forceinline__ void mask_to_lds(const Logits &l, int64_t row, uint32_t *lds) {
     if constexpr (MASK == CLASSES) {
         for (int32_t i = threadIdx.x; i < (int32_t)l.words; i += blockDim.x) lds[i] = (uint32_t)l.bits[row * l.words + i];
+        __syncthreads();
+    }
+    if constexpr (MASK == CLASS_TABLE) {  // (pad bits have entries too)
+        for (int32_t i = threadIdx.x; i < (int32_t)l.words * 32; i += blockDim.x)
+            lds[i] = (uint32_t)l.bits[row * l.words + (i >> 5)] >> (i & 31) & 1 ? 0x7F800000u : 0xFF800000u;
         __syncthreads();
     }
 }
@@ -153,25 +195,65 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t place) { return (uint64_t)order_of(x) << 32 | (uint32_t)~place; }
 
-__device__ __forceinline__ uint64_t exchanged(uint64_t key, int distance, bool keep_larger) {
-    const uint64_t other = __shfl_xor((unsigned long long)key, distance);
+// What lane ^ D has, by moves between lanes: one through LDS takes as long as five of them, and a sort has 21 in a row.
+template <int D>
+__device__ __forceinline__ uint32_t across(uint32_t x) {
+    if constexpr (D == 1) return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, false);  // quads 1 0 3 2
+    if constexpr (D == 2) return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, false);  // 2 3 0 1
+    if constexpr (D == 4) {  // the other way round within eight, and again within four
+        const uint32_t y = __builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, false);
+        return __builtin_amdgcn_mov_dpp(y, 0x1B, 0xF, 0xF, false);
+    }
+    if constexpr (D == 8) return __builtin_amdgcn_mov_dpp(x, 0x128, 0xF, 0xF, false);  // rows of 16 turned by 8
+    if constexpr (D == 16) {
+        const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? y[0] : y[1];
+    }
+    if constexpr (D == 32) {
+        const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? y[0] : y[1];
+    }
+}
+template <int D>
+__device__ __forceinline__ float across(float x) {
+    return __builtin_bit_cast(float, across<D>(__builtin_bit_cast(uint32_t, x)));
+}
+template <int D>
+__device__ __forceinline__ uint64_t exchanged(uint64_t key, bool keep_larger) {
+    const uint64_t other = (uint64_t)across<D>((uint32_t)(key >> 32)) << 32 | across<D>((uint32_t)key);
     return (key > other) == keep_larger ? key : other;
+}
+// f(D) for D = FROM, FROM / 2, .. 1
+template <int FROM, typename F>
+__device__ __forceinline__ void halving(F &&f) {
+    f(std::integral_constant<int, FROM>{});
+    if constexpr (FROM > 1) halving<FROM / 2>(f);
 }
 // a wave's 64 keys, the largest first
 __device__ __forceinline__ uint64_t sorted(uint64_t key, int lane) {
-#pragma unroll
-    for (int size = 2; size <= kWave; size *= 2)
-#pragma unroll
-        for (int d = size / 2; d > 0; d /= 2) key = exchanged(key, d, ((lane & d) == 0) == ((lane & size) == 0));
+    each<6>([&](auto s) CFGZIP_INLINE {
+        constexpr int size = 2 << s.value;
+        halving<size / 2>([&](auto d) CFGZIP_INLINE {
+            key = exchanged<d.value>(key, ((lane & d.value) == 0) == ((lane & size) == 0 || size == kWave));
+        });
+    });
     return key;
 }
-// the 64 largest of two sorted lists, sorted
+// the 64 largest of two lists, sorted: a the largest first, b the smallest first
 __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, int lane) {
-    const uint64_t other = __shfl((unsigned long long)b, kWave - 1 - lane);
-    a = a > other ? a : other;
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d /= 2) a = exchanged(a, d, (lane & d) == 0);
+    a = a > b ? a : b;
+    halving<kWave / 2>([&](auto d) CFGZIP_INLINE { a = exchanged<d.value>(a, (lane & d.value) == 0); });
     return a;
+}
+__device__ __forceinline__ uint64_t turned(uint64_t key, int lane) { return __shfl((unsigned long long)key, kWave - 1 - lane); }
+
+__device__ __forceinline__ float largest_of(float x) {
+    halving<kWave / 2>([&](auto d) CFGZIP_INLINE { x = fmaxf(x, across<d.value>(x)); });
+    return x;
+}
+__device__ __forceinline__ float sum_of(float x) {
+    halving<kWave / 2>([&](auto d) CFGZIP_INLINE { x += across<d.value>(x); });
+    return x;
 }
 
 // ---------------------------------------------------------------- forward
@@ -204,8 +286,26 @@ struct ScoreArgs {
     uint64_t *part_keys;  // [N][splits][top]
 };
 
-// What belongs to a row, from its sums and its best keys (lane i of wave 0 has the i-th).  For all threads of a workgroup.
-__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const Sums &sums, uint64_t key) {
+// A given token and its logit, asked for before what they are used with is known: the way there is four loads, one after the other.
+struct Given {
+    int32_t token;
+    float x;  // -inf where it is not admitted, or none
+    __device__ __forceinline__ Given(const ScoreArgs &a, int64_t row, int32_t j = threadIdx.x) : token(-1), x(-kInf) {
+        if (j >= a.n) return;
+        token = a.tokens[row * a.n + j];
+        if (token < 0 || token >= a.l.V) return;
+        const float z = logit_of(a.l, a.dtype, row, token);
+        bool ok = true;
+        if (a.l.bits) {
+            const int32_t k = a.l.class_of_token ? a.l.class_of_token[token] : token;
+            ok = a.l.bits[row * a.l.words + (k >> 5)] >> (k & 31) & 1;
+        }
+        if (ok) x = z;
+    }
+};
+
+// What belongs to a row, from its sums, its best keys (lane i of wave 0 has the i-th) and a thread's given token.  For all threads of a workgroup.
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const Sums &sums, uint64_t key, Given given) {
     const float log_s = __builtin_amdgcn_logf(sums.s);  // log2; -inf where nothing is admitted
     if (threadIdx.x == 0) {
         if (a.stats) a.stats[row] = f32x2_any{sums.s == 0.0f ? -kInf : sums.m, kLn2 * log_s};
@@ -215,18 +315,9 @@ __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const
         }
     }
     for (int32_t j = threadIdx.x; j < a.n; j += blockDim.x) {
-        const int32_t t = a.tokens[row * a.n + j];
-        float out = 0.0f;
-        if (t >= 0 && t < a.l.V) {
-            bool ok = true;
-            if (a.l.bits) {
-                const int32_t k = a.l.class_of_token ? a.l.class_of_token[t] : t;
-                ok = a.l.bits[row * a.l.words + (k >> 5)] >> (k & 31) & 1;
-            }
-            const float x = ok ? logit_of(a.l, a.dtype, row, t) : -kInf;
-            out = x == -kInf ? -kInf : (x - sums.m) * a.per_temperature - kLn2 * log_s;
-        }
-        a.logprob[row * a.n + j] = out;
+        if (j >= (int32_t)blockDim.x) given = Given(a, row, j);
+        const bool none = given.token < 0 || given.token >= a.l.V;
+        a.logprob[row * a.n + j] = none ? 0.0f : given.x == -kInf ? -kInf : (given.x - sums.m) * a.per_temperature - kLn2 * log_s;
     }
     if (threadIdx.x < (uint32_t)a.top) {
         const bool there = key != 0;
@@ -272,14 +363,9 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             if (u + i * kThreads >= u1) break;
-            const uint32_t bits = ok[i].bits(a.l, row, mask);
             float v[8];
-            float here = -kInf;
-            each<8>([&](auto j) CFGZIP_INLINE {
-                const float z = x[i].template value<j.value>();
-                v[j.value] = MASK == ALL || (bits >> j.value & 1) ? z : -kInf;
-                here = fmaxf(here, v[j.value]);
-            });
+            ok[i].values(x[i], a.l, row, mask, v);
+            const float here = larger_of(larger_of(larger_of(v[0], v[1], v[2]), v[3], v[4]), larger_of(v[5], v[6], v[7]));
             if (here > most) {
                 most = here;
                 at = u + i * kThreads;
@@ -288,22 +374,23 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
             each<8>([&](auto j) CFGZIP_INLINE {
                 const float d = v[j.value] - sums.m, e = __builtin_amdgcn_exp2f(d * a.c);
                 sums.s += e;
-                sums.t = __builtin_fmaf(e, fmaxf(d, no_more), sums.t);
+                sums.t = __builtin_fmaf(e, larger_of(d, no_more), sums.t);
             });
         }
     }
 
+    const Given given(a, row, a.splits == 1 ? threadIdx.x : a.n);
     // the workgroup's sums
     if (TOP) keys[threadIdx.x] = most > -kInf ? key_of(most, at) : 0;
     float all = most;
-    for (int d = 1; d < kWave; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+    all = largest_of(all);
     if (lane == 0) shared_most[wave] = all;
     if (threadIdx.x < 2) count[threadIdx.x] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) all = fmaxf(all, shared_most[i]);
     if (all > -kInf) sums.raise(all, a.c);
-    for (int d = 1; d < kWave; d *= 2) sums.s += __shfl_xor(sums.s, d), sums.t += __shfl_xor(sums.t, d);
+    sums.s = sum_of(sums.s), sums.t = sum_of(sums.t);
     if (lane == 0) shared_sums[wave] = sums;
     __syncthreads();
     sums = shared_sums[0];
@@ -356,19 +443,19 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
             if (found <= kCandidates) {
                 for (int32_t i = 0; i < found; i += kWave) {
                     const uint64_t k = sorted(i + lane < found ? candidates[i + lane] : 0, lane);
-                    best = i == 0 ? k : merged(best, k, lane);
+                    best = i == 0 ? k : merged(best, turned(k, lane), lane);
                 }
             } else {  // (rows whose large logits lie in a few threads' units)
                 for (int32_t i = 0; i < items; i += kWave)
                     look_again(i + lane, [&](uint64_t k) CFGZIP_INLINE {
                         const uint64_t least = __shfl((unsigned long long)best, a.top - 1);
-                        if (__builtin_amdgcn_ballot_w64(k > least) != 0) best = merged(best, sorted(k, lane), lane);
+                        if (__builtin_amdgcn_ballot_w64(k > least) != 0) best = merged(best, turned(sorted(k, lane), lane), lane);
                     });
             }
         }
     }
     if (a.splits == 1) {
-        write_row(a, row, sums, best);
+        write_row(a, row, sums, best, given);
         return;
     }
     const int64_t part = row * a.splits + split;
@@ -381,25 +468,35 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a) {
     __shared__ uint64_t lists[kWaves][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t row = blockIdx.x, first = row * a.splits;
+    const Given given(a, row);
     const f32x4 part = lane < a.splits ? a.parts[first + lane] : f32x4{-kInf, 0.0f, 0.0f, 0.0f};
     Sums sums{part[0] > -kInf ? part[0] : 0.0f, part[1], part[2]};
-    float all = part[0];
-    for (int d = 1; d < kWave; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
-    if (all > -kInf) sums.raise(all, a.c);
-    for (int d = 1; d < kWave; d *= 2) sums.s += __shfl_xor(sums.s, d), sums.t += __shfl_xor(sums.t, d);
     uint64_t best = 0;
     if (a.top) {
-        for (int32_t p = wave; p < a.splits; p += kWaves) {
-            const uint64_t k = lane < a.top ? a.part_keys[(first + p) * a.top + lane] : 0;
-            best = p == wave ? k : merged(best, k, lane);
+        // a wave's lists, every second one the smallest first, all on their way before the first is used
+        constexpr int kLists = kWave / kWaves;
+        uint64_t k[kLists];
+        const int back = kWave - 1 - lane;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) {
+            const int32_t p = wave + i * kWaves;
+            const int at = i == 0 ? lane : back;
+            k[i] = p < a.splits && at < a.top ? a.part_keys[(first + p) * a.top + at] : 0;
         }
+        best = k[0];
+#pragma unroll
+        for (int i = 1; i < kLists; ++i)
+            if (wave + i * kWaves < a.splits) best = merged(best, k[i], lane);
         lists[wave][lane] = best;
         for (int half = kWaves / 2; half > 0; half /= 2) {
             __syncthreads();
-            if (wave < half) lists[wave][lane] = best = merged(best, lists[wave + half][lane], lane);
+            if (wave < half) lists[wave][lane] = best = merged(best, lists[wave + half][kWave - 1 - lane], lane);
         }
     }
-    write_row(a, row, sums, best);
+    const float all = largest_of(part[0]);
+    if (all > -kInf) sums.raise(all, a.c);
+    sums.s = sum_of(sums.s), sums.t = sum_of(sums.t);
+    write_row(a, row, sums, best, given);
 }
 
 // ---------------------------------------------------------------- backward
@@ -416,6 +513,7 @@ struct GradArgs {
     void *out;
     int64_t out_ld;
     int32_t splits, per;
+    int32_t mask_words;  // of LDS in front of the given tokens' results
 };
 
 // eight results as they lie
@@ -448,12 +546,12 @@ __device__ __forceinline__ void write_unit(void *out, int64_t at, int32_t left, 
 }
 
 // A workgroup has a piece of a row.  With e = 2^y, y = c (x - m), and S of the row's statistics p is e / S, and a logit's gradient
-// e (A + B y) with constants of the row.  Tokens that are given are marked in LDS, a bit each; a thread that meets one adds up its gradients
-// in their order.  May write where it reads.
+// e (A + B y) with constants of the row.  Given tokens are worked out ahead of the others, their gradients added up in their order, and written
+// behind them: nothing in the loop asks for them.  May write where it reads.
 template <int DTYPE, int MASK>
 __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
     extern __shared__ uint32_t mask[];
-    __shared__ uint32_t marks[kGradUnits / 4];
+    float *const given = reinterpret_cast<float *>(mask + a.mask_words);
     const int lane = threadIdx.x % kWave;
     const int64_t row = blockIdx.x / a.splits;
     const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
@@ -462,22 +560,16 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
     const float *const logprob = a.logprob + row * a.n, *const grads = a.grad_logprob + row * a.n;
     auto grad_of = [&](int32_t j) { return tokens[j] >= 0 && tokens[j] < a.l.V && logprob[j] != -kInf ? grads[j] : 0.0f; };
 
-    for (int32_t i = threadIdx.x; i < kGradUnits / 4; i += kGradThreads) marks[i] = 0;
-    __syncthreads();
     float g = 0.0f;
     bool any = false;
     for (int32_t j = lane; j < a.n; j += kWave) {
         const float x = grad_of(j);
         g += x;
         any |= x != 0.0f;
-        const int32_t v = tokens[j] - u0 * 8;
-        if (x != 0.0f && v >= 0 && v < (u1 - u0) * 8 && threadIdx.x < kWave) atomicOr(&marks[v >> 5], 1u << (v & 31));
     }
-    for (int d = 1; d < kWave; d *= 2) g += __shfl_xor(g, d);
+    g = sum_of(g);
     const float bonus = a.grad_entropy ? a.grad_entropy[row] : 0.0f, m = a.stats[2 * row], log_s = a.stats[2 * row + 1];
-    const bool live = m != -kInf && (__builtin_amdgcn_ballot_w64(any) != 0 || bonus != 0.0f);
-    __syncthreads();
-    if (!live) {
+    if (m == -kInf || (__builtin_amdgcn_ballot_w64(any) == 0 && bonus == 0.0f)) {
         const float zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         for (int32_t u = u0 + threadIdx.x; u < u1; u += kGradThreads)
             write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)u * 8, a.l.V - u * 8, zeros);
@@ -488,6 +580,26 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
     const float scale = -a.per_temperature * __builtin_amdgcn_exp2f(-log_s * kLog2e);
     const float B = bonus != 0.0f ? bonus * kLn2 * scale : 0.0f;
     const float A = (bonus != 0.0f ? g + bonus * (a.entropy[row] - log_s) : g) * scale;
+    auto gradient = [&](float x) {
+        const float y = (x - m) * a.c;
+        return __builtin_amdgcn_exp2f(y) * __builtin_fmaf(B, larger_of(y, kNoMore), A);
+    };
+    // the j-th given token if it lies in the piece and has a gradient of its own
+    auto mine = [&](int32_t j) {
+        const int32_t v = tokens[j] - u0 * 8;
+        return v >= 0 && v < (u1 - u0) * 8 && tokens[j] < a.l.V && logprob[j] != -kInf;
+    };
+    for (int32_t j = threadIdx.x; j < a.n; j += kGradThreads) {
+        if (!mine(j)) continue;
+        const int32_t t = tokens[j];
+        const float x = logit_of(a.l, DTYPE, row, t);
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int32_t q = 0; q < a.n; ++q) sum += tokens[q] == t ? grad_of(q) : 0.0f;
+        given[j] = gradient(x) + sum * a.per_temperature;
+    }
+    if (a.n) __syncthreads();  // given tokens' logits have been read
+
     constexpr int kUnits = kAhead<DTYPE>;
     for (int32_t u = u0 + threadIdx.x; u < u1; u += kGradThreads * kUnits) {
         Unit<DTYPE> x[kUnits];
@@ -506,24 +618,20 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
             const uint32_t bits = ok[i].bits(a.l, row, mask);
             float d[8];
             each<8>([&](auto j) CFGZIP_INLINE {
-                const float z = x[i].template value<j.value>();
-                const float y = (z - m) * a.c;
-                const float f = __builtin_amdgcn_exp2f(y) * __builtin_fmaf(B, fmaxf(y, kNoMore), A);
+                const float f = gradient(x[i].template value<j.value>());
                 d[j.value] = MASK == ALL || (bits >> j.value & 1) ? f : 0.0f;
             });
-            const uint32_t marked = marks[(unit - u0) >> 2] >> ((unit - u0) & 3) * 8 & 255;
-            if (marked) {
-                each<8>([&](auto j) CFGZIP_INLINE {
-                    if (marked >> j.value & 1) {
-                        float sum = 0.0f;
-                        for (int32_t q = 0; q < a.n; ++q)
-                            if (tokens[q] == unit * 8 + j.value) sum += grad_of(q);
-                        d[j.value] += sum * a.per_temperature;
-                    }
-                });
-            }
             write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)unit * 8, a.l.V - unit * 8, d);
         }
+    }
+    if (!a.n) return;
+    __syncthreads();  // the others are written
+    for (int32_t j = threadIdx.x; j < a.n; j += kGradThreads) {
+        if (!mine(j)) continue;
+        if constexpr (DTYPE == CFGZIP_DTYPE_F32) static_cast<float *>(a.out)[row * a.out_ld + tokens[j]] = given[j];
+        else
+            static_cast<uint16_t *>(a.out)[row * a.out_ld + tokens[j]] =
+                std::conditional_t<DTYPE == CFGZIP_DTYPE_BF16, Bf16, Fp16>::round(given[j]);
     }
 }
 
@@ -588,6 +696,7 @@ int with(int32_t dtype, int mask, F &&f) {
             case ALL: return f(type, std::integral_constant<int, ALL>{});
             case TOKENS: return f(type, std::integral_constant<int, TOKENS>{});
             case CLASSES: return f(type, std::integral_constant<int, CLASSES>{});
+            case CLASS_TABLE: return f(type, std::integral_constant<int, CLASS_TABLE>{});
             default: return f(type, std::integral_constant<int, CLASSES_FAR>{});
         }
     };
@@ -639,8 +748,9 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
         a.part_keys = carve.take<uint64_t>((size_t)N * a.splits * top);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int mask = mask_of(c);
-    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : 0;
+    int mask = mask_of(c);
+    if (mask == CLASSES && a.l.words <= kTableWords && (int64_t)a.per * 8 >= (int64_t)kTableUse * C) mask = CLASS_TABLE;
+    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : mask == CLASS_TABLE ? (uint32_t)a.l.words * 128 : 0;
     CFGZIP_TRY(with(dtype, mask, [&](auto type, auto kind) {
         const dim3 grid((uint32_t)N * a.splits);
         if (top) hipLaunchKernelGGL((score_kernel<type.value, kind.value, true>), grid, dim3(kThreads), lds, s, a);
@@ -677,9 +787,11 @@ extern "C" int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int
     if ((int64_t)N * a.splits > 0xFFFFFFFF / kGradThreads) return CFGZIP_E_TOO_LARGE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int mask = mask_of(c);
-    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : 0;
+    a.mask_words = mask == CLASSES ? (int32_t)a.l.words : 0;
+    const uint32_t lds = ((uint32_t)a.mask_words + n) * 4;
     return with(dtype, mask, [&](auto type, auto kind) {
-        hipLaunchKernelGGL((grad_kernel<type.value, kind.value>), dim3((uint32_t)N * a.splits), dim3(kGradThreads), lds, s, a);
+        constexpr int kMask = kind.value == CLASS_TABLE ? CLASSES : kind.value;  // (of a piece a table is more to make than to use)
+        hipLaunchKernelGGL((grad_kernel<type.value, kMask>), dim3((uint32_t)N * a.splits), dim3(kGradThreads), lds, s, a);
         return check_launch();
     });
 }
