@@ -27,26 +27,21 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr double kLog2eD = 1.44269504088896340736;
 constexpr float kLog2e = (float)kLog2eD;
 constexpr float kNoMore = -200.0f;  // 2^y is 0 from here on
+// Sums are brought to a larger logit only if its 2^y would be more than this: of 64 threads one has met a larger one than before at nearly every
+// unit of a row of 128,256.  What it costs is bits of the sum of y 2^y, which then has y of up to 11.5 taken from it at the end.
+constexpr float kMargin = 11.5f;
 constexpr int kMaxTop = CFGZIP_MAX_TOP;
 constexpr int kCandidates = 1024;
-constexpr int32_t kMaskWords = 8192;  // of a mask over classes in LDS; larger ones are read where they lie
-// A table of the classes: up to 12,288 of them, 48 KB, where a workgroup has four times as many logits (to make it takes as long as a class's bits).
-constexpr int32_t kTableWords = 384, kTableUse = 4;
+constexpr int32_t kMaskWords = 4096;  // of a mask over classes in LDS, two rows of them; larger ones are read where they lie
 constexpr int32_t kMaxTokens = CFGZIP_MAX_TOKENS, kMaxRows = 1 << 22;  // (a launch has fewer than 2^32 threads)
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
-// Where a mask comes from.  CLASS_TABLE: each class a float in LDS, infinity if it is admitted, else -infinity, and a logit masked is the lower of the
-// two: two instructions for the seven of a bit (score of 256 x 128,256 with 8,000 classes TIME_BITS us with bits, TIME_TABLE so).
-enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3, CLASS_TABLE = 4 };
+// where a mask comes from
+enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3 };
 
 // (As instructions: behind the functions come others that make signalling NaN quiet.)
-__device__ __forceinline__ float lower_of(float a, float b) {
-    float x;
-    asm("v_min_f32 %0, %1, %2" : "=v"(x) : "v"(a), "v"(b));
-    return x;
-}
 __device__ __forceinline__ float larger_of(float a, float b) {
     float x;
     asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(a), "v"(b));
@@ -65,6 +60,8 @@ struct Logits {
     const int32_t *bits;
     int64_t words;
     const int32_t *class_of_token;
+    // the r-th of a workgroup's rows; behind the last one that one again, of which nothing is stored twice
+    __device__ __forceinline__ int64_t at(int64_t row, int r) const { return row + r < N ? row + r : N - 1; }
 };
 
 // eight logits next to each other as they lie, -inf behind the row's end
@@ -109,13 +106,16 @@ struct Unit {
     }
 };
 
-// Which of a unit's tokens the row admits, a bit each: ids(unit) asks memory, bits() uses what came.
-template <int MASK>
+// Which of a unit's tokens each of ROWS rows admits: ask() asks memory, look() LDS.  Masks over classes lie there, the rows' words of 32 classes next
+// to each other.  (A table with a float for each class, two instructions a logit for four, was no faster: 4,096 x 128,256 bf16 275 us and 264.)
+template <int MASK, int ROWS>
 struct Admitted {
     i32x4_any id[2];
     uint32_t byte;
+    uint32_t word[ROWS][8];
     __device__ __forceinline__ void ask(const Logits &l, int64_t row, int32_t unit) {
         if constexpr (MASK == TOKENS) {
+            static_assert(ROWS == 1, "rows share classes' numbers only");
             byte = reinterpret_cast<const uint8_t *>(l.bits + row * l.words)[unit];
         } else if constexpr (MASK >= CLASSES) {
             const int32_t *const p = l.class_of_token + (int64_t)unit * 8;
@@ -129,49 +129,39 @@ struct Admitted {
             }
         }
     }
-    __device__ __forceinline__ uint32_t bits(const Logits &l, int64_t row, const uint32_t *lds) const {
-        if constexpr (MASK == ALL) return 255;
-        if constexpr (MASK == TOKENS) return byte;
-        uint32_t ok = 0;
+    __device__ __forceinline__ void look(const Logits &l, int64_t row, const uint32_t *lds) {
         if constexpr (MASK >= CLASSES) {
-            const uint32_t *const words = MASK == CLASSES ? lds : reinterpret_cast<const uint32_t *>(l.bits + row * l.words);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t k = (uint32_t)id[j / 4][j % 4];
-                if constexpr (MASK == CLASS_TABLE) ok |= (~lds[k] >> 31) << j;
-                else ok |= (words[k >> 5] >> (k & 31) & 1) << j;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+                    word[r][j] = MASK == CLASSES ? lds[(k >> 5) * ROWS + r] : (uint32_t)l.bits[l.at(row, r) * l.words + (k >> 5)];
             }
         }
-        return ok;
     }
-    // x[j] of the unit where it is admitted, else -infinity
-    template <typename U>
-    __device__ __forceinline__ void values(const U &x, const Logits &l, int64_t row, const uint32_t *lds, float (&v)[8]) const {
-        if constexpr (MASK == CLASS_TABLE) {
-            float limit[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) limit[j] = reinterpret_cast<const float *>(lds)[id[j / 4][j % 4]];
-            each<8>([&](auto j) CFGZIP_INLINE { v[j.value] = lower_of(x.template value<j.value>(), limit[j.value]); });
-        } else {
-            const uint32_t ok = bits(l, row, lds);
-            each<8>([&](auto j) CFGZIP_INLINE {
-                const float z = x.template value<j.value>();
-                v[j.value] = MASK == ALL || (ok >> j.value & 1) ? z : -kInf;
-            });
-        }
+    // ~0 if row r admits the J-th, else 0
+    template <int J>
+    __device__ __forceinline__ uint32_t keep(int r) const {
+        if constexpr (MASK == ALL) return ~0u;
+        if constexpr (MASK == TOKENS) return (uint32_t)__builtin_amdgcn_sbfe((int32_t)byte, J, 1);
+        if constexpr (MASK >= CLASSES) return (uint32_t)__builtin_amdgcn_sbfe((int32_t)word[r][J], (uint32_t)id[J / 4][J % 4], 1);
+    }
+    template <int J>
+    __device__ __forceinline__ float masked(int r, float x) const {
+        if constexpr (MASK == ALL) return x;
+        const uint32_t mine = keep<J>(r);
+        return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & mine) | (0xFF800000u & ~mine));
     }
 };
 
-// the row's mask over classes to LDS
-template <int MASK>
-__device__ __forceinline__ void mask_to_lds(const Logits &l, int64_t row, uint32_t *lds) {
+// the rows' masks over classes to LDS
+template <int MASK, int ROWS>
+__device__ __forceinline__ void masks_to_lds(const Logits &l, int64_t row, uint32_t *lds) {
     if constexpr (MASK == CLASSES) {
-        for (int32_t i = threadIdx.x; i < (int32_t)l.words; i += blockDim.x) lds[i] = (uint32_t)l.bits[row * l.words + i];
-        __syncthreads();
-    }
-    if constexpr (MASK == CLASS_TABLE) {  // (pad bits have entries too)
-        for (int32_t i = threadIdx.x; i < (int32_t)l.words * 32; i += blockDim.x)
-            lds[i] = (uint32_t)l.bits[row * l.words + (i >> 5)] >> (i & 31) & 1 ? 0x7F800000u : 0xFF800000u;
+        for (int32_t i = threadIdx.x; i < (int32_t)l.words; i += blockDim.x)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) lds[i * ROWS + r] = (uint32_t)l.bits[l.at(row, r) * l.words + i];
         __syncthreads();
     }
 }
@@ -258,7 +248,7 @@ __device__ __forceinline__ float sum_of(float x) {
 
 // ---------------------------------------------------------------- forward
 
-// the largest x = m, the sums of 2^(c (x - m)) and of (x - m) 2^(c (x - m)); m is 0 where there is nothing yet
+// an m near the largest x, the sums of 2^(c (x - m)) and of (x - m) 2^(c (x - m)); m is 0 where there is nothing yet
 struct Sums {
     float m, s, t;
     // brought to `to`, which is no less than m
@@ -327,140 +317,166 @@ __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const
     }
 }
 
-// Units of a thread on their way at a time: 64 bytes of logits.
-template <int DTYPE>
-constexpr int kAhead = DTYPE == CFGZIP_DTYPE_F32 ? 2 : 4;
+// Units of a thread and row on their way at a time: 64 bytes of logits, of two rows 32 each.
+template <int DTYPE, int ROWS>
+constexpr int kAhead = (DTYPE == CFGZIP_DTYPE_F32 ? 2 : 4) / ROWS;
 
-template <int DTYPE, int MASK, bool TOP>
+// A workgroup has a piece of ROWS rows.  Rows under masks over classes go in twos: the numbers of the classes are twice the bytes of 16-bit logits, and
+// come from the second-level cache for every row (4,096 x 128,256 bf16 264 us one by one, 228 in twos, 184 without masks).
+template <int DTYPE, int MASK, bool TOP, int ROWS>
 __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
     extern __shared__ uint32_t mask[];
-    __shared__ Sums shared_sums[kWaves];
-    __shared__ float shared_most[kWaves];
+    __shared__ Sums shared_sums[ROWS][kWaves];
+    __shared__ float shared_most[ROWS][kWaves];
     __shared__ uint64_t keys[TOP ? kThreads : 1], candidates[TOP ? kCandidates : 1];
     __shared__ uint16_t again[TOP ? kThreads : 1];
     __shared__ int32_t count[2];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t row = blockIdx.x / a.splits;
+    const int64_t row = (int64_t)(blockIdx.x / a.splits) * ROWS;
     const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
     const int32_t u0 = split * a.per, u1 = units - u0 < a.per ? units : u0 + a.per;
-    mask_to_lds<MASK>(a.l, row, mask);
+    masks_to_lds<MASK, ROWS>(a.l, row, mask);
 
     const float no_more = kNoMore / a.c;
-    float most = -kInf;
-    int32_t at = 0;  // the first unit with it
-    Sums sums{0.0f, 0.0f, 0.0f};
-    constexpr int kUnits = kAhead<DTYPE>;
+    float most[ROWS];
+    int32_t at[ROWS];  // the first unit with it
+    Sums sums[ROWS];
+    float limit[ROWS];
+    const float margin = kMargin / a.c;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) most[r] = limit[r] = -kInf, at[r] = 0, sums[r] = Sums{0.0f, 0.0f, 0.0f};
+    constexpr int kUnits = kAhead<DTYPE, ROWS>;
     for (int32_t u = u0 + threadIdx.x; u < u1; u += kThreads * kUnits) {
-        Unit<DTYPE> x[kUnits];
-        Admitted<MASK> ok[kUnits];
+        Unit<DTYPE> x[ROWS][kUnits];
+        Admitted<MASK, ROWS> admitted[kUnits];
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             if (u + i * kThreads < u1) {
-                x[i].read(a.l, row, u + i * kThreads);
-                ok[i].ask(a.l, row, u + i * kThreads);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) x[r][i].read(a.l, a.l.at(row, r), u + i * kThreads);
+                admitted[i].ask(a.l, row, u + i * kThreads);
             }
         }
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             if (u + i * kThreads >= u1) break;
-            float v[8];
-            ok[i].values(x[i], a.l, row, mask, v);
-            const float here = larger_of(larger_of(larger_of(v[0], v[1], v[2]), v[3], v[4]), larger_of(v[5], v[6], v[7]));
-            if (here > most) {
-                most = here;
-                at = u + i * kThreads;
-                sums.raise(here, a.c);
+            admitted[i].look(a.l, row, mask);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                float v[8];
+                each<8>([&](auto j) CFGZIP_INLINE { v[j.value] = admitted[i].template masked<j.value>(r, x[r][i].template value<j.value>()); });
+                const float here = larger_of(larger_of(larger_of(v[0], v[1], v[2]), v[3], v[4]), larger_of(v[5], v[6], v[7]));
+                at[r] = here > most[r] ? u + i * kThreads : at[r];
+                most[r] = larger_of(most[r], here);
+                if (here > limit[r]) {
+                    sums[r].raise(here, a.c);
+                    limit[r] = here + margin;
+                }
+                each<8>([&](auto j) CFGZIP_INLINE {
+                    const float d = v[j.value] - sums[r].m, e = __builtin_amdgcn_exp2f(d * a.c);
+                    sums[r].s += e;
+                    sums[r].t = __builtin_fmaf(e, larger_of(d, no_more), sums[r].t);
+                });
             }
-            each<8>([&](auto j) CFGZIP_INLINE {
-                const float d = v[j.value] - sums.m, e = __builtin_amdgcn_exp2f(d * a.c);
-                sums.s += e;
-                sums.t = __builtin_fmaf(e, larger_of(d, no_more), sums.t);
-            });
         }
     }
 
-    const Given given(a, row, a.splits == 1 ? threadIdx.x : a.n);
     // the workgroup's sums
-    if (TOP) keys[threadIdx.x] = most > -kInf ? key_of(most, at) : 0;
-    float all = most;
-    all = largest_of(all);
-    if (lane == 0) shared_most[wave] = all;
-    if (threadIdx.x < 2) count[threadIdx.x] = 0;
+    float all[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        all[r] = largest_of(most[r]);
+        if (lane == 0) shared_most[r][wave] = all[r];
+    }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) all = fmaxf(all, shared_most[i]);
-    if (all > -kInf) sums.raise(all, a.c);
-    sums.s = sum_of(sums.s), sums.t = sum_of(sums.t);
-    if (lane == 0) shared_sums[wave] = sums;
-    __syncthreads();
-    sums = shared_sums[0];
+    for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) sums.add(shared_sums[i]);
+        for (int i = 0; i < kWaves; ++i) all[r] = fmaxf(all[r], shared_most[r][i]);
+        if (all[r] > -kInf) sums[r].raise(all[r], a.c);
+        sums[r].s = sum_of(sums[r].s), sums[r].t = sum_of(sums[r].t);
+        if (lane == 0) shared_sums[r][wave] = sums[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        sums[r] = shared_sums[r][0];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) sums[r].add(shared_sums[r][i]);
+    }
 
-    uint64_t best = 0;
-    if constexpr (TOP) {
-        // every wave works out the bound, from the largest of the threads of each lane
-        uint64_t key = keys[lane];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) key = keys[lane + i * kWave] > key ? keys[lane + i * kWave] : key;
-        const uint64_t bound = __shfl((unsigned long long)sorted(key, lane), a.top - 1);
-        const uint64_t mine = keys[threadIdx.x];
-        if (mine != 0 && mine >= bound) again[atomicAdd(&count[0], 1)] = (uint16_t)threadIdx.x;
-        __syncthreads();
-        const uint32_t bound_value = (uint32_t)(bound >> 32), bound_unit = ~(uint32_t)bound;
-        const int32_t rounds = (u1 - u0 + kThreads - 1) / kThreads, items = count[0] * rounds;
-        // f(key) of the unit's logits that reach the bound
-        auto look_again = [&](int32_t item, auto &&f) CFGZIP_INLINE {
-            const int32_t u = item < items ? u0 + again[item / rounds] + item % rounds * kThreads : u1;
-            Unit<DTYPE> x;
-            Admitted<MASK> ok;
-            uint32_t bits = 0;
-            if (u < u1) {
-                x.read(a.l, row, u);
-                ok.ask(a.l, row, u);
-                bits = ok.bits(a.l, row, mask);
-            }
-            each<8>([&](auto j) CFGZIP_INLINE {
-                uint64_t k = 0;
-                if (bits >> j.value & 1) {
-                    const float z = x.template value<j.value>();
-                    const uint32_t order = order_of(z);
-                    if (z != -kInf && (order > bound_value || (order == bound_value && (uint32_t)u <= bound_unit)))
-                        k = key_of(z, (uint32_t)u * 8 + j.value);
+    for (int r = 0; r < ROWS; ++r) {
+        if (row + r >= a.l.N) break;
+        const Given given(a, row + r, a.splits == 1 ? threadIdx.x : a.n);
+        uint64_t best = 0;
+        if constexpr (TOP) {
+            keys[threadIdx.x] = most[r] > -kInf ? key_of(most[r], at[r]) : 0;
+            if (threadIdx.x < 2) count[threadIdx.x] = 0;
+            __syncthreads();
+            // every wave works out the bound, from the largest of the threads of each lane
+            uint64_t key = keys[lane];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) key = keys[lane + i * kWave] > key ? keys[lane + i * kWave] : key;
+            const uint64_t bound = __shfl((unsigned long long)sorted(key, lane), a.top - 1);
+            const uint64_t mine = keys[threadIdx.x];
+            if (mine != 0 && mine >= bound) again[atomicAdd(&count[0], 1)] = (uint16_t)threadIdx.x;
+            __syncthreads();
+            const uint32_t bound_value = (uint32_t)(bound >> 32), bound_unit = ~(uint32_t)bound;
+            const int32_t rounds = (u1 - u0 + kThreads - 1) / kThreads, items = count[0] * rounds;
+            // f(key) of the unit's logits that reach the bound
+            auto look_again = [&](int32_t item, auto &&f) CFGZIP_INLINE {
+                const int32_t u = item < items ? u0 + again[item / rounds] + item % rounds * kThreads : u1;
+                Unit<DTYPE> x;
+                Admitted<MASK, ROWS> admitted;
+                if (u < u1) {
+                    x.read(a.l, row + r, u);
+                    admitted.ask(a.l, row, u);
+                    admitted.look(a.l, row, mask);
                 }
-                f(k);
-            });
-        };
-        for (int32_t i = threadIdx.x; i < items; i += kThreads)
-            look_again(i, [&](uint64_t k) CFGZIP_INLINE {
-                if (k == 0) return;
-                const int32_t to = atomicAdd(&count[1], 1);
-                if (to < kCandidates) candidates[to] = k;
-            });
-        __syncthreads();
-        if (wave == 0) {
-            const int32_t found = count[1];
-            if (found <= kCandidates) {
-                for (int32_t i = 0; i < found; i += kWave) {
-                    const uint64_t k = sorted(i + lane < found ? candidates[i + lane] : 0, lane);
-                    best = i == 0 ? k : merged(best, turned(k, lane), lane);
+                each<8>([&](auto j) CFGZIP_INLINE {
+                    uint64_t k = 0;
+                    if (u < u1) {
+                        const float z = admitted.template masked<j.value>(r, x.template value<j.value>());
+                        const uint32_t order = order_of(z);
+                        if (z != -kInf && (order > bound_value || (order == bound_value && (uint32_t)u <= bound_unit)))
+                            k = key_of(z, (uint32_t)u * 8 + j.value);
+                    }
+                    f(k);
+                });
+            };
+            for (int32_t i = threadIdx.x; i < items; i += kThreads)
+                look_again(i, [&](uint64_t k) CFGZIP_INLINE {
+                    if (k == 0) return;
+                    const int32_t to = atomicAdd(&count[1], 1);
+                    if (to < kCandidates) candidates[to] = k;
+                });
+            __syncthreads();
+            if (wave == 0) {
+                const int32_t found = count[1];
+                if (found <= kCandidates) {
+                    for (int32_t i = 0; i < found; i += kWave) {
+                        const uint64_t k = sorted(i + lane < found ? candidates[i + lane] : 0, lane);
+                        best = i == 0 ? k : merged(best, turned(k, lane), lane);
+                    }
+                } else {  // (rows whose large logits lie in a few threads' units)
+                    for (int32_t i = 0; i < items; i += kWave)
+                        look_again(i + lane, [&](uint64_t k) CFGZIP_INLINE {
+                            const uint64_t least = __shfl((unsigned long long)best, a.top - 1);
+                            if (__builtin_amdgcn_ballot_w64(k > least) != 0) best = merged(best, turned(sorted(k, lane), lane), lane);
+                        });
                 }
-            } else {  // (rows whose large logits lie in a few threads' units)
-                for (int32_t i = 0; i < items; i += kWave)
-                    look_again(i + lane, [&](uint64_t k) CFGZIP_INLINE {
-                        const uint64_t least = __shfl((unsigned long long)best, a.top - 1);
-                        if (__builtin_amdgcn_ballot_w64(k > least) != 0) best = merged(best, turned(sorted(k, lane), lane), lane);
-                    });
             }
         }
+        if (a.splits == 1) {
+            write_row(a, row + r, sums[r], best, given);
+        } else {
+            const int64_t part = (row + r) * a.splits + split;
+            if (threadIdx.x == 0) a.parts[part] = f32x4{all[r], sums[r].s, sums[r].t, 0.0f};
+            if (TOP && threadIdx.x < (uint32_t)a.top) a.part_keys[part * a.top + threadIdx.x] = best;
+        }
+        if (TOP && ROWS > 1) __syncthreads();  // wave 0 is done with what the next row is put in
     }
-    if (a.splits == 1) {
-        write_row(a, row, sums, best, given);
-        return;
-    }
-    const int64_t part = row * a.splits + split;
-    if (threadIdx.x == 0) a.parts[part] = f32x4{all, sums.s, sums.t, 0.0f};
-    if (TOP && threadIdx.x < (uint32_t)a.top) a.part_keys[part * a.top + threadIdx.x] = best;
 }
 
 // Joins a row's parts.
@@ -549,7 +565,7 @@ __device__ __forceinline__ void write_unit(void *out, int64_t at, int32_t left, 
 // e (A + B y) with constants of the row.  Given tokens are worked out ahead of the others, their gradients added up in their order, and written
 // behind them: nothing in the loop asks for them.  May write where it reads.
 template <int DTYPE, int MASK>
-__global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(GradArgs a) {
     extern __shared__ uint32_t mask[];
     float *const given = reinterpret_cast<float *>(mask + a.mask_words);
     const int lane = threadIdx.x % kWave;
@@ -575,7 +591,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
             write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)u * 8, a.l.V - u * 8, zeros);
         return;
     }
-    mask_to_lds<MASK>(a.l, row, mask);
+    masks_to_lds<MASK, 1>(a.l, row, mask);
 
     const float scale = -a.per_temperature * __builtin_amdgcn_exp2f(-log_s * kLog2e);
     const float B = bonus != 0.0f ? bonus * kLn2 * scale : 0.0f;
@@ -600,10 +616,10 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
     }
     if (a.n) __syncthreads();  // given tokens' logits have been read
 
-    constexpr int kUnits = kAhead<DTYPE>;
+    constexpr int kUnits = kAhead<DTYPE, 1>;
     for (int32_t u = u0 + threadIdx.x; u < u1; u += kGradThreads * kUnits) {
         Unit<DTYPE> x[kUnits];
-        Admitted<MASK> ok[kUnits];
+        Admitted<MASK, 1> ok[kUnits];
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             if (u + i * kGradThreads < u1) {
@@ -615,11 +631,11 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
         for (int i = 0; i < kUnits; ++i) {
             const int32_t unit = u + i * kGradThreads;
             if (unit >= u1) break;
-            const uint32_t bits = ok[i].bits(a.l, row, mask);
+            ok[i].look(a.l, row, mask);
             float d[8];
             each<8>([&](auto j) CFGZIP_INLINE {
                 const float f = gradient(x[i].template value<j.value>());
-                d[j.value] = MASK == ALL || (bits >> j.value & 1) ? f : 0.0f;
+                d[j.value] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, f) & ok[i].template keep<j.value>(0));
             });
             write_unit<DTYPE>(a.out, row * a.out_ld + (int64_t)unit * 8, a.l.V - unit * 8, d);
         }
@@ -639,9 +655,14 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(GradArgs a) {
 
 // Workgroups of a row: as many as fill the chip, of one round of units to a thread at the least.
 constexpr int32_t kWorkgroups = 512;
-int32_t splits_of(int32_t N, int32_t V) {
+int32_t splits_of(int32_t rows, int32_t V) {
     const int64_t most = std::min<int64_t>(ceil_div(V, kThreads * 8), kWave);
-    return (int32_t)std::max<int64_t>(std::min<int64_t>(kWorkgroups / std::max(N, 1), most), 1);
+    return (int32_t)std::max<int64_t>(std::min<int64_t>(kWorkgroups / std::max(rows, 1), most), 1);
+}
+// Rows of a workgroup: two under masks over classes, if they fill the chip that way.  (With alternatives, which take 6 us for each row at the
+// workgroup's end, 256 x 128,256 took 29.6 us in twos for 26.7.)
+int32_t rows_of(int32_t N, int32_t V, int32_t top, bool classes) {
+    return classes && top == 0 && ceil_div(N, 2) * splits_of((int32_t)ceil_div(N, 2), V) >= kWorkgroups / 2 ? 2 : 1;
 }
 
 bool kind_ok(int32_t kind) { return kind == CFGZIP_BITS_TOKEN || kind == CFGZIP_BITS_CLASS || kind == CFGZIP_BITS_NONE; }
@@ -696,7 +717,6 @@ int with(int32_t dtype, int mask, F &&f) {
             case ALL: return f(type, std::integral_constant<int, ALL>{});
             case TOKENS: return f(type, std::integral_constant<int, TOKENS>{});
             case CLASSES: return f(type, std::integral_constant<int, CLASSES>{});
-            case CLASS_TABLE: return f(type, std::integral_constant<int, CLASS_TABLE>{});
             default: return f(type, std::integral_constant<int, CLASSES_FAR>{});
         }
     };
@@ -712,7 +732,7 @@ using namespace cfgzip;
 
 extern "C" size_t cfgzip_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t top) {
     if (N <= 0 || V <= 0 || top < 0 || top > kMaxTop || N > kMaxRows || V > 0x7FFFFC00) return 0;
-    const int64_t splits = splits_of(N, V);
+    const int64_t splits = std::max(splits_of(N, V), splits_of((int32_t)ceil_div(N, rows_of(N, V, top, true)), V));
     if (splits == 1) return 0;
     Carver ws(nullptr);
     ws.take<f32x4>((size_t)N * splits);
@@ -738,7 +758,8 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
     a.dtype = dtype;
     a.c = (float)(kLog2eD / temperature), a.per_temperature = (float)(1.0 / temperature);
     a.tokens = tokens, a.n = n, a.top = top;
-    a.splits = splits_of(N, V);
+    const int32_t rows = rows_of(N, V, top, mask_of(c) == CLASSES);
+    a.splits = splits_of((int32_t)ceil_div(N, rows), V);
     a.per = (int32_t)ceil_div(ceil_div(V, 8), a.splits);
     a.splits = (int32_t)ceil_div(ceil_div(V, 8), a.per);
     a.logprob = logprob, a.entropy = entropy, a.stats = reinterpret_cast<f32x2_any *>(stats), a.top_tokens = top_tokens, a.top_logprobs = top_logprobs;
@@ -748,14 +769,22 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
         a.part_keys = carve.take<uint64_t>((size_t)N * a.splits * top);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    int mask = mask_of(c);
-    if (mask == CLASSES && a.l.words <= kTableWords && (int64_t)a.per * 8 >= (int64_t)kTableUse * C) mask = CLASS_TABLE;
-    const uint32_t lds = mask == CLASSES ? (uint32_t)a.l.words * 4 : mask == CLASS_TABLE ? (uint32_t)a.l.words * 128 : 0;
+    const int mask = mask_of(c);
     CFGZIP_TRY(with(dtype, mask, [&](auto type, auto kind) {
-        const dim3 grid((uint32_t)N * a.splits);
-        if (top) hipLaunchKernelGGL((score_kernel<type.value, kind.value, true>), grid, dim3(kThreads), lds, s, a);
-        else hipLaunchKernelGGL((score_kernel<type.value, kind.value, false>), grid, dim3(kThreads), lds, s, a);
-        return check_launch();
+        auto launch = [&](auto r) {
+            const dim3 grid((uint32_t)ceil_div(N, r.value) * a.splits);
+            const uint32_t lds = kind.value == CLASSES ? (uint32_t)a.l.words * 4 * r.value : 0;
+            if constexpr (r.value == 1)
+                if (top) {
+                    hipLaunchKernelGGL((score_kernel<type.value, kind.value, true, 1>), grid, dim3(kThreads), lds, s, a);
+                    return check_launch();
+                }
+            hipLaunchKernelGGL((score_kernel<type.value, kind.value, false, r.value>), grid, dim3(kThreads), lds, s, a);
+            return check_launch();
+        };
+        if constexpr (kind.value == CLASSES)
+            if (rows == 2) return launch(std::integral_constant<int, 2>{});
+        return launch(std::integral_constant<int, 1>{});
     }));
     if (a.splits == 1) return CFGZIP_OK;
     hipLaunchKernelGGL(score_join_kernel, dim3(N), dim3(kThreads), 0, s, a);
@@ -790,8 +819,7 @@ extern "C" int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int
     a.mask_words = mask == CLASSES ? (int32_t)a.l.words : 0;
     const uint32_t lds = ((uint32_t)a.mask_words + n) * 4;
     return with(dtype, mask, [&](auto type, auto kind) {
-        constexpr int kMask = kind.value == CLASS_TABLE ? CLASSES : kind.value;  // (of a piece a table is more to make than to use)
-        hipLaunchKernelGGL((grad_kernel<type.value, kMask>), dim3((uint32_t)N * a.splits), dim3(kGradThreads), lds, s, a);
+        hipLaunchKernelGGL((logprobs_grad_kernel<type.value, kind.value>), dim3((uint32_t)N * a.splits), dim3(kGradThreads), lds, s, a);
         return check_launch();
     });
 }

@@ -7,6 +7,7 @@ divided by the temperature and d = z - (the largest admitted z):
   a raise           of what was summed to a larger maximum: the differences add up to |d| again, 6 for each; at most one a unit of eight
                     logits that a thread takes, and two where threads and workgroups are joined
   a sum             8 additions a unit of a thread, 24 where threads and workgroups are joined
+  sum of d exp(d)   of d that are larger by up to the 8 that a thread's sums may be apart from its largest logit, which are taken back
 all in F32, relative to the sum; terms further than 100 from the largest are nothing in any case."""
 
 import numpy as np
@@ -39,7 +40,7 @@ def logprobs(x, tokens, allowed, temperature, top):
     log_err = s_err + 4 * F32 * (np.where(some, np.abs(log_s), 0.0) + 1)
     weight = np.where(p > 0, p * np.where(p > 0, -d, 0.0), 0.0).sum(1)
     out = {"stats": np.stack([most, log_s], 1), "log_sum_err": log_err, "entropy": entropy,
-           "entropy_err": log_err + weight * (2 * s_err + 8 * F32) + 2 * F32 * np.abs(entropy),
+           "entropy_err": log_err + (weight + 8) * (2 * s_err + 8 * F32) + 2 * F32 * np.abs(entropy),
            "p": p, "log_p": log_p, "d": d, "admitted": admitted, "some": some}
     inside = (tokens >= 0) & (tokens < V)
     at = np.clip(tokens, 0, V - 1)
