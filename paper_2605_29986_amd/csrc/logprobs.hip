@@ -653,16 +653,27 @@ __global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(GradArgs a)
 
 // ---------------------------------------------------------------- host
 
-// Workgroups of a row: as many as fill the chip, of one round of units to a thread at the least.
-constexpr int32_t kWorkgroups = 512;
-int32_t splits_of(int32_t rows, int32_t V) {
-    const int64_t most = std::min<int64_t>(ceil_div(V, kThreads * 8), kWave);
-    return (int32_t)std::max<int64_t>(std::min<int64_t>(kWorkgroups / std::max(rows, 1), most), 1);
-}
-// Rows of a workgroup: two under masks over classes, if they fill the chip that way.  (With alternatives, which take 6 us for each row at the
-// workgroup's end, 256 x 128,256 took 29.6 us in twos for 26.7.)
-int32_t rows_of(int32_t N, int32_t V, int32_t top, bool classes) {
-    return classes && top == 0 && ceil_div(N, 2) * splits_of((int32_t)ceil_div(N, 2), V) >= kWorkgroups / 2 ? 2 : 1;
+// Rows of a workgroup and workgroups of a row.  A compute unit takes 1.3e-4 us a logit of a row, whether it has one workgroup or more; a row that is
+// split costs a launch that joins its parts, and each workgroup 0.6 us at its end, 1.6 with alternatives.  48 x 32,000 bf16 under masks over
+// classes: whole 7.3 us, in two 9.7; 300 x 128,256 35.1, in two 31.1, three 29.1, four 28.2, sixteen 35.7; 256: 25.0, 24.7, 24.2, 24.6; 1,024: 69, 71, 73, 75.
+// Two rows to a workgroup go under masks over classes where rows are many (128,256: 128 rows 14.0 one by one and 15.5 in twos, 256 24.2 and 22.1,
+// 1,024 69 and 57); not with alternatives, which take 6 us for each row at the workgroup's end (256: 26.7 and 29.6).
+struct Plan {
+    int32_t rows, splits;
+};
+constexpr int32_t kPiece = 8192, kComputeUnits = 256, kPairs = 384, kPairPiece = 32768;
+Plan plan_of(int32_t N, int32_t V, int32_t top, bool classes) {
+    const int64_t most = std::min<int64_t>(ceil_div(V, kPiece), kWave);
+    Plan p{classes && top == 0 && ceil_div(N, 2) * ceil_div(V, kPairPiece) >= kPairs ? 2 : 1, 1};
+    const int64_t rows = ceil_div(N, p.rows);
+    const double row_time = V * 1.3e-4 * p.rows;
+    double best = 0;
+    for (int64_t s = 1; s <= most; ++s) {
+        const double rounds = (double)ceil_div(rows * s, kComputeUnits);
+        const double time = rounds / (double)s * row_time + (s > 1 ? 4.0 : 0.0) + (top ? 1.6 : 0.6) * rounds;
+        if (s == 1 || time < best) best = time, p.splits = (int32_t)s;
+    }
+    return p;
 }
 
 bool kind_ok(int32_t kind) { return kind == CFGZIP_BITS_TOKEN || kind == CFGZIP_BITS_CLASS || kind == CFGZIP_BITS_NONE; }
@@ -732,7 +743,7 @@ using namespace cfgzip;
 
 extern "C" size_t cfgzip_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t top) {
     if (N <= 0 || V <= 0 || top < 0 || top > kMaxTop || N > kMaxRows || V > 0x7FFFFC00) return 0;
-    const int64_t splits = std::max(splits_of(N, V), splits_of((int32_t)ceil_div(N, rows_of(N, V, top, true)), V));
+    const int64_t splits = std::max(plan_of(N, V, top, false).splits, plan_of(N, V, top, true).splits);  // (whatever the masks)
     if (splits == 1) return 0;
     Carver ws(nullptr);
     ws.take<f32x4>((size_t)N * splits);
@@ -758,9 +769,8 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
     a.dtype = dtype;
     a.c = (float)(kLog2eD / temperature), a.per_temperature = (float)(1.0 / temperature);
     a.tokens = tokens, a.n = n, a.top = top;
-    const int32_t rows = rows_of(N, V, top, mask_of(c) == CLASSES);
-    a.splits = splits_of((int32_t)ceil_div(N, rows), V);
-    a.per = (int32_t)ceil_div(ceil_div(V, 8), a.splits);
+    const Plan plan = plan_of(N, V, top, mask_of(c) == CLASSES);
+    a.per = (int32_t)ceil_div(ceil_div(V, 8), plan.splits);
     a.splits = (int32_t)ceil_div(ceil_div(V, 8), a.per);
     a.logprob = logprob, a.entropy = entropy, a.stats = reinterpret_cast<f32x2_any *>(stats), a.top_tokens = top_tokens, a.top_logprobs = top_logprobs;
     Carver carve(ws);
@@ -783,7 +793,7 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
             return check_launch();
         };
         if constexpr (kind.value == CLASSES)
-            if (rows == 2) return launch(std::integral_constant<int, 2>{});
+            if (plan.rows == 2) return launch(std::integral_constant<int, 2>{});
         return launch(std::integral_constant<int, 1>{});
     }));
     if (a.splits == 1) return CFGZIP_OK;

@@ -71,7 +71,7 @@ def test_workspace_query(raw):
     q = raw.cfgzip_token_logprobs_workspace_bytes
     assert q(0, 10, 1) == 0 and q(1, 0, 1) == 0 and q(1, 10, -1) == 0 and q(1, 100_000, 65) == 0
     assert q(1, 4096, 8) == 0 and q(600, 100_000, 64) == 0  # one workgroup to a row
-    assert q(1, 128_256, 0) >= 16 * 31 and q(1, 128_256, 20) >= q(1, 128_256, 0) + 31 * 20 * 8
+    assert q(1, 32_000, 20) == 0 and q(1, 128_256, 0) >= 16 * 2 and q(1, 128_256, 20) >= q(1, 128_256, 0) + 2 * 20 * 8
 
 
 def test_binding_refuses_cpu_tensors():
