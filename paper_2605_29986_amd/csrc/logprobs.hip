@@ -532,14 +532,15 @@ struct GradArgs {
     int32_t mask_words;  // of LDS in front of the given tokens' results
 };
 
-// eight results as they lie
+// Eight results as they lie.  They are not to be kept: what is written and kept goes to memory while the next call reads (score of 777 x 50,003 fp32
+// behind its gradient 52 us for 33, 4,096 x 128,256 bf16 231 for 208; the gradients themselves 70 for 81, 444 for 438).
 template <int DTYPE>
 __device__ __forceinline__ void write_unit(void *out, int64_t at, int32_t left, const float (&v)[8]) {
     if constexpr (DTYPE == CFGZIP_DTYPE_F32) {
         float *const p = static_cast<float *>(out) + at;
         if (left >= 8) {
-            *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4_any *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_any *>(p));
+            __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_any *>(p + 4));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -552,7 +553,7 @@ __device__ __forceinline__ void write_unit(void *out, int64_t at, int32_t left, 
             u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = T::round2(v[2 * j], v[2 * j + 1]);
-            *reinterpret_cast<u32x4_any *>(p) = w;
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any *>(p));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -569,7 +570,7 @@ __global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(GradArgs a)
     extern __shared__ uint32_t mask[];
     float *const given = reinterpret_cast<float *>(mask + a.mask_words);
     const int lane = threadIdx.x % kWave;
-    const int64_t row = blockIdx.x / a.splits;
+    const int64_t row = a.l.N - 1 - blockIdx.x / a.splits;  // the last rows first: they were read last, and may be in a cache
     const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
     const int32_t u0 = split * a.per, u1 = units - u0 < a.per ? units : u0 + a.per;
     const int32_t *const tokens = a.tokens + row * a.n;
