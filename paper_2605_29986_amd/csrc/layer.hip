@@ -15,12 +15,14 @@
 namespace cfgzip {
 namespace {
 
+using ShapeSmall = Shape<64, 64, 2, 2, 2>;
 using Shape64 = Shape<128, 64, 4, 1, 3>;
 using Shape128 = Shape<256, 128, 4, 2, 3>;
 using Shape256 = Shape<256, 256, 2, 2, 2>;
 
 constexpr int32_t kFewRows = 16;
 constexpr int32_t kMaxRows = 1 << 22;
+constexpr int64_t kComputeUnits = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -219,7 +221,9 @@ __device__ __forceinline__ f32x4 taken(const f32x4 &acc) {
         });
         return z;
     }
-    return acc;
+    f32x4 z = acc;
+    asm volatile("" : "+v"(z));  // (nor are they kept in memory, to be picked by number)
+    return z;
 }
 
 // A wave's sums on their way out: 16 rows of 16 FRAGMENTS columns at a time through the part of LDS that the operands' buffers leave, so that
@@ -563,39 +567,43 @@ bool whole_units(const void *p, int64_t stride, int32_t D) { return aligned_to(p
 // workgroups that are at work at a time: as many to a compute unit as its LDS holds
 template <typename S>
 constexpr int64_t slots() {
-    return 256 * (160 * 1024 / (S::kStages * S::kLds));
+    return kComputeUnits * (160 * 1024 / (S::kStages * S::kLds + S::WM * S::WN * Way<S>::kBytes));
 }
-// What a product's tiles take, in microseconds: rounds of as many as are at work at a time, of so many steps each and a beginning and an end.
+// What a step and a tile's ends take a compute unit, in microseconds.  A step is bound by bringing its operands from the second-level cache, 45 to 60 KB/us
+// for a compute unit whether one workgroup does it or more, but for the largest tile; so tiles are worth as much as they read little.
 template <typename S>
-constexpr double kStepTime = S::BM * S::BN == 65536 ? 1.6 : S::BM * S::BN == 32768 ? 1.0 : 0.6;
+constexpr double kStepTime = S::BM * S::BN == 65536 ? 1.45 : S::BM * S::BN == 32768 ? 0.9 : S::BM * S::BN == 8192 ? 0.38 : 0.31;
 template <typename S>
-constexpr double kEndsTime = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.0 : 4.0;
+constexpr double kEndsTime = S::BM * S::BN == 65536 ? 10.0 : S::BM * S::BN == 32768 ? 6.5 : S::BM * S::BN == 8192 ? 2.2 : 1.2;
 
+enum class Tiles : int { SMALL, MIDDLE, LARGE, LARGEST };
 struct Plan {
-    int shape;  // 64, 128, 256: its extent in n
+    Tiles tiles;
     int32_t k_split, splits;
 };
 
-// A product [n][m] over k.  large: the largest tile is there too (it is not for weights at odd addresses).
-Plan plan_of(int64_t m, int64_t n, int64_t k, bool large) {
+// A product [n][m] over k.  all: the smallest and the largest tiles are there too (they are not for weights at odd addresses).
+Plan plan_of(int64_t m, int64_t n, int64_t k, bool all) {
     Plan p{};
     double best = 0;
-    auto look = [&](auto shape) {
+    auto look = [&](auto shape, Tiles which) {
         using S = decltype(shape);
         const int64_t tiles = ceil_div(m, S::BM) * ceil_div(n, S::BN), steps = ceil_div(k, kStepK);
-        for (int64_t s = 1; s <= 32 && (s == 1 || (s * 4 <= steps && tiles * s <= slots<S>())); ++s) {
+        for (int64_t s = 1; s <= 32 && (s == 1 || (s * 2 <= steps && tiles * s <= slots<S>())); ++s) {
             const int64_t per = ceil_div(steps, s);
-            const double shares = s > 1 ? 4.0 + (double)s * n * pad(m, 4) * 8.0 / 4e6 : 0.0;
-            const double time = (double)ceil_div(tiles * s, slots<S>()) * ((double)per * kStepTime<S> + kEndsTime<S>) + shares;
+            // a launch, and the shares written and read
+            const double shares = s > 1 ? 3.5 + (double)s * n * pad(m, 4) * 8.0 / 8e6 : 0.0;
+            const double time = (double)ceil_div(tiles * s, kComputeUnits) * ((double)per * kStepTime<S> + kEndsTime<S>) + shares;
             if (best == 0 || time < best) {
                 best = time;
-                p = Plan{S::BN, (int32_t)(per * kStepK), (int32_t)ceil_div(steps, per)};
+                p = Plan{which, (int32_t)(per * kStepK), (int32_t)ceil_div(steps, per)};
             }
         }
     };
-    look(Shape64{});
-    look(Shape128{});
-    if (large) look(Shape256{});
+    if (all) look(ShapeSmall{}, Tiles::SMALL);
+    look(Shape64{}, Tiles::MIDDLE);
+    look(Shape128{}, Tiles::LARGE);
+    if (all) look(Shape256{}, Tiles::LARGEST);
     return p;
 }
 
@@ -617,16 +625,16 @@ int product(ProductArgs a, const E &end, bool direct, Carver &ws, hipStream_t st
     a.sums_ld = (int32_t)pad(a.m, 4);
     if (p.splits > 1) a.sums = ws.take<float>((size_t)p.splits * a.n * a.sums_ld);
     if (!launch) return CFGZIP_OK;
-    if constexpr (!(A_COLUMNS && B_COLUMNS)) {
-        if (!direct) {
-            if (p.shape == 64) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
-            else CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
-        }
-    }
     if (direct) {
-        if (p.shape == 64) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
-        else if (p.shape == 128) CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
-        else CFGZIP_TRY((launch_product_of<T, Shape256, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+        switch (p.tiles) {
+            case Tiles::SMALL: CFGZIP_TRY((launch_product_of<T, ShapeSmall, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
+            case Tiles::MIDDLE: CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
+            case Tiles::LARGE: CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
+            default: CFGZIP_TRY((launch_product_of<T, Shape256, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+        }
+    } else if constexpr (!(A_COLUMNS && B_COLUMNS)) {
+        if (p.tiles == Tiles::MIDDLE) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
+        else CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
     }
     if (p.splits == 1) return CFGZIP_OK;
     const int64_t units = (int64_t)a.n * (a.sums_ld / 4);
