@@ -20,7 +20,7 @@ using Shape64 = Shape<128, 64, 4, 1, 3>;
 using Shape128 = Shape<256, 128, 4, 2, 3>;
 using Shape256 = Shape<256, 256, 2, 2, 2>;
 
-constexpr int32_t kFewRows = 16;
+constexpr int64_t kFewWeights = 1 << 22;
 constexpr int32_t kMaxRows = 1 << 22;
 constexpr int64_t kComputeUnits = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -102,7 +102,18 @@ __device__ __forceinline__ void write4(uint16_t *p, u32x2 v, int32_t left) {
     if (left >= 4) {
         *reinterpret_cast<u32x2_any *>(p) = v;
     } else {
-        for (int i = 0; i < left; ++i) p[i] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+        p[0] = (uint16_t)v[0];
+        if (left > 1) p[1] = (uint16_t)(v[0] >> 16);
+        if (left > 2) p[2] = (uint16_t)v[1];
+    }
+}
+__device__ __forceinline__ void write4(float *p, f32x4 v, int32_t left) {
+    if (left >= 4) {
+        *reinterpret_cast<f32x4_any *>(p) = v;
+    } else {
+        p[0] = v[0];
+        if (left > 1) p[1] = v[1];
+        if (left > 2) p[2] = v[2];
     }
 }
 template <typename T>
@@ -146,32 +157,28 @@ struct Forward {
         u32x2 codes;
         act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value>(z, b, r, codes); });
         if (slope) write4(slope + n * slope_ld + m, codes, left);
-        if (!f32) {
-            write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y), left);
-            return;
-        }
-        float *const p = static_cast<float *>(out) + n * out_ld + m;
-        if (left >= 4) {
-            *reinterpret_cast<f32x4_any *>(p) = y;
-        } else {
-            for (int i = 0; i < left; ++i) p[i] = y[i];
-        }
+        if (f32) write4(static_cast<float *>(out) + n * out_ld + m, y, left);
+        else write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y), left);
     }
-    // P rows, STEP apart, all of whose four results are there: nothing branches among the results
+    // Those of P rows, STEP apart, that there are: nothing branches among the results.
     template <typename T, int P, int STEP>
-    __device__ __forceinline__ void store_rows(int32_t n, int32_t m, f32x4 (&z)[P], Column b, const Row (&r)[P]) const {
+    __device__ __forceinline__ void store_rows(int32_t n, int32_t N, int32_t m, f32x4 (&z)[P], Column b, const Row (&r)[P]) const {
         u32x2 codes[P];
         act.with([&](auto kind) CFGZIP_INLINE {
             each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value>(z[p.value], b, r[p.value], codes[p.value]); });
         });
-        if (slope) each<P>([&](auto p) CFGZIP_INLINE { write4(slope + (n + p.value * STEP) * slope_ld + m, codes[p.value], 4); });
+        if (slope)
+            each<P>([&](auto p) CFGZIP_INLINE {
+                if (n + p.value * STEP < N) write4(slope + (n + p.value * STEP) * slope_ld + m, codes[p.value], M - m);
+            });
         if (f32) {
             each<P>([&](auto p) CFGZIP_INLINE {
-                *reinterpret_cast<f32x4_any *>(static_cast<float *>(out) + (n + p.value * STEP) * out_ld + m) = z[p.value];
+                if (n + p.value * STEP < N) write4(static_cast<float *>(out) + (n + p.value * STEP) * out_ld + m, z[p.value], M - m);
             });
         } else {
             each<P>([&](auto p) CFGZIP_INLINE {
-                write4(static_cast<uint16_t *>(out) + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value]), 4);
+                if (n + p.value * STEP < N)
+                    write4(static_cast<uint16_t *>(out) + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value]), M - m);
             });
         }
     }
@@ -192,8 +199,10 @@ struct Gradient {
         write4(out + n * out_ld + m, round4<T>(z * back), M - m);
     }
     template <typename T, int P, int STEP>
-    __device__ __forceinline__ void store_rows(int32_t n, int32_t m, f32x4 (&z)[P], Column back, const Row (&)[P]) const {
-        each<P>([&](auto p) CFGZIP_INLINE { write4(out + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value] * back), 4); });
+    __device__ __forceinline__ void store_rows(int32_t n, int32_t N, int32_t m, f32x4 (&z)[P], Column back, const Row (&)[P]) const {
+        each<P>([&](auto p) CFGZIP_INLINE {
+            if (n + p.value * STEP < N) write4(out + (n + p.value * STEP) * out_ld + m, round4<T>(z[p.value] * back), M - m);
+        });
     }
 };
 
@@ -243,12 +252,12 @@ struct Way {
     static __device__ __forceinline__ int at(int r, int u) { return r * (kLanes * 16) + ((u ^ (r & 7)) * 16); }
 };
 
-template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool DIRECT, typename E>
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E end) {
     // (B goes on with zeros to the end of a step, so what A has there only has to be finite; hidden states by columns go on with zeros too: with
     // ANY the largest tile's addresses are out of the registers, 122 of them)
-    using TileA = Tile<S::BM, S::kThreads, A_COLUMNS, DIRECT, A_COLUMNS && B_COLUMNS ? PADDED : ANY>;
-    using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, true, PADDED>;
+    using TileA = Tile<S::BM, S::kThreads, A_COLUMNS, A_DIRECT, A_COLUMNS && B_COLUMNS ? PADDED : ANY>;
+    using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, B_DIRECT, PADDED>;
     CFGZIP_STAGES(S, lds);
     __shared__ __attribute__((aligned(16))) char way[S::WM * S::WN * Way<S>::kBytes];
     auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
@@ -273,7 +282,6 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
         typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
         lds_char *const mine = (lds_char *)way + (wm * S::WN + wn) * W::kBytes;
         const int32_t m0 = tm * S::BM + wm * S::TM + lane % W::kLanes * 4, n0 = tn * S::BN + wn * S::TN + lane / W::kLanes;
-        const bool all = (a.m & 3) == 0 && tn * S::BN + wn * S::TN + S::TN <= a.n;
         typename E::Column column{}, next_column{};
         typename E::Row row[W::kPasses], next[W::kPasses];
         auto ask = [&](int32_t chunk) CFGZIP_INLINE {
@@ -281,7 +289,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
             if (a.sums || m >= a.m) return;
             next_column = end.column(m);
             each<W::kPasses>([&](auto p) CFGZIP_INLINE {
-                if (all || n + p.value * W::kRows < a.n) next[p.value] = end.row(n + p.value * W::kRows, m);
+                if (n + p.value * W::kRows < a.n) next[p.value] = end.row(n + p.value * W::kRows, m);
             });
         };
         ask(0);
@@ -308,12 +316,8 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
                 each<W::kPasses>([&](auto p) CFGZIP_INLINE {
                     if (n + p.value * W::kRows < a.n) *reinterpret_cast<f32x4 *>(p0 + (int64_t)p.value * W::kRows * a.sums_ld) = z[p.value];
                 });
-            } else if (all) {
-                end.template store_rows<T, W::kPasses, W::kRows>(n, m, z, column, row);
             } else {
-                each<W::kPasses>([&](auto p) CFGZIP_INLINE {
-                    if (n + p.value * W::kRows < a.n) end.template store<T>(n + p.value * W::kRows, m, z[p.value], column, row[p.value]);
-                });
+                end.template store_rows<T, W::kPasses, W::kRows>(n, a.n, m, z, column, row);
             }
         }
     };
@@ -350,7 +354,6 @@ struct FewArgs {
     int32_t N, M, D;
 };
 constexpr int kFewWaves = 16, kFewThreads = kFewWaves * kWave;
-constexpr int kFewAhead = 4;  // steps of 64 on their way at a time
 
 // eight elements of a row of which `left` are there, at any alignment
 __device__ __forceinline__ u32x4 eight(const uint16_t *p, int32_t left) {
@@ -363,52 +366,64 @@ __device__ __forceinline__ u32x4 eight(const uint16_t *p, int32_t left) {
 }
 
 // Lane l has row l & 15 of both sides and of every 64 elements those of 16 (l >> 4) on, which two products take as if they were apart: a sum has
-// no order of its own, and a row's 128 bytes come in one line.
-template <typename T>
+// no order of its own, and a row's 128 bytes come in one line.  FRAGMENTS of 16 rows of hidden states.
+template <typename T, int FRAGMENTS>
 __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a, Forward end) {
-    __shared__ f32x4 shared[kFewWaves][kWave];
+    constexpr int kAhead = FRAGMENTS == 1 ? 4 : 2;  // steps of 64 on their way at a time
+    __shared__ f32x4 shared[FRAGMENTS][kFewWaves][kWave];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int r = lane & 15, g = lane >> 4;
     const int32_t m0 = blockIdx.x * 16, steps = (a.D + 63) / 64;
     const int32_t s0 = (int32_t)((int64_t)steps * wave / kFewWaves), s1 = (int32_t)((int64_t)steps * (wave + 1) / kFewWaves);
-    const uint16_t *const w = a.w + (m0 + r < a.M ? m0 + r : a.M - 1) * a.w_ld;
-    const uint16_t *const x = a.x + (r < a.N ? r : a.N - 1) * a.x_ld;
-    const int32_t m = m0 + 4 * g;
+    const uint16_t *const w = a.w + (m0 + r < a.M ? m0 + r : a.M - 1) * a.w_ld + g * 16;
+    const uint16_t *x[FRAGMENTS];
+#pragma unroll
+    for (int f = 0; f < FRAGMENTS; ++f) x[f] = a.x + (f * 16 + r < a.N ? f * 16 + r : a.N - 1) * a.x_ld + g * 16;
+    // wave f ends fragment f's results
+    const int32_t m = m0 + 4 * g, n = wave * 16 + r;
+    const bool mine = wave < FRAGMENTS && n < a.N && m < a.M;
     u32x2 bias = {0, 0}, residual = {0, 0};
-    if (wave == 0 && r < a.N && m < a.M) bias = end.column(m), residual = end.row(r, m);
-    f32x4 acc = {0, 0, 0, 0};
-    for (int32_t s = s0; s < s1; s += kFewAhead) {
-        u32x4 p[kFewAhead][2], q[kFewAhead][2];
-        if (s + kFewAhead <= s1 && (s + kFewAhead) * 64 <= a.D) {
+    if (mine) bias = end.column(m), residual = end.row(n, m);
+    f32x4 acc[FRAGMENTS];
 #pragma unroll
-            for (int i = 0; i < kFewAhead; ++i)
+    for (int f = 0; f < FRAGMENTS; ++f) acc[f] = f32x4{0, 0, 0, 0};
+    for (int32_t s = s0; s < s1; s += kAhead) {
+        u32x4 p[kAhead][2], q[FRAGMENTS][kAhead][2];
+        if (s + kAhead <= s1 && (s + kAhead) * 64 <= a.D) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) p[i][h] = *reinterpret_cast<const u32x4_any *>(w + (s + i) * 64 + g * 16 + h * 8);
-#pragma unroll
-            for (int i = 0; i < kFewAhead; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) q[i][h] = *reinterpret_cast<const u32x4_any *>(x + (s + i) * 64 + g * 16 + h * 8);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kFewAhead; ++i)
+            for (int i = 0; i < kAhead; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int32_t c = (s + i) * 64 + g * 16 + h * 8, left = s + i < s1 ? a.D - c : 0;
+                    p[i][h] = *reinterpret_cast<const u32x4_any *>(w + (s + i) * 64 + h * 8);
+#pragma unroll
+                    for (int f = 0; f < FRAGMENTS; ++f) q[f][i][h] = *reinterpret_cast<const u32x4_any *>(x[f] + (s + i) * 64 + h * 8);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int32_t c = (s + i) * 64 + h * 8, left = s + i < s1 ? a.D - c - g * 16 : 0;
                     p[i][h] = eight(w + c, left);
-                    q[i][h] = eight(x + c, left);
+#pragma unroll
+                    for (int f = 0; f < FRAGMENTS; ++f) q[f][i][h] = eight(x[f] + c, left);
                 }
         }
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i)
+        for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) acc = T::mma(p[i][h], q[i][h], acc);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int f = 0; f < FRAGMENTS; ++f) acc[f] = T::mma(p[i][h], q[f][i][h], acc[f]);
     }
-    shared[wave][lane] = acc;
-    __syncthreads();
-    if (threadIdx.x >= kWave) return;
 #pragma unroll
-    for (int i = 1; i < kFewWaves; ++i) acc += shared[i][lane];
-    if (r < a.N && m < a.M) end.template store<T>(r, m, acc, bias, residual);
+    for (int f = 0; f < FRAGMENTS; ++f) shared[f][wave][lane] = acc[f];
+    __syncthreads();
+    if (wave >= FRAGMENTS) return;
+    f32x4 z = shared[wave][0][lane];
+#pragma unroll
+    for (int i = 1; i < kFewWaves; ++i) z += shared[wave][i][lane];
+    if (mine) end.template store<T>(n, m, z, bias, residual);
 }
 
 // ---------------------------------------------------------------- dz and the gradient of the bias
@@ -483,12 +498,55 @@ __global__ __launch_bounds__(256) void largest_kernel(const void *grad_out, int6
     if (threadIdx.x == 0) largest[blockIdx.x] = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
 }
 
-// A workgroup has 512 columns of `rows` rows, a wave every fourth of them, a thread eight columns.
+// eight of grad_out's values and their slopes as they lie
+template <bool F32>
+struct Eight {
+    u32x4 g[F32 ? 2 : 1], s;
+    __device__ __forceinline__ void read(const DzArgs &a, int32_t row, int32_t c) {
+        const int32_t left = a.M - c;
+        if constexpr (F32) {
+            const float *const p = static_cast<const float *>(a.grad_out) + row * a.grad_ld + c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (left >= 8) {
+                    g[h] = __builtin_bit_cast(u32x4, f32x4(*reinterpret_cast<const f32x4_any *>(p + 4 * h)));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) g[h][j] = 4 * h + j < left ? __builtin_bit_cast(uint32_t, p[4 * h + j]) : 0u;
+                }
+            }
+        } else {
+            g[0] = eight(static_cast<const uint16_t *>(a.grad_out) + row * a.grad_ld + c, left);
+        }
+        if (a.slope) s = eight(a.slope + row * a.slope_ld + c, left);
+    }
+    template <typename T>
+    __device__ __forceinline__ void values(const DzArgs &a, float (&v)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t x = F32 ? g[j / 4][j % 4] : g[0][j / 2] >> (j % 2 * 16);
+            v[j] = F32 ? __builtin_bit_cast(float, x) : T::value((uint16_t)x);
+            if (a.slope) v[j] *= slope_value(s[j / 2] >> (j % 2 * 16));
+        }
+    }
+};
+
+// A workgroup has 512 columns of `rows` rows, a wave every fourth of them, a thread eight columns.  Rows are asked for four at a time, the first
+// ahead of what scales them.
 template <typename T, bool F32>
 __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
     __shared__ float shared[4][kWave][9];
     __shared__ float most_of[4];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int32_t c = (blockIdx.x * kWave + lane) * 8, r0 = blockIdx.y * a.rows + wave;
+    constexpr int kAhead = 4;
+    Eight<F32> x[kAhead];
+    auto read = [&](int32_t i) CFGZIP_INLINE {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + 4 * k + wave < a.rows && r0 + i + 4 * k < a.N && c < a.dz_ld) x[k].read(a, r0 + i + 4 * k, c);
+    };
+    read(0);
     float factor = 1.0f;
     if (a.largest) {
         float most = a.largest[threadIdx.x];
@@ -502,28 +560,26 @@ __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
         factor = __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.unscale = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
     }
-    const int32_t c = (blockIdx.x * kWave + lane) * 8, r0 = blockIdx.y * a.rows;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (c < a.dz_ld) {
-#pragma unroll 4
-        for (int32_t i = wave; i < a.rows; i += 4) {
-            const int32_t row = r0 + i;
-            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (row < a.N) {
-                read8<T, F32>(static_cast<const char *>(a.grad_out) + row * a.grad_ld * (F32 ? 4 : 2), c, a.M - c, v);
-                if (a.slope) {
-                    const u32x4 s = eight(a.slope + row * a.slope_ld + c, a.M - c);
+        for (int32_t i = 0; i + wave < a.rows; i += 4 * kAhead) {
+            if (i) read(i);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] *= slope_value(s[j / 2] >> (j % 2 * 16));
+            for (int k = 0; k < kAhead; ++k) {
+                const int32_t row = r0 + i + 4 * k;
+                if (i + 4 * k + wave >= a.rows) break;
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (row < a.N) {
+                    x[k].template values<T>(a, v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += v[j];
                 }
+                if (a.dz) {
+                    u32x4 d;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += v[j];
-            }
-            if (a.dz) {
-                u32x4 d;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) d[j] = T::round2(v[2 * j] * factor, v[2 * j + 1] * factor);
-                *reinterpret_cast<u32x4 *>(a.dz + (int64_t)row * a.dz_ld + c) = d;
+                    for (int j = 0; j < 4; ++j) d[j] = T::round2(v[2 * j] * factor, v[2 * j + 1] * factor);
+                    *reinterpret_cast<u32x4 *>(a.dz + (int64_t)row * a.dz_ld + c) = d;
+                }
             }
         }
     }
@@ -539,19 +595,23 @@ __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
     }
 }
 
+// A workgroup has 64 columns, a wave every fourth block of rows.
 template <typename T>
-__global__ __launch_bounds__(kWave) void bias_kernel(const float *sums, int32_t blocks, int32_t ld, int32_t M, uint16_t *out) {
-    const int32_t c = blockIdx.x * kWave + threadIdx.x;
-    if (c >= M) return;
+__global__ __launch_bounds__(256) void bias_kernel(const float *sums, int32_t blocks, int32_t ld, int32_t M, uint16_t *out) {
+    __shared__ float shared[4][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int32_t c = blockIdx.x * kWave + lane;  // (ld is whole steps of 64 columns)
     float x = 0.0f;
-    for (int32_t b = 0; b < blocks; b += 8) {
+    for (int32_t b = wave; b < blocks; b += 32) {
         float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = b + i < blocks ? sums[(int64_t)(b + i) * ld + c] : 0.0f;
+        for (int i = 0; i < 8; ++i) y[i] = b + 4 * i < blocks ? sums[(int64_t)(b + 4 * i) * ld + c] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x += y[i];
     }
-    out[c] = T::round(x);
+    shared[wave][lane] = x;
+    __syncthreads();
+    if (wave == 0 && c < M) out[c] = T::round((shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]));
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
@@ -607,34 +667,42 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool all) {
     return p;
 }
 
-template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool DIRECT, typename E>
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
 int launch_product_of(ProductArgs a, const E &end, hipStream_t stream) {
     a.tiles_m = (int32_t)ceil_div(a.m, S::BM);
     a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
     const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = std::min(work, slots<S>());
     if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
-    hipLaunchKernelGGL((product_kernel<T, S, A_COLUMNS, B_COLUMNS, DIRECT, E>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a, end);
+    hipLaunchKernelGGL((product_kernel<T, S, A_COLUMNS, B_COLUMNS, A_DIRECT, B_DIRECT, E>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a, end);
     return check_launch();
 }
 
-// ws: room for the shares of a sum that is split; taken, or with `launch` used
+// Which operand is not in whole units of 16 bytes, or does not go on with zeros to the end of a step: it comes through registers.
+enum class Odd : int { NONE, A, B };
+
+// ws: room for the shares of a sum that is split; taken, or with `launch` used.  B may be odd, and A of columns with columns, in the smallest tiles only.
 template <typename T, bool A_COLUMNS, bool B_COLUMNS, typename E>
-int product(ProductArgs a, const E &end, bool direct, Carver &ws, hipStream_t stream, bool launch) {
-    const Plan p = plan_of(a.m, a.n, a.k, direct);
+int product(ProductArgs a, const Plan &p, const E &end, Odd odd, Carver &ws, hipStream_t stream, bool launch) {
     a.k_split = p.k_split, a.splits = p.splits;
     a.sums_ld = (int32_t)pad(a.m, 4);
     if (p.splits > 1) a.sums = ws.take<float>((size_t)p.splits * a.n * a.sums_ld);
     if (!launch) return CFGZIP_OK;
-    if (direct) {
+    if (odd == Odd::NONE) {
         switch (p.tiles) {
-            case Tiles::SMALL: CFGZIP_TRY((launch_product_of<T, ShapeSmall, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
-            case Tiles::MIDDLE: CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
-            case Tiles::LARGE: CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, true>(a, end, stream))); break;
-            default: CFGZIP_TRY((launch_product_of<T, Shape256, A_COLUMNS, B_COLUMNS, true>(a, end, stream)));
+            case Tiles::SMALL: CFGZIP_TRY((launch_product_of<T, ShapeSmall, A_COLUMNS, B_COLUMNS, true, true>(a, end, stream))); break;
+            case Tiles::MIDDLE: CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, true, true>(a, end, stream))); break;
+            case Tiles::LARGE: CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, true, true>(a, end, stream))); break;
+            default: CFGZIP_TRY((launch_product_of<T, Shape256, A_COLUMNS, B_COLUMNS, true, true>(a, end, stream)));
         }
-    } else if constexpr (!(A_COLUMNS && B_COLUMNS)) {
-        if (p.tiles == Tiles::MIDDLE) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
-        else CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, false>(a, end, stream)));
+    } else if constexpr (A_COLUMNS && B_COLUMNS) {
+        CFGZIP_TRY((launch_product_of<T, ShapeSmall, true, true, false, true>(a, end, stream)));
+    } else {
+        if constexpr (!A_COLUMNS)
+            if (odd == Odd::B) CFGZIP_TRY((launch_product_of<T, ShapeSmall, false, false, true, false>(a, end, stream)));
+        if (odd == Odd::A) {
+            if (p.tiles == Tiles::MIDDLE) CFGZIP_TRY((launch_product_of<T, Shape64, A_COLUMNS, B_COLUMNS, false, true>(a, end, stream)));
+            else CFGZIP_TRY((launch_product_of<T, Shape128, A_COLUMNS, B_COLUMNS, false, true>(a, end, stream)));
+        }
     }
     if (p.splits == 1) return CFGZIP_OK;
     const int64_t units = (int64_t)a.n * (a.sums_ld / 4);
@@ -669,23 +737,36 @@ int copy_rows(const Call &c, uint16_t *y, int32_t y_ld, int32_t all, hipStream_t
     return check_launch();
 }
 
+// Every workgroup of 16 columns reads all hidden states from the second-level cache, so rows are few, or weights: against tiles, whose sums are split and
+// joined by a launch of their own, 33 x 2,000 x 1,000 took 7.6 us for 11.7, 24 x 4,096 x 4,096 12.6 for 16, 16 x 16,384 x 4,096 37 for 29, 8 x that 31.
+bool few_rows(const Call &c) {
+    const int64_t weights = (int64_t)c.M * c.D;
+    return c.N <= 8 || (c.N <= 32 && weights <= 4 * kFewWeights) || (c.N <= 64 && weights <= kFewWeights);
+}
+
 template <typename T>
 int forward(const Call &c, const Forward &end, bool direct, Carver &ws, hipStream_t stream, bool launch) {
-    if (c.N <= kFewRows) {
+    if (few_rows(c)) {
         if (!launch) return CFGZIP_OK;
         const FewArgs a{c.x(), c.w(), c.hidden_stride, c.weight_stride, c.N, c.M, c.D};
-        hipLaunchKernelGGL(few_rows_kernel<T>, dim3((uint32_t)ceil_div(c.M, 16)), dim3(kFewThreads), 0, stream, a, end);
+        const dim3 grid((uint32_t)ceil_div(c.M, 16));
+        if (c.N <= 16) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, dim3(kFewThreads), 0, stream, a, end);
+        else if (c.N <= 32) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, dim3(kFewThreads), 0, stream, a, end);
+        else hipLaunchKernelGGL((few_rows_kernel<T, 4>), grid, dim3(kFewThreads), 0, stream, a, end);
         return check_launch();
     }
     const int32_t d_pad = (int32_t)pad(c.D, kStepK);
     uint16_t *copy = ws.take<uint16_t>((size_t)c.N * d_pad);
+    const Plan p = plan_of(c.M, c.N, c.D, direct);
     const bool as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.D % kStepK == 0 && c.hidden_stride < kMaxStride;
-    if (launch && !as_it_is) CFGZIP_TRY(copy_rows(c, copy, d_pad, c.N, stream));
+    // (small products of odd hidden states are shorter than copying those, 6 us of 16 for 777 x 1,000 x 1,000)
+    const bool odd = !as_it_is && p.tiles == Tiles::SMALL && c.hidden_stride < kMaxStride;
+    if (launch && !as_it_is && !odd) CFGZIP_TRY(copy_rows(c, copy, d_pad, c.N, stream));
     ProductArgs a{};
     a.A = by_rows(c.w(), c.weight_stride, c.M);
-    a.B = as_it_is ? by_rows(c.x(), c.hidden_stride, c.N) : by_rows(copy, d_pad, c.N);
+    a.B = as_it_is || odd ? by_rows(c.x(), c.hidden_stride, c.N) : by_rows(copy, d_pad, c.N);
     a.m = c.M, a.n = c.N, a.k = c.D;
-    return product<T, false, false>(a, end, direct, ws, stream, launch);
+    return product<T, false, false>(a, p, end, !direct ? Odd::A : odd ? Odd::B : Odd::NONE, ws, stream, launch);
 }
 
 struct Grads {
@@ -701,7 +782,7 @@ struct Grads {
 template <typename T>
 int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t stream, bool launch) {
     const int32_t m_pad = (int32_t)pad(c.M, kStepK), n_pad = (int32_t)pad(c.N, kStepK), d_units = (int32_t)pad(c.D, 8);
-    const int32_t rows = c.N <= 1024 ? 16 : 64, blocks = n_pad / rows;
+    const int32_t rows = c.N <= 1024 ? 8 : 64, blocks = n_pad / rows;
     float *unscale = ws.take<float>(1), *largest = ws.take<float>(kLargestBlocks), *sums = ws.take<float>((size_t)blocks * m_pad);
     uint16_t *dz = ws.take<uint16_t>((size_t)n_pad * m_pad), *copy = ws.take<uint16_t>((size_t)n_pad * d_units);
     // grad_out is dz where nothing has to be done to it
@@ -722,7 +803,7 @@ int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t
         else hipLaunchKernelGGL((dz_kernel<T, false>), grid, dim3(256), 0, stream, a);
         CFGZIP_TRY(check_launch());
         if (g.bias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((uint32_t)ceil_div(c.M, kWave)), dim3(kWave), 0, stream, sums, blocks, m_pad, c.M, g.bias);
+            hipLaunchKernelGGL(bias_kernel<T>, dim3((uint32_t)ceil_div(c.M, kWave)), dim3(256), 0, stream, sums, blocks, m_pad, c.M, g.bias);
             CFGZIP_TRY(check_launch());
         }
     }
@@ -735,18 +816,20 @@ int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t
         a.m = c.D, a.n = c.N, a.k = c.M;
         Carver own = ws;
         const Gradient end{scaled ? unscale : nullptr, g.hidden, g.hidden_stride, c.D};
-        CFGZIP_TRY((product<T, true, false>(a, end, direct, own, stream, launch)));
+        CFGZIP_TRY((product<T, true, false>(a, plan_of(a.m, a.n, a.k, direct), end, direct ? Odd::NONE : Odd::A, own, stream, launch)));
         if (!launch) ws.used = std::max(ws.used, own.used);
     }
     if (g.weight || !launch) {
         const bool x_as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.N % kStepK == 0 && c.hidden_stride < kMaxStride;
-        if (launch && !x_as_it_is) CFGZIP_TRY(copy_rows(c, copy, d_units, n_pad, stream));
+        const Plan p = plan_of(c.D, c.M, c.N, true);
+        const bool odd = !x_as_it_is && p.tiles == Tiles::SMALL && c.hidden_stride < kMaxStride;
+        if (launch && !x_as_it_is && !odd) CFGZIP_TRY(copy_rows(c, copy, d_units, n_pad, stream));
         ProductArgs a{};
-        a.A = x_as_it_is ? by_columns(c.x(), c.hidden_stride, c.D) : by_columns(copy, d_units, d_units);
+        a.A = x_as_it_is || odd ? by_columns(c.x(), c.hidden_stride, c.D) : by_columns(copy, d_units, d_units);
         a.B = by_columns(d, d_ld, m_pad);
         a.m = c.D, a.n = c.M, a.k = c.N;
         const Gradient end{scaled ? unscale : nullptr, g.weight, g.weight_stride, c.D};
-        CFGZIP_TRY((product<T, true, true>(a, end, true, ws, stream, launch)));
+        CFGZIP_TRY((product<T, true, true>(a, p, end, odd ? Odd::A : Odd::NONE, ws, stream, launch)));
     }
     return CFGZIP_OK;
 }
