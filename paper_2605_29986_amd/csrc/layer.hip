@@ -21,7 +21,7 @@ using Shape128 = Shape<256, 128, 4, 2, 3>;
 using Shape256 = Shape<256, 256, 2, 2, 2>;
 
 constexpr int64_t kFewWeights = 1 << 22;
-constexpr int32_t kMaxRows = 1 << 22;
+constexpr int32_t kMaxRows = 1 << 21;  // (a launch goes over them in blocks of 64, fewer than 2^16)
 constexpr int64_t kComputeUnits = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));

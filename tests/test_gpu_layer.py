@@ -106,6 +106,13 @@ def test_many_tiles(lib, N, M, D, dtype):
     check(lib, make(4, N, M, D, dtype, bias=False, residual=False), dtype, None)
 
 
+@pytest.mark.parametrize("N,M,D", [(4000, 4100, 4104), (12, 8200, 2100), (20, 10000, 2000), (50, 1030, 4000)])
+def test_largest_tiles_and_few_rows(lib, N, M, D):
+    """The largest tiles in all three products; rows on either side of where every workgroup reads all of them"""
+    print(f"case N={N} M={M} D={D}", flush=True)
+    check(lib, make(11, N, M, D, "bf16"), "bf16", "silu")
+
+
 def test_odd_weights_in_large_tiles(lib):
     check(lib, make(5, 1000, 1111, 777, "bf16", w_offset=1), "bf16", "relu")
     check(lib, make(5, 1000, 1111, 777, "f16", w_gap=2), "f16", "relu")

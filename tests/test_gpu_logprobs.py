@@ -126,6 +126,14 @@ def test_masks(lib, N, V, n, top, mask, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,V", [(769, 3001), (801, 9000), (131, 200_001)])
+def test_two_rows_to_a_workgroup(lib, N, V, dtype):
+    """Many rows under masks over classes, whole and in pieces; an odd one out"""
+    print(f"case N={N} V={V} {dtype}", flush=True)
+    check(lib, make(N, N, V, dtype, mask="class", n=2, C=700), dtype, rows=[0, 1, 2, 3, N // 2, N - 2, N - 1])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("values", ["ties", "equal", "rising", "peaked", "large", "lowest", "infinite", "zeros"])
 def test_values(lib, values, dtype):
     print(f"case {values} {dtype}", flush=True)

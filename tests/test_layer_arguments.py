@@ -54,7 +54,7 @@ def test_refusals(raw, memory):
     for call in (_layer, _grad):
         for change in (dict(work=None), dict(work=p + 16), dict(size=64)):
             assert call(raw, p, N=70, **change) == -2, change
-        for change in (dict(N=(1 << 22) + 1), dict(ws=1 << 22), dict(D=1 << 22, hs=1 << 22, ws=1 << 22),
+        for change in (dict(N=(1 << 21) + 1), dict(ws=1 << 22), dict(D=1 << 22, hs=1 << 22, ws=1 << 22),
                        dict(M=1 << 22, rs=1 << 22, os=1 << 22, ss=1 << 22, gs=1 << 22)):
             change = {k: v for k, v in change.items() if k not in (("gs",) if call is _layer else ("rs", "os"))}
             assert call(raw, p, **change) == -5, change
@@ -65,7 +65,7 @@ def test_refusals(raw, memory):
 def test_workspace_queries(raw):
     q, g = raw.cfgzip_head_layer_workspace_bytes, raw.cfgzip_head_layer_grad_workspace_bytes
     for f in (q, g):
-        assert f(0, 8, 8) == 0 and f(8, 0, 8) == 0 and f(8, 8, 0) == 0 and f(8, 1 << 22, 8) == 0 and f((1 << 22) + 1, 8, 8) == 0
+        assert f(0, 8, 8) == 0 and f(8, 0, 8) == 0 and f(8, 8, 0) == 0 and f(8, 1 << 22, 8) == 0 and f((1 << 21) + 1, 8, 8) == 0
     assert q(1, 4096, 4096) == 0 and q(32, 4096, 4096) == 0 and q(65, 100, 100) >= 65 * 128 * 2
     # dz, hidden states in whole units, columns' sums; never the weights
     assert 4096 * (16384 + 4096) * 2 <= g(4096, 16384, 4096) < 4096 * (16384 + 4096) * 2 + (8 << 20)
