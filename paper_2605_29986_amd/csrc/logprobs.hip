@@ -10,6 +10,9 @@
 // entropy = log S - T / (S temperature), in which nothing large is taken from something as large.  What the gradient needs of a row are m
 // and log S, two numbers: lse in one rounds large logits' to few digits behind the point.
 //
+// A row that is nearly certain has S = 1 and very little, and that little is its log probability, its entropy and its gradient: so S is kept
+// without the largest logit's 1, and where the rest is small the thread that met that logit has its units added up again without it.
+//
 // Alternatives cost the pass nothing: the k-th largest of 64 threads' (or groups of threads') maxima is a bound that k logits at the least reach,
 // so only threads whose maximum reaches it can have had one of the k best.  Their few units are read again (from a cache), what reaches
 // the bound is put together and sorted.  A logit is compared by (value, lower token first) as one 64-bit number.
@@ -260,6 +263,11 @@ struct Sums {
     }
     __device__ __forceinline__ void add(const Sums &o) { s += o.s, t += o.t; }
 };
+// of a row or a part of it: m is the largest logit (-inf: nothing is admitted), the sums are those of all others
+struct Whole {
+    float m, rest, t;
+};
+constexpr float kCertain = 0.0625f;  // a rest below this is added up apart from the 1
 
 struct ScoreArgs {
     Logits l;
@@ -272,7 +280,7 @@ struct ScoreArgs {
     f32x2_any *stats;
     int32_t *top_tokens;
     float *top_logprobs;
-    f32x4 *parts;         // [N][splits]: m (-inf where nothing is admitted), S, T
+    f32x4 *parts;         // [N][splits]: Whole
     uint64_t *part_keys;  // [N][splits][top]
 };
 
@@ -295,25 +303,26 @@ struct Given {
 };
 
 // What belongs to a row, from its sums, its best keys (lane i of wave 0 has the i-th) and a thread's given token.  For all threads of a workgroup.
-__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const Sums &sums, uint64_t key, Given given) {
-    const float log_s = __builtin_amdgcn_logf(sums.s);  // log2; -inf where nothing is admitted
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const Whole &sums, uint64_t key, Given given) {
+    const bool none_at_all = sums.m == -kInf;
+    const float log_s = none_at_all ? -kInf : log1pf(sums.rest);
     if (threadIdx.x == 0) {
-        if (a.stats) a.stats[row] = f32x2_any{sums.s == 0.0f ? -kInf : sums.m, kLn2 * log_s};
+        if (a.stats) a.stats[row] = f32x2_any{sums.m, log_s};
         if (a.entropy) {
-            const float h = kLn2 * log_s - sums.t / sums.s * a.per_temperature;
-            a.entropy[row] = sums.s == 0.0f || h < 0.0f ? 0.0f : h;
+            const float h = log_s - sums.t / (1.0f + sums.rest) * a.per_temperature;
+            a.entropy[row] = none_at_all || h < 0.0f ? 0.0f : h;
         }
     }
     for (int32_t j = threadIdx.x; j < a.n; j += blockDim.x) {
         if (j >= (int32_t)blockDim.x) given = Given(a, row, j);
         const bool none = given.token < 0 || given.token >= a.l.V;
-        a.logprob[row * a.n + j] = none ? 0.0f : given.x == -kInf ? -kInf : (given.x - sums.m) * a.per_temperature - kLn2 * log_s;
+        a.logprob[row * a.n + j] = none ? 0.0f : given.x == -kInf ? -kInf : (given.x - sums.m) * a.per_temperature - log_s;
     }
     if (threadIdx.x < (uint32_t)a.top) {
         const bool there = key != 0;
         a.top_tokens[row * a.top + threadIdx.x] = there ? (int32_t)~(uint32_t)key : -1;
         a.top_logprobs[row * a.top + threadIdx.x] =
-            there ? (value_of((uint32_t)(key >> 32)) - sums.m) * a.per_temperature - kLn2 * log_s : -kInf;
+            there ? (value_of((uint32_t)(key >> 32)) - sums.m) * a.per_temperature - log_s : -kInf;
     }
 }
 
@@ -389,20 +398,55 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
         if (lane == 0) shared_most[r][wave] = all[r];
     }
     __syncthreads();
+    Whole whole[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) all[r] = fmaxf(all[r], shared_most[r][i]);
         if (all[r] > -kInf) sums[r].raise(all[r], a.c);
-        sums[r].s = sum_of(sums[r].s), sums[r].t = sum_of(sums[r].t);
-        if (lane == 0) shared_sums[r][wave] = sums[r];
+        const float s = sum_of(sums[r].s), t = sum_of(sums[r].t);
+        if (lane == 0) shared_sums[r][wave] = Sums{0.0f, s, t};
     }
+    auto add_up = [&](int r) CFGZIP_INLINE {
+        Sums x = shared_sums[r][0];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) x.add(shared_sums[r][i]);
+        return x;
+    };
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        sums[r] = shared_sums[r][0];
+        const Sums x = add_up(r);
+        whole[r] = Whole{all[r], x.s - 1.0f, x.t};
+    }
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) sums[r].add(shared_sums[r][i]);
+    for (int r = 0; r < ROWS; ++r) {
+        if (all[r] == -kInf || !(whole[r].rest < kCertain)) continue;  // (the same for all threads)
+        __syncthreads();
+        const bool met = most[r] == all[r];
+        const uint64_t here = __builtin_amdgcn_ballot_w64(met);
+        float s = met ? 0.0f : sums[r].s, t = met ? 0.0f : sums[r].t;
+        if (here) {  // one thread of the workgroup: the sum is below 2.  Its wave has its units
+            const int32_t first = u0 + wave * kWave + __builtin_ctzll(here);
+            for (int32_t u = first + lane * kThreads; u < u1; u += kWave * kThreads) {
+                Unit<DTYPE> x;
+                Admitted<MASK, ROWS> ok;
+                x.read(a.l, a.l.at(row, r), u);
+                ok.ask(a.l, row, u);
+                ok.look(a.l, row, mask);
+                each<8>([&](auto j) CFGZIP_INLINE {
+                    const float v = ok.template masked<j.value>(r, x.template value<j.value>()), d = v - all[r];
+                    const float e = v == all[r] ? 0.0f : __builtin_amdgcn_exp2f(d * a.c);
+                    s += e;
+                    t = __builtin_fmaf(e, larger_of(d, no_more), t);
+                });
+            }
+        }
+        s = sum_of(s), t = sum_of(t);
+        if (lane == 0) shared_sums[r][wave] = Sums{0.0f, s, t};
+        __syncthreads();
+        const Sums x = add_up(r);
+        whole[r] = Whole{all[r], x.s, x.t};
     }
 
 #pragma unroll
@@ -469,10 +513,10 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
             }
         }
         if (a.splits == 1) {
-            write_row(a, row + r, sums[r], best, given);
+            write_row(a, row + r, whole[r], best, given);
         } else {
             const int64_t part = (row + r) * a.splits + split;
-            if (threadIdx.x == 0) a.parts[part] = f32x4{all[r], sums[r].s, sums[r].t, 0.0f};
+            if (threadIdx.x == 0) a.parts[part] = f32x4{whole[r].m, whole[r].rest, whole[r].t, 0.0f};
             if (TOP && threadIdx.x < (uint32_t)a.top) a.part_keys[part * a.top + threadIdx.x] = best;
         }
         if (TOP && ROWS > 1) __syncthreads();  // wave 0 is done with what the next row is put in
@@ -486,7 +530,6 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a) {
     const int64_t row = blockIdx.x, first = row * a.splits;
     const Given given(a, row);
     const f32x4 part = lane < a.splits ? a.parts[first + lane] : f32x4{-kInf, 0.0f, 0.0f, 0.0f};
-    Sums sums{part[0] > -kInf ? part[0] : 0.0f, part[1], part[2]};
     uint64_t best = 0;
     if (a.top) {
         // a wave's lists, every second one the smallest first, all on their way before the first is used
@@ -509,10 +552,13 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a) {
             if (wave < half) lists[wave][lane] = best = merged(best, lists[wave + half][kWave - 1 - lane], lane);
         }
     }
+    // the part with the largest logit keeps its rest, of the others all is brought to that logit
     const float all = largest_of(part[0]);
-    if (all > -kInf) sums.raise(all, a.c);
-    sums.s = sum_of(sums.s), sums.t = sum_of(sums.t);
-    write_row(a, row, sums, best, given);
+    Sums sums{part[0], 1.0f + part[1], part[2]};
+    if (part[0] == -kInf) sums = Sums{0.0f, 0.0f, 0.0f};
+    else if (lane == __builtin_ctzll(__builtin_amdgcn_ballot_w64(part[0] == all))) sums.s = part[1];
+    else sums.raise(all, a.c);
+    write_row(a, row, Whole{all, sum_of(sums.s), sum_of(sums.t)}, best, given);
 }
 
 // ---------------------------------------------------------------- backward
@@ -613,7 +659,14 @@ __global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(GradArgs a)
         float sum = 0.0f;
 #pragma unroll 8
         for (int32_t q = 0; q < a.n; ++q) sum += tokens[q] == t ? grad_of(q) : 0.0f;
-        given[j] = gradient(x) + sum * a.per_temperature;
+        const float lp = (x - m) * a.per_temperature - log_s;
+        if (lp > -0.5f) {  // of a token that is nearly certain 1 - p from its log probability
+            float d = (sum - g) - g * expm1f(lp);
+            if (bonus != 0.0f) d -= bonus * __builtin_amdgcn_exp2f(lp * kLog2e) * (lp + a.entropy[row]);
+            given[j] = d * a.per_temperature;
+        } else {
+            given[j] = gradient(x) + sum * a.per_temperature;
+        }
     }
     if (a.n) __syncthreads();  // given tokens' logits have been read
 

@@ -5,7 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from head_reference import pack
+from head_reference import F32, pack
 from logprobs_reference import gradient, logprobs
 
 pytestmark = pytest.mark.gpu
@@ -153,6 +153,46 @@ def test_temperatures(lib, dtype, temperature):
 def test_rows_anywhere(lib, offset, gap, dtype):
     print(f"case {offset} {gap} {dtype}", flush=True)
     check(lib, make(3, 4, 5003, dtype, mask="token", n=1, offset=offset, gap=gap), dtype, top=5)
+
+
+@pytest.mark.parametrize("N,V,mask", [(1, 128_256, "none"), (3, 5001, "class"), (4, 70_001, "token"), (800, 4000, "class")])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_certain_rows(lib, N, V, mask, dtype):
+    """Rows of which one token has nearly all: what is left of 1 is their log probability, entropy and gradient, and is as exact relative to itself"""
+    print(f"case {N} {V} {mask} {dtype}", flush=True)
+    s = make(15, N, V, dtype, mask=mask, n=1)
+    rng = np.random.default_rng(1)
+    rows = [0, N - 1] if N < 5 else [0, 5, N - 1]
+    for i in rows:
+        if s["allowed"][i].any():
+            best = rng.choice(np.flatnonzero(s["allowed"][i]))
+            s["tokens"][i] = best
+            s["logits"][i, int(best)] = 24.0 + 6 * rng.random()
+    s["x"] = s["logits"].double().cpu().numpy()
+    lp, h, st, _, _, grad = check(lib, s, dtype, rows=rows)
+    r = logprobs(s["x"][rows], s["tokens"][rows], s["allowed"][rows], 1.0, 0)
+    for k, i in enumerate(rows):
+        if not s["allowed"][i].any():
+            continue
+        # exactly, by the largest logit's token: its log p is log(1 - all others), and theirs are apart from it by d
+        others, d, t = r["p"][k].copy(), r["d"][k], int(s["tokens"][i, 0])
+        best = int(np.argmax(others))
+        others[best] = 0.0
+        top = np.log1p(-others.sum()) if others.sum() < 0.5 else r["log_p"][k, best]
+        want = top + d[t]
+        # the sum of all others is off relative to itself: terms as in logprobs(), d up to 40 here; its logarithm by two steps more
+        rounds = -(-V // (8 * 512))
+        rel = F32 * (6 * 60 + 6 * (rounds + 2) + 4 + 8 * rounds + 24 + 8)
+        assert abs(float(lp[k, 0]) - want) <= rel * (abs(top) + abs(d[t])) + 2.0 ** -126, (i, float(lp[k, 0]), want)
+        with np.errstate(all="ignore"):
+            entropy = -top * r["p"][k, best] - np.where(others > 0, others * (np.where(others > 0, d, 0.0) + top), 0.0).sum()
+        assert abs(float(h[k]) - entropy) <= 3 * rel * entropy + 2.0 ** -120, (i, float(h[k]), entropy)
+        left = others.sum() if t == best else 1.0 - r["p"][k, t]
+        if dtype == "f32":  # with an entropy bonus in it: what both give to the token, each as exact
+            g, ge = float(s["g"][i, 0]), float(s["ge"][i])
+            parts = abs(g) * left + abs(ge) * entropy + abs(ge * want)
+            exact = g * left - ge * (1 - left) * (want + entropy)
+            assert abs(float(grad[i, t]) - exact) <= 8 * rel * parts + 2.0 ** -120, (i, float(grad[i, t]), exact)
 
 
 def test_many_classes(lib):
