@@ -113,6 +113,19 @@ def test_largest_tiles_and_few_rows(lib, N, M, D):
     check(lib, make(11, N, M, D, "bf16"), "bf16", "silu")
 
 
+def test_offsets_beyond_32_bits(lib):
+    """Results that begin more than 2^31 elements behind the first one"""
+    N, M, D = 140_000, 16_384, 64
+    s = make(12, N, M, D, "bf16", bias=True, residual=False)
+    out, slope = lib.cfgzip_head_layer(s["x"], s["w"], s["b"], activation="silu", want_slope=True)
+    y, y_err, sl, sl_err = forward(s["x"][-200:].double(), s["w"].double(), s["b"].double(), "silu", None, "bf16")
+    within(out[-200:], y, y_err, "out")
+    within(slopes(slope[-200:]), sl, sl_err, "slope")
+    gh = lib.cfgzip_head_layer_grad(s["x"], s["w"], s["g"], slope=slope, want_weight=False)[0]
+    want = gradients(s["x"][-200:].double(), s["w"].double(), s["g"][-200:].double(), slopes(slope[-200:]), "bf16", False)
+    within(gh[-200:], *want["grad_hidden"], "grad_hidden")
+
+
 def test_odd_weights_in_large_tiles(lib):
     check(lib, make(5, 1000, 1111, 777, "bf16", w_offset=1), "bf16", "relu")
     check(lib, make(5, 1000, 1111, 777, "f16", w_gap=2), "f16", "relu")

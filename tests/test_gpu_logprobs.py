@@ -195,6 +195,26 @@ def test_certain_rows(lib, N, V, mask, dtype):
             assert abs(float(grad[i, t]) - exact) <= 8 * rel * parts + 2.0 ** -120, (i, float(grad[i, t]), exact)
 
 
+def test_offsets_beyond_32_bits(lib):
+    """Rows that begin more than 2^31 elements behind the first one"""
+    N, V = 17_000, 128_256
+    x = torch.zeros((N, V), dtype=torch.bfloat16, device="cuda")
+    s = make(16, 2, V, "bf16", n=1)
+    x[N - 2:] = s["logits"]
+    tokens = torch.zeros((N, 1), dtype=torch.int32, device="cuda")
+    tokens[N - 2:] = torch.from_numpy(s["tokens"]).cuda()
+    g = torch.zeros((N, 1), device="cuda")
+    g[N - 2:] = torch.from_numpy(s["g"]).cuda()
+    lp, h, st, tt, tl = lib.cfgzip_token_logprobs(x, tokens, top=5)
+    lib.cfgzip_token_logprobs_grad(x, tokens, lp, st, g, grad_logits=x)
+    r = logprobs(s["x"], s["tokens"], s["allowed"], 1.0, 5)
+    within(lp[N - 2:], r["logprob"], r["logprob_err"], "logprob")
+    within(h[N - 2:], r["entropy"], r["entropy_err"], "entropy")
+    assert (tt[N - 2:].cpu().numpy() == r["top_tokens"]).all()
+    within(x[N - 2:], *gradient(r, s["tokens"], s["g"].astype(np.float64), None, 1.0, "bf16"), "grad_logits")
+    assert not x[:N - 2].any()
+
+
 def test_many_classes(lib):
     """Masks over more classes than LDS holds"""
     check(lib, make(4, 3, 300_000, "bf16", mask="class", C=280_000, n=2), "bf16", top=9)
