@@ -76,7 +76,8 @@ struct Activation {
             slope = __builtin_fmaf(z * 0.39894228040143267794f, bell, q);
             return z * q;
         } else {
-            const float zz = z * z, u = z * __builtin_fmaf(b, zz, a);
+            const float zz = __builtin_fminf(z * z, 1e30f);  // (an infinity is no factor of b = 0, and q is 0 or 1 from far less on)
+            const float u = z * __builtin_fmaf(b, zz, a);
             const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -kLog2e));
             slope = __builtin_fmaf(z * q * (1.0f - q), __builtin_fmaf(3.0f * b, zz, a), q);
             return z * q;

@@ -88,6 +88,21 @@ def test_large_arguments(lib, name, size):
     check(lib, s, "bf16", name, f32=True)
 
 
+@pytest.mark.parametrize("N", [5, 200])
+@pytest.mark.parametrize("name", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("size", [1e5, 1e12, 1e17])
+def test_arguments_whose_squares_are_no_numbers(lib, size, name, N):
+    """z of 1e10 to 1e34: z or 0, with slopes of 1 or 0"""
+    s = make(17, N, 72, 24, "bf16", bias=False, residual=False)
+    s["x"].mul_(size)
+    s["w"].mul_(size)
+    out, slope = lib.cfgzip_head_layer(s["x"], s["w"], activation=name, want_slope=True)
+    z, z_err = forward(s["x"].double(), s["w"].double(), None, None, None, "bf16")[:2]
+    assert float(z.abs().min()) > 1e3
+    within(out, z.clamp(min=0.0), z_err, "out")
+    assert (slope == torch.where(z > 0, 1 << 14, 0)).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("N", [7, 150])
 @pytest.mark.parametrize("offset,gap,w_offset,w_gap", [(0, 8, 0, 8), (1, 0, 0, 0), (0, 3, 1, 0), (8, 8, 4, 4), (3, 6, 3, 2), (0, 0, 0, 5)])
