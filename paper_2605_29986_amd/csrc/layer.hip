@@ -433,10 +433,10 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewArgs a, Forwar
 __global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t *x, int64_t x_ld, int32_t N, int32_t D, uint16_t *y, int32_t y_ld,
                                                         int32_t all) {
     const int32_t units = y_ld / 8;
-    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (k >= (int64_t)all * units) return;
-    const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
-    *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = eight(x + row * x_ld + c, row < N ? D - c : 0);
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < (int64_t)all * units; k += gridDim.x * 256u) {
+        const int32_t row = (int32_t)(k / units), c = (int32_t)(k % units) * 8;
+        *reinterpret_cast<u32x4 *>(y + (int64_t)row * y_ld + c) = eight(x + row * x_ld + c, row < N ? D - c : 0);
+    }
 }
 
 struct DzArgs {
@@ -733,8 +733,8 @@ int check_call(const Call &c) {
 
 int copy_rows(const Call &c, uint16_t *y, int32_t y_ld, int32_t all, hipStream_t stream) {
     const int64_t units = (int64_t)all * (y_ld / 8);
-    hipLaunchKernelGGL(copy_rows_kernel, dim3((uint32_t)ceil_div(units, 256)), dim3(256), 0, stream, c.x(), c.hidden_stride, c.N, c.D, y, y_ld,
-                       all);
+    const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(units, 256), 1 << 16);  // (of many rows units are more than threads can be)
+    hipLaunchKernelGGL(copy_rows_kernel, dim3(grid), dim3(256), 0, stream, c.x(), c.hidden_stride, c.N, c.D, y, y_ld, all);
     return check_launch();
 }
 

@@ -141,6 +141,29 @@ def test_offsets_beyond_32_bits(lib):
     within(gh[-200:], *want["grad_hidden"], "grad_hidden")
 
 
+def test_offsets_beyond_32_bits_in_the_weights_gradient(lib):
+    """Only the last rows have gradients"""
+    N, M, D = 140_000, 16_384, 64
+    s = make(13, N, M, D, "bf16", bias=True, residual=False)
+    s["g"][:-200] = 0
+    slope = lib.cfgzip_head_layer(s["x"], s["w"], s["b"], activation="gelu", want_slope=True)[1]
+    _, gw, gb = lib.cfgzip_head_layer_grad(s["x"], s["w"], s["g"], slope=slope, want_hidden=False, want_bias=True)
+    want = gradients(s["x"][-200:].double(), s["w"].double(), s["g"][-200:].double(), slopes(slope[-200:]), "bf16", False)
+    within(gw, *want["grad_weight"], "grad_weight")
+    within(gb, *want["grad_bias"], "grad_bias")
+
+
+def test_many_odd_rows_are_copied(lib):
+    """More units than a copy has threads"""
+    N, M, D = 21_000, 24, 7_001
+    s = make(14, N, M, D, "bf16", bias=True, residual=False)
+    out = lib.cfgzip_head_layer(s["x"], s["w"], s["b"])[0]
+    gw = lib.cfgzip_head_layer_grad(s["x"], s["w"], s["g"], want_hidden=False)[1]
+    x, w, b, g = (s[k].double() for k in "xwbg")
+    within(out, *forward(x, w, b, None, None, "bf16")[:2], "out")
+    within(gw, *gradients(x, w, g, None, "bf16", True)["grad_weight"], "grad_weight")
+
+
 def test_odd_weights_in_large_tiles(lib):
     check(lib, make(5, 1000, 1111, 777, "bf16", w_offset=1), "bf16", "relu")
     check(lib, make(5, 1000, 1111, 777, "f16", w_gap=2), "f16", "relu")
