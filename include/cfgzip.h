@@ -590,7 +590,8 @@ int cfgzip_token_logprobs_grad(const void *logits, int32_t dtype, int32_t N, int
  * dz is rounded to the inputs' type (not for grad_bias, and not where slope is NULL and grad_out of that type); in F16 it is brought into range by a
  * power of two first, so grad_out may be of any size: what is less than 2^-38 of its largest counts as multiples of that.
  * All sums are fp32, and nothing is added in an order that changes from call to call.  N = 0 enqueues nothing (grad_weight and grad_bias
- * are set to 0).  At most 2^21 rows; M, D and the weights' stride below 2^22.  Results must not overlap inputs or each other, but for the residual.
+ * are set to 0).  At most 2^21 rows; M, D and the weights' stride below 2^22.  Results must not overlap inputs or each other, but for the
+ * residual; those that begin where one of these does are refused.
  */
 #define CFGZIP_ACT_NONE 0
 #define CFGZIP_ACT_RELU 1

@@ -9,6 +9,7 @@
 // Up to 16 rows it is reading the weights that counts: a workgroup's 16 waves split the k of 16 rows of weights, each with loads of its own
 // straight to registers, and join through LDS.
 #include <algorithm>
+#include <initializer_list>
 
 #include "gemm16.hpp"
 
@@ -835,6 +836,15 @@ int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t
     return CFGZIP_OK;
 }
 
+// A result in the place of something that is read while it is written.  (Only what begins at the same place is looked for: rows of others may lie between.)
+bool same_place(std::initializer_list<const void *> results, std::initializer_list<const void *> inputs) {
+    for (const void *const *r = results.begin(); r != results.end(); ++r) {
+        if (!*r) continue;
+        if (std::find(inputs.begin(), inputs.end(), *r) != inputs.end() || std::find(results.begin(), r, *r) != r) return true;
+    }
+    return false;
+}
+
 bool size_ok(int32_t N, int32_t M, int32_t D) {
     return N > 0 && M > 0 && D > 0 && N <= kMaxRows && M < kMaxStride - 64 && D < kMaxStride - 64;
 }
@@ -879,6 +889,8 @@ extern "C" int cfgzip_head_layer(const void *hidden, int64_t hidden_stride, cons
     if (!out || !aligned_to(out, f32 ? 4 : 2)) return CFGZIP_E_INVALID;
     const size_t need = cfgzip_head_layer_workspace_bytes(N, M, D);
     if (need && (!ws || !aligned_to(ws, 256) || ws_bytes < need)) return CFGZIP_E_WORKSPACE;
+    if (same_place({out, slope}, {hidden, weight, bias}) || (slope && slope == residual)) return CFGZIP_E_INVALID;
+    if (out == residual && (f32 || out_stride != residual_stride)) return CFGZIP_E_INVALID;
     const double a = 2.0 * 0.79788456080286535588;  // 2 sqrt(2 / pi)
     const bool tanh = activation == CFGZIP_ACT_GELU_TANH;
     const Activation act{activation,
@@ -920,6 +932,7 @@ extern "C" int cfgzip_head_layer_grad(const void *hidden, int64_t hidden_stride,
     const bool f32 = grad_out_dtype == CFGZIP_DTYPE_F32;
     if (!grad_out || !aligned_to(grad_out, f32 ? 4 : 2) || grad_out_stride < M) return CFGZIP_E_INVALID;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cfgzip_head_layer_grad_workspace_bytes(N, M, D)) return CFGZIP_E_WORKSPACE;
+    if (same_place({grad_hidden, grad_weight, grad_bias}, {hidden, weight, grad_out, slope})) return CFGZIP_E_INVALID;
     const Grads g{grad_out, grad_out_stride, f32, static_cast<const uint16_t *>(slope), slope_stride, static_cast<uint16_t *>(grad_hidden),
                   static_cast<uint16_t *>(grad_weight), static_cast<uint16_t *>(grad_bias), grad_hidden_stride, grad_weight_stride};
     Carver carve(ws);

@@ -62,6 +62,18 @@ def test_refusals(raw, memory):
     assert _grad(raw, p, N=0, hidden=None, g=None, gw=None, gb=None) == 0
 
 
+def test_results_in_the_place_of_inputs(raw, memory):
+    p = memory[0]
+    apart = dict(hidden=p, weight=p + 256, bias=p + 512, residual=p + 768, out=p + 1024, slope=p + 1280)
+    for change in (dict(out=p), dict(out=p + 256), dict(out=p + 512), dict(slope=p), dict(slope=p + 768), dict(slope=p + 1024),
+                   dict(out=p + 768, os=12), dict(out=p + 768, out_dtype=0)):
+        assert _layer(raw, p, **{**apart, **change}) == -1, change
+    apart = dict(hidden=p, weight=p + 256, g=p + 512, slope=p + 768, gh=p + 1024, gw=p + 1280, gb=p + 1536)
+    for change in (dict(gh=p), dict(gh=p + 512), dict(gw=p + 256), dict(gw=p), dict(gw=p + 512), dict(gb=p + 768), dict(gh=p + 1280),
+                   dict(gb=p + 1024)):
+        assert _grad(raw, p, **{**apart, **change}) == -1, change
+
+
 def test_workspace_queries(raw):
     q, g = raw.cfgzip_head_layer_workspace_bytes, raw.cfgzip_head_layer_grad_workspace_bytes
     for f in (q, g):
