@@ -13,9 +13,10 @@
 // A row that is nearly certain has S = 1 and very little, and that little is its log probability, its entropy and its gradient: so S is kept
 // without the largest logit's 1, and where the rest is small the thread that met that logit has its units added up again without it.
 //
-// Alternatives cost the pass nothing: the k-th largest of 64 threads' (or groups of threads') maxima is a bound that k logits at the least reach,
-// so only threads whose maximum reaches it can have had one of the k best.  Their few units are read again (from a cache), what reaches
-// the bound is put together and sorted.  A logit is compared by (value, lower token first) as one 64-bit number.
+// Alternatives cost the pass little: the k-th largest of threads' (or groups of threads') maxima is a bound that k logits at the least reach,
+// so only threads whose maximum reaches it can have had one of the k best.  A thread leaves the maxima of its units in LDS, in 16 bits and no less
+// than they are; units whose maximum reaches the bound are read again, what reaches it itself is put together and sorted.  A
+// logit is compared by (value, lower token first) as one 64-bit number.
 #include <algorithm>
 
 #include "gemm16.hpp"
@@ -35,11 +36,17 @@ constexpr float kNoMore = -200.0f;  // 2^y is 0 from here on
 constexpr float kMargin = 11.5f;
 constexpr int kMaxTop = CFGZIP_MAX_TOP;
 constexpr int kCandidates = 1024;
+constexpr int kSlots = 32;  // of a thread's maxima in LDS.  (All units of threads that reach the bound read again: 256 x 128,256 bf16, 64 best 72 us for 46.)
+// Up to so many the bound comes from 64 groups of threads, 0.4 us shorter; 64 best have 300 candidates with that one, 70 with that of all threads (46 us
+// for 33, one row 20 for 14).
+constexpr int kFewBest = 32;
 constexpr int32_t kMaskWords = 4096;  // of a mask over classes in LDS, two rows of them; larger ones are read where they lie
 constexpr int32_t kMaxTokens = CFGZIP_MAX_TOKENS, kMaxRows = 1 << 22;  // (a launch has fewer than 2^32 threads)
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+
+static_assert(kThreads * 10 + kCandidates * 10 + 1024 + kMaskWords * 4 + kSlots * kThreads * 2 <= 65536, "LDS of a launch with alternatives");
 
 // where a mask comes from
 enum : int { ALL = 0, TOKENS = 1, CLASSES = 2, CLASSES_FAR = 3 };
@@ -276,6 +283,7 @@ struct ScoreArgs {
     const int32_t *tokens;     // [N][n]
     int32_t n, top;
     int32_t splits, per;  // of a row's units, `per` to a workgroup
+    int32_t slot_shift;   // a slot is for 2^slot_shift units of a thread
     float *logprob, *entropy;
     f32x2_any *stats;
     int32_t *top_tokens;
@@ -326,6 +334,14 @@ __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, const
     }
 }
 
+// the upper half of a float that is no less, and of bf16 logits the same
+template <int DTYPE>
+__device__ __forceinline__ uint16_t upper_half(float x) {
+    uint32_t b = __builtin_bit_cast(uint32_t, x);
+    if constexpr (DTYPE != CFGZIP_DTYPE_BF16) b += ~((int32_t)b >> 31) & 0xFFFF;
+    return (uint16_t)(b >> 16);
+}
+
 // Units of a thread and row on their way at a time: 64 bytes of logits, of two rows 32 each.
 template <int DTYPE, int ROWS>
 constexpr int kAhead = (DTYPE == CFGZIP_DTYPE_F32 ? 2 : 4) / ROWS;
@@ -338,8 +354,9 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
     __shared__ Sums shared_sums[ROWS][kWaves];
     __shared__ float shared_most[ROWS][kWaves];
     __shared__ uint64_t keys[TOP ? kThreads : 1], candidates[TOP ? kCandidates : 1];
-    __shared__ uint16_t again[TOP ? kThreads : 1];
-    __shared__ int32_t count[2];
+    __shared__ uint16_t again[TOP ? kThreads : 1], listed[TOP ? kCandidates : 1];
+    __shared__ int32_t count[3];
+    uint16_t *const slots = reinterpret_cast<uint16_t *>(mask + (MASK == CLASSES ? a.l.words * ROWS : 0));
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t row = (int64_t)(blockIdx.x / a.splits) * ROWS;
     const int32_t split = (int32_t)(blockIdx.x % a.splits), units = (a.l.V + 7) / 8;
@@ -355,7 +372,9 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) most[r] = limit[r] = -kInf, at[r] = 0, sums[r] = Sums{0.0f, 0.0f, 0.0f};
     constexpr int kUnits = kAhead<DTYPE, ROWS>;
-    for (int32_t u = u0 + threadIdx.x; u < u1; u += kThreads * kUnits) {
+    int32_t round = 0;
+    float slot_most = -kInf;
+    for (int32_t u = u0 + threadIdx.x; u < u1; u += kThreads * kUnits, round += kUnits) {
         Unit<DTYPE> x[ROWS][kUnits];
         Admitted<MASK, ROWS> admitted[kUnits];
 #pragma unroll
@@ -377,6 +396,10 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
                 const float here = larger_of(larger_of(larger_of(v[0], v[1], v[2]), v[3], v[4]), larger_of(v[5], v[6], v[7]));
                 at[r] = here > most[r] ? u + i * kThreads : at[r];
                 most[r] = larger_of(most[r], here);
+                if constexpr (TOP) {
+                    slot_most = ((round + i) & ((1 << a.slot_shift) - 1)) == 0 ? here : larger_of(slot_most, here);
+                    slots[((round + i) >> a.slot_shift) * kThreads + threadIdx.x] = upper_half<DTYPE>(slot_most);
+                }
                 if (here > limit[r]) {
                     sums[r].raise(here, a.c);
                     limit[r] = here + margin;
@@ -456,21 +479,52 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
         uint64_t best = 0;
         if constexpr (TOP) {
             keys[threadIdx.x] = most[r] > -kInf ? key_of(most[r], at[r]) : 0;
-            if (threadIdx.x < 2) count[threadIdx.x] = 0;
+            if (threadIdx.x < 3) count[threadIdx.x] = 0;
             __syncthreads();
-            // every wave works out the bound, from the largest of the threads of each lane
-            uint64_t key = keys[lane];
-#pragma unroll
-            for (int i = 1; i < kWaves; ++i) key = keys[lane + i * kWave] > key ? keys[lane + i * kWave] : key;
-            const uint64_t bound = __shfl((unsigned long long)sorted(key, lane), a.top - 1);
             const uint64_t mine = keys[threadIdx.x];
+            // the bound, in the place of candidates
+            if (a.top > kFewBest) {  // from all threads' largest
+                uint64_t key = sorted(mine, lane);
+                candidates[threadIdx.x] = key;
+                for (int half = kWaves / 2; half > 0; half /= 2) {
+                    __syncthreads();
+                    if (wave < half) candidates[threadIdx.x] = key = merged(key, candidates[(wave + half + 1) * kWave - 1 - lane], lane);
+                }
+            } else if (wave == 0) {  // from the largest of the threads of each lane
+                uint64_t key = mine;
+#pragma unroll
+                for (int i = 1; i < kWaves; ++i) key = keys[lane + i * kWave] > key ? keys[lane + i * kWave] : key;
+                candidates[lane] = sorted(key, lane);
+            }
+            __syncthreads();
+            const uint64_t bound = candidates[a.top - 1];
             if (mine != 0 && mine >= bound) again[atomicAdd(&count[0], 1)] = (uint16_t)threadIdx.x;
             __syncthreads();
             const uint32_t bound_value = (uint32_t)(bound >> 32), bound_unit = ~(uint32_t)bound;
-            const int32_t rounds = (u1 - u0 + kThreads - 1) / kThreads, items = count[0] * rounds;
+            const int32_t rounds = (u1 - u0 + kThreads - 1) / kThreads, of_thread = (rounds + (1 << a.slot_shift) - 1) >> a.slot_shift;
+            const int32_t all_slots = count[0] * of_thread;
+            auto slot_of = [&](int32_t i) { return again[i / of_thread] + i % of_thread * kThreads; };
+            auto first_of = [&](int32_t slot) { return u0 + slot % kThreads + ((slot / kThreads) << a.slot_shift) * kThreads; };
+            // Where slots are many, those that reach the bound: each is a line of memory.
+            bool list = all_slots > kThreads;
+            if (list) {
+                for (int32_t i = threadIdx.x; i < all_slots; i += kThreads) {
+                    const int32_t slot = slot_of(i), first = first_of(slot);
+                    const float z = __builtin_bit_cast(float, (uint32_t)slots[slot] << 16);
+                    const uint32_t order = order_of(z);
+                    if (first < u1 && z != -kInf && (order > bound_value || (order == bound_value && (uint32_t)first <= bound_unit))) {
+                        const int32_t to = atomicAdd(&count[2], 1);
+                        if (to < kCandidates) listed[to] = (uint16_t)slot;
+                    }
+                }
+                __syncthreads();
+                list = count[2] <= kCandidates;
+            }
+            const int32_t items = (list ? count[2] : all_slots) << a.slot_shift;
             // f(key) of the unit's logits that reach the bound
             auto look_again = [&](int32_t item, auto &&f) CFGZIP_INLINE {
-                const int32_t u = item < items ? u0 + again[item / rounds] + item % rounds * kThreads : u1;
+                const int32_t i = item >> a.slot_shift;
+                const int32_t u = item < items ? first_of(list ? listed[i] : slot_of(i)) + (item & ((1 << a.slot_shift) - 1)) * kThreads : u1;
                 Unit<DTYPE> x;
                 Admitted<MASK, ROWS> admitted;
                 if (u < u1) {
@@ -711,7 +765,7 @@ __global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(GradArgs a)
 // split costs a launch that joins its parts, and each workgroup 0.6 us at its end, 1.6 with alternatives.  48 x 32,000 bf16 under masks over
 // classes: whole 7.3 us, in two 9.7; 300 x 128,256 35.1, in two 31.1, three 29.1, four 28.2, sixteen 35.7; 256: 25.0, 24.7, 24.2, 24.6; 1,024: 69, 71, 73, 75.
 // Two rows to a workgroup go under masks over classes where rows are many (128,256: 128 rows 14.0 one by one and 15.5 in twos, 256 24.2 and 22.1,
-// 1,024 69 and 57); not with alternatives, which take 6 us for each row at the workgroup's end (256: 26.7 and 29.6).
+// 1,024 69 and 57); not with alternatives, which take 4 us for each row at the workgroup's end (256: 31 and 36; 512: 45 and 52; 1,024 77 and 77).
 struct Plan {
     int32_t rows, splits;
 };
@@ -823,9 +877,12 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
     a.dtype = dtype;
     a.c = (float)(kLog2eD / temperature), a.per_temperature = (float)(1.0 / temperature);
     a.tokens = tokens, a.n = n, a.top = top;
-    const Plan plan = plan_of(N, V, top, mask_of(c) == CLASSES);
+    const int mask = mask_of(c);
+    const Plan plan = plan_of(N, V, top, mask == CLASSES);
     a.per = (int32_t)ceil_div(ceil_div(V, 8), plan.splits);
     a.splits = (int32_t)ceil_div(ceil_div(V, 8), a.per);
+    const int64_t rounds = ceil_div(a.per, kThreads);
+    while (ceil_div(rounds, 1 << a.slot_shift) > kSlots) ++a.slot_shift;
     a.logprob = logprob, a.entropy = entropy, a.stats = reinterpret_cast<f32x2_any *>(stats), a.top_tokens = top_tokens, a.top_logprobs = top_logprobs;
     Carver carve(ws);
     if (a.splits > 1) {
@@ -833,11 +890,11 @@ extern "C" int cfgzip_token_logprobs(const void *logits, int32_t dtype, int32_t 
         a.part_keys = carve.take<uint64_t>((size_t)N * a.splits * top);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int mask = mask_of(c);
     CFGZIP_TRY(with(dtype, mask, [&](auto type, auto kind) {
         auto launch = [&](auto r) {
             const dim3 grid((uint32_t)ceil_div(N, r.value) * a.splits);
-            const uint32_t lds = kind.value == CLASSES ? (uint32_t)a.l.words * 4 * r.value : 0;
+            uint32_t lds = kind.value == CLASSES ? (uint32_t)a.l.words * 4 * r.value : 0;
+            if (top) lds += (uint32_t)ceil_div(rounds, 1 << a.slot_shift) * kThreads * 2;
             if constexpr (r.value == 1)
                 if (top) {
                     hipLaunchKernelGGL((score_kernel<type.value, kind.value, true, 1>), grid, dim3(kThreads), lds, s, a);

@@ -220,6 +220,23 @@ def test_many_classes(lib):
     check(lib, make(4, 3, 300_000, "bf16", mask="class", C=280_000, n=2), "bf16", top=9)
 
 
+@pytest.mark.parametrize("dtype,mask,top,C", [("bf16", "none", 64, 0), ("f16", "token", 33, 0), ("f32", "class", 20, 3000), ("bf16", "class", 50, 131_072)])
+def test_alternatives_of_long_rows(lib, dtype, mask, top, C):
+    """A thread has more units than slots, some of them behind the row's end"""
+    print(f"case {dtype} {mask} top={top}", flush=True)
+    check(lib, make(18, 200, 270_001, dtype, mask, n=1, C=C), dtype, top=top, rows=[0, 1, 2, 101, 199])
+
+
+@pytest.mark.parametrize("N,V", [(260, 131_000), (3, 20_000)])
+@pytest.mark.parametrize("top", [5, 24, 64])
+def test_alternatives_that_differ_in_their_last_bits(lib, N, V, top):
+    """Of fp32 logits that are one value in fewer bits, all slots look as if they had one of the best"""
+    s = make(19, N, V, "f32", n=1)
+    s["logits"].mul_(2.0 ** -12).add_(1.0 if top != 24 else -1.0)
+    s["x"] = s["logits"].double().cpu().numpy()
+    check(lib, s, "f32", top=top, rows=[0, 1, N - 1])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_large_logits_in_a_few_threads(lib, dtype):
     """The best logits lie in units that the same few threads take: more of them than there is room to put together"""
