@@ -254,16 +254,15 @@ struct Way {
     static __device__ __forceinline__ int at(int r, int u) { return r * (kLanes * 16) + ((u ^ (r & 7)) * 16); }
 };
 
+// One of `blocks` workgroups' part of a product.
 template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
-__global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E end) {
+__device__ __forceinline__ void make_product(const ProductArgs &a, const E &end, const Stage (&lds)[4], lds_char *way, uint32_t block, uint32_t blocks) {
     // (B goes on with zeros to the end of a step, so what A has there only has to be finite; hidden states by columns go on with zeros too: with
     // ANY the largest tile's addresses are out of the registers, 122 of them)
     using TileA = Tile<S::BM, S::kThreads, A_COLUMNS, A_DIRECT, A_COLUMNS && B_COLUMNS ? PADDED : ANY>;
     using TileB = Tile<S::BN, S::kThreads, B_COLUMNS, B_DIRECT, PADDED>;
-    CFGZIP_STAGES(S, lds);
-    __shared__ __attribute__((aligned(16))) char way[S::WM * S::WN * Way<S>::kBytes];
     auto place = [&](int32_t i, int32_t &tm, int32_t &tn, int32_t &split) CFGZIP_INLINE {
-        const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = blockIdx.x + i * gridDim.x;
+        const uint32_t total = (uint32_t)a.tiles_m * a.tiles_n * a.splits, t = block + i * blocks;
         if (t >= total) return false;
         tile_of(t, total, a.tiles_m, a.tiles_n * a.splits, tm, tn);
         split = tn / a.tiles_n;
@@ -282,7 +281,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
         place(i, tm, tn, split);
         using W = Way<S>;
         typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-        lds_char *const mine = (lds_char *)way + (wm * S::WN + wn) * W::kBytes;
+        lds_char *const mine = way + (wm * S::WN + wn) * W::kBytes;
         const int32_t m0 = tm * S::BM + wm * S::TM + lane % W::kLanes * 4, n0 = tn * S::BN + wn * S::TN + lane / W::kLanes;
         typename E::Column column{}, next_column{};
         typename E::Row row[W::kPasses], next[W::kPasses];
@@ -324,6 +323,13 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E e
         }
     };
     multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
+}
+
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, E end) {
+    CFGZIP_STAGES(S, lds);
+    __shared__ __attribute__((aligned(16))) char way[S::WM * S::WN * Way<S>::kBytes];
+    make_product<T, S, A_COLUMNS, B_COLUMNS, A_DIRECT, B_DIRECT>(a, end, lds, (lds_char *)way, blockIdx.x, gridDim.x);
 }
 
 // Adds up the shares of a sum that was split.
@@ -597,23 +603,59 @@ __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
     }
 }
 
+struct BiasArgs {
+    const float *sums;  // [blocks][ld]
+    int32_t blocks, ld, M;
+    uint16_t *out;
+};
 // A workgroup has 64 columns, a wave every fourth block of rows.
 template <typename T>
-__global__ __launch_bounds__(256) void bias_kernel(const float *sums, int32_t blocks, int32_t ld, int32_t M, uint16_t *out) {
-    __shared__ float shared[4][kWave];
+__device__ __forceinline__ void add_up_bias(const BiasArgs &a, float (&shared)[4][kWave], uint32_t block) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int32_t c = blockIdx.x * kWave + lane;  // (ld is whole steps of 64 columns)
+    const int32_t c = block * kWave + lane;  // (ld is whole steps of 64 columns)
     float x = 0.0f;
-    for (int32_t b = wave; b < blocks; b += 32) {
+    for (int32_t b = wave; b < a.blocks; b += 32) {
         float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = b + 4 * i < blocks ? sums[(int64_t)(b + 4 * i) * ld + c] : 0.0f;
+        for (int i = 0; i < 8; ++i) y[i] = b + 4 * i < a.blocks ? a.sums[(int64_t)(b + 4 * i) * a.ld + c] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x += y[i];
     }
     shared[wave][lane] = x;
     __syncthreads();
-    if (wave == 0 && c < M) out[c] = T::round((shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]));
+    if (wave == 0 && c < a.M) a.out[c] = T::round((shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]));
+}
+template <typename T>
+__global__ __launch_bounds__(256) void bias_kernel(BiasArgs a) {
+    __shared__ float shared[4][kWave];
+    add_up_bias<T>(a, shared, blockIdx.x);
+}
+
+// All that comes of dz in one launch, where the tiles of each product are few and small: the workgroups of one fill what those of the other leave.
+struct AllArgs {
+    ProductArgs hidden, weight;
+    Gradient hidden_end, weight_end;
+    uint32_t hidden_blocks, weight_blocks;  // behind them those of the bias
+    BiasArgs bias;
+};
+template <typename T, bool X_DIRECT>
+__global__ __launch_bounds__(ShapeSmall::kThreads) void all_gradients_kernel(AllArgs a) {
+    using S = ShapeSmall;
+    static_assert(S::kThreads == 256, "as many as the bias's sums take");
+    CFGZIP_STAGES(S, lds);
+    __shared__ __attribute__((aligned(16))) char way[S::WM * S::WN * Way<S>::kBytes];
+    static_assert(sizeof(way) >= sizeof(float[4][kWave]), "what the bias's sums take");
+    uint32_t block = blockIdx.x;
+    if (block < a.weight_blocks) {
+        make_product<T, S, true, true, X_DIRECT, true>(a.weight, a.weight_end, lds, (lds_char *)way, block, a.weight_blocks);
+        return;
+    }
+    block -= a.weight_blocks;
+    if (block < a.hidden_blocks) {
+        make_product<T, S, true, false, true, true>(a.hidden, a.hidden_end, lds, (lds_char *)way, block, a.hidden_blocks);
+        return;
+    }
+    add_up_bias<T>(a.bias, *reinterpret_cast<float(*)[4][kWave]>(way), block - a.hidden_blocks);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t *out, int64_t out_ld, int32_t n, int32_t D) {
@@ -669,13 +711,20 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool all) {
     return p;
 }
 
-template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
-int launch_product_of(ProductArgs a, const E &end, hipStream_t stream) {
+// the workgroups of a product (0: it has too many tiles)
+template <typename S>
+uint32_t blocks_of(ProductArgs &a) {
     a.tiles_m = (int32_t)ceil_div(a.m, S::BM);
     a.tiles_n = (int32_t)ceil_div(a.n, S::BN);
-    const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits, grid = std::min(work, slots<S>());
-    if (work > 0x7FFFFFFF - slots<S>()) return CFGZIP_E_TOO_LARGE;
-    hipLaunchKernelGGL((product_kernel<T, S, A_COLUMNS, B_COLUMNS, A_DIRECT, B_DIRECT, E>), dim3((uint32_t)grid), dim3(S::kThreads), 0, stream, a, end);
+    const int64_t work = (int64_t)a.tiles_m * a.tiles_n * a.splits;
+    return work > 0x7FFFFFFF - slots<S>() ? 0 : (uint32_t)std::min(work, slots<S>());
+}
+
+template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
+int launch_product_of(ProductArgs a, const E &end, hipStream_t stream) {
+    const uint32_t grid = blocks_of<S>(a);
+    if (grid == 0) return CFGZIP_E_TOO_LARGE;
+    hipLaunchKernelGGL((product_kernel<T, S, A_COLUMNS, B_COLUMNS, A_DIRECT, B_DIRECT, E>), dim3(grid), dim3(S::kThreads), 0, stream, a, end);
     return check_launch();
 }
 
@@ -804,35 +853,44 @@ int backward(const Call &c, const Grads &g, bool direct, Carver &ws, hipStream_t
         if (g.f32) hipLaunchKernelGGL((dz_kernel<T, true>), grid, dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((dz_kernel<T, false>), grid, dim3(256), 0, stream, a);
         CFGZIP_TRY(check_launch());
-        if (g.bias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((uint32_t)ceil_div(c.M, kWave)), dim3(256), 0, stream, sums, blocks, m_pad, c.M, g.bias);
-            CFGZIP_TRY(check_launch());
-        }
     }
+    const BiasArgs bias{sums, blocks, m_pad, c.M, g.bias};
+    const uint32_t bias_blocks = g.bias ? (uint32_t)ceil_div(c.M, kWave) : 0;
     const uint16_t *const d = as_it_is ? static_cast<const uint16_t *>(g.grad_out) : dz;
     const int64_t d_ld = as_it_is ? g.grad_out_stride : m_pad;
+    const Gradient hidden_end{scaled ? unscale : nullptr, g.hidden, g.hidden_stride, c.D}, weight_end{scaled ? unscale : nullptr, g.weight, g.weight_stride, c.D};
+    const Plan hidden_plan = plan_of(c.D, c.N, c.M, direct), weight_plan = plan_of(c.D, c.M, c.N, true);
+    const bool x_as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.N % kStepK == 0 && c.hidden_stride < kMaxStride;
+    const bool odd = !x_as_it_is && weight_plan.tiles == Tiles::SMALL && c.hidden_stride < kMaxStride;
+    if (launch && g.weight && !x_as_it_is && !odd) CFGZIP_TRY(copy_rows(c, copy, d_units, n_pad, stream));
+    ProductArgs h{}, w{};
+    h.A = by_columns(c.w(), c.weight_stride, c.D);
+    h.B = by_rows(d, d_ld, c.N);
+    h.m = c.D, h.n = c.N, h.k = c.M;
+    w.A = x_as_it_is || odd ? by_columns(c.x(), c.hidden_stride, c.D) : by_columns(copy, d_units, d_units);
+    w.B = by_columns(d, d_ld, m_pad);
+    w.m = c.D, w.n = c.M, w.k = c.N;
+    if (launch && g.hidden && g.weight && direct && hidden_plan.tiles == Tiles::SMALL && weight_plan.tiles == Tiles::SMALL &&
+        hidden_plan.splits == 1 && weight_plan.splits == 1) {
+        AllArgs all{h, w, hidden_end, weight_end, 0, 0, bias};
+        for (ProductArgs *a : {&all.hidden, &all.weight}) a->k_split = (int32_t)pad(a->k, kStepK), a->splits = 1;
+        all.hidden_blocks = blocks_of<ShapeSmall>(all.hidden), all.weight_blocks = blocks_of<ShapeSmall>(all.weight);
+        if (!all.hidden_blocks || !all.weight_blocks) return CFGZIP_E_TOO_LARGE;
+        const dim3 grid(all.weight_blocks + all.hidden_blocks + bias_blocks);
+        if (odd) hipLaunchKernelGGL((all_gradients_kernel<T, false>), grid, dim3(ShapeSmall::kThreads), 0, stream, all);
+        else hipLaunchKernelGGL((all_gradients_kernel<T, true>), grid, dim3(ShapeSmall::kThreads), 0, stream, all);
+        return check_launch();
+    }
+    if (launch && g.bias) {
+        hipLaunchKernelGGL(bias_kernel<T>, dim3(bias_blocks), dim3(256), 0, stream, bias);
+        CFGZIP_TRY(check_launch());
+    }
     if (g.hidden || !launch) {
-        ProductArgs a{};
-        a.A = by_columns(c.w(), c.weight_stride, c.D);
-        a.B = by_rows(d, d_ld, c.N);
-        a.m = c.D, a.n = c.N, a.k = c.M;
         Carver own = ws;
-        const Gradient end{scaled ? unscale : nullptr, g.hidden, g.hidden_stride, c.D};
-        CFGZIP_TRY((product<T, true, false>(a, plan_of(a.m, a.n, a.k, direct), end, direct ? Odd::NONE : Odd::A, own, stream, launch)));
+        CFGZIP_TRY((product<T, true, false>(h, hidden_plan, hidden_end, direct ? Odd::NONE : Odd::A, own, stream, launch)));
         if (!launch) ws.used = std::max(ws.used, own.used);
     }
-    if (g.weight || !launch) {
-        const bool x_as_it_is = whole_units(c.hidden, c.hidden_stride, c.D) && c.N % kStepK == 0 && c.hidden_stride < kMaxStride;
-        const Plan p = plan_of(c.D, c.M, c.N, true);
-        const bool odd = !x_as_it_is && p.tiles == Tiles::SMALL && c.hidden_stride < kMaxStride;
-        if (launch && !x_as_it_is && !odd) CFGZIP_TRY(copy_rows(c, copy, d_units, n_pad, stream));
-        ProductArgs a{};
-        a.A = x_as_it_is || odd ? by_columns(c.x(), c.hidden_stride, c.D) : by_columns(copy, d_units, d_units);
-        a.B = by_columns(d, d_ld, m_pad);
-        a.m = c.D, a.n = c.M, a.k = c.N;
-        const Gradient end{scaled ? unscale : nullptr, g.weight, g.weight_stride, c.D};
-        CFGZIP_TRY((product<T, true, true>(a, p, end, odd ? Odd::A : Odd::NONE, ws, stream, launch)));
-    }
+    if (g.weight || !launch) CFGZIP_TRY((product<T, true, true>(w, weight_plan, weight_end, odd ? Odd::A : Odd::NONE, ws, stream, launch)));
     return CFGZIP_OK;
 }
 
