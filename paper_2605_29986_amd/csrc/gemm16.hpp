@@ -351,6 +351,7 @@ __device__ __forceinline__ void wait_for_loads() {
 // What a workgroup multiplies: for each of its tiles, A's and B's first rows and the steps along k.
 struct Work {
     int32_t m0, n0, step0, k;  // k elements from step0 steps on
+    int32_t turn = 0;          // the step of them to begin with, where multiply() knows turns; only of whole steps
 };
 
 // Scales of what is multiplied, for operands that have them: those of two steps at a time (kStages of them), kept by the lane that has
@@ -365,8 +366,9 @@ struct NoScales {
 };
 
 // Makes tile after tile: work(i, Work &) says whether there is an i-th one and which, store(i, acc, ..) takes its sums.  While
-// the sums of one are stored the first steps of the next are on their way into LDS.
-template <typename T, typename S, typename TileA, typename TileB, typename W, typename E, typename X>
+// the sums of one are stored the first steps of the next are on their way into LDS.  TURNS: a tile may begin with another step than its first, and
+// goes on with that one behind its last.
+template <typename T, typename S, typename TileA, typename TileB, bool TURNS = false, typename W, typename E, typename X>
 __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, const Stage (&lds)[4], W &&work, E &&store, X &&scales) {
     constexpr bool kScaled = std::remove_reference_t<X>::kScaled;
     static_assert(!kScaled || S::kStages == 2, "scales of two steps at a time");
@@ -380,6 +382,7 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, con
     if (!work(0, w)) return;
     // of the loads: k from the step to be loaded next on; how many of them that step has; and of the step loaded last
     int32_t k_left, whole, loaded;
+    int32_t to_end;  // steps until a turned tile goes on with its first; below 1: it does not
     auto look = [&]() CFGZIP_INLINE {
         whole = kStepK;
         if (k_left < kStepK) {
@@ -393,13 +396,16 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &B, con
         if (k_left > kStepK) {  // else the base stays at elements that are there
             ta.base += ta.step;
             tb.base += tb.step;
+            if constexpr (TURNS)
+                if (--to_end == 0) ta.base -= w.k / kStepK * ta.step, tb.base -= w.k / kStepK * tb.step;
         }
         k_left -= kStepK;
         look();
     };
     auto start = [&]() CFGZIP_INLINE {
-        ta.init(A, w.m0, w.step0);
-        tb.init(B, w.n0, w.step0);
+        ta.init(A, w.m0, w.step0 + (TURNS ? w.turn : 0));
+        tb.init(B, w.n0, w.step0 + (TURNS ? w.turn : 0));
+        if constexpr (TURNS) to_end = w.turn ? w.k / kStepK - w.turn : 0;
         k_left = w.k;
         look();
     };

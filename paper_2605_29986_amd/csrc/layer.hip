@@ -6,7 +6,7 @@
 //
 // All three products are made in tiles on the matrix cores (gemm16.hpp); the tile's sums become results in the accumulators.  Where
 // the tiles are too few to fill the chip their sum over k is split, the shares are added up by a kernel that ends with the same epilogue.
-// Up to 16 rows it is reading the weights that counts: a workgroup's 16 waves split the k of 16 rows of weights, each with loads of its own
+// Of few rows it is reading the weights that counts: a workgroup's 16 waves split the k of 16 rows of weights, each with loads of its own
 // straight to registers, and join through LDS.
 #include <algorithm>
 #include <initializer_list>
@@ -22,6 +22,10 @@ using Shape128 = Shape<256, 128, 4, 2, 3>;
 using Shape256 = Shape<256, 256, 2, 2, 2>;
 
 constexpr int64_t kFewWeights = 1 << 22;
+// Of long sums the largest tiles' panels begin at different eighths: rows that lie far apart begin at the same memory channels, and all workgroups asked those
+// (4,096 x 4,096 x 16,384 with gelu_tanh 489 us and 436, gradient of hidden states of 4,096 x 16,384 x 4,096 402 and 393; of k = 4,096 no
+// difference).  Results of equal rows of hidden states stay equal.
+constexpr int32_t kTurned = 8192;
 constexpr int32_t kMaxRows = 1 << 21;  // (a launch goes over them in blocks of 64, fewer than 2^16)
 constexpr int64_t kComputeUnits = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -240,7 +244,7 @@ __device__ __forceinline__ f32x4 taken(const f32x4 &acc) {
 // A wave's sums on their way out: 16 rows of 16 FRAGMENTS columns at a time through the part of LDS that the operands' buffers leave, so that
 // a lane has four columns next to its neighbours', of rows that a loop goes through.  (With the epilogue's code written out for every
 // fragment's four results, 64 times in the largest tile, it came from memory for each tile: 40 us a tile whatever the activation, 590 us for
-// 4,096 x 16,384 x 4,096.)  What a chunk asks of memory is asked for ahead of the stores of the one before it: a load waits for all stores before it.
+// 4,096 x 16,384 x 4,096; now 428 to 445, with gelu_tanh and slope 500.)  What a chunk asks of memory is asked for ahead of the stores of the one before it: a load waits for all stores before it.
 template <typename S>
 struct Way {
     static constexpr int FRAGMENTS = S::FM == 8 ? 8 : 2;
@@ -274,6 +278,7 @@ __device__ __forceinline__ void make_product(const ProductArgs &a, const E &end,
         if (!place(i, tm, tn, split)) return false;
         const int32_t k0 = split * a.k_split;
         w = Work{tm * S::BM, tn * S::BN, k0 / kStepK, a.k - k0 < a.k_split ? a.k - k0 : a.k_split};
+        if (S::kGroup == 4 && w.k >= kTurned && w.k % kStepK == 0) w.turn = tm / kPanel * 3 % 8 * (w.k / kStepK / 8);
         return true;
     };
     auto store = [&](int32_t i, f32x4(&acc)[S::FM][S::FN], int wm, int wn, int lane) CFGZIP_INLINE {
@@ -322,7 +327,7 @@ __device__ __forceinline__ void make_product(const ProductArgs &a, const E &end,
             }
         }
     };
-    multiply<T, S, TileA, TileB>(a.A, a.B, lds, work, store, NoScales{});
+    multiply<T, S, TileA, TileB, S::kGroup == 4>(a.A, a.B, lds, work, store, NoScales{});
 }
 
 template <typename T, typename S, bool A_COLUMNS, bool B_COLUMNS, bool A_DIRECT, bool B_DIRECT, typename E>
@@ -631,7 +636,8 @@ __global__ __launch_bounds__(256) void bias_kernel(BiasArgs a) {
     add_up_bias<T>(a, shared, blockIdx.x);
 }
 
-// All that comes of dz in one launch, where the tiles of each product are few and small: the workgroups of one fill what those of the other leave.
+// All that comes of dz in one launch, where the tiles of each product are few and small: the workgroups of one fill what those of the other leave
+// (777 x 1,001 x 1,000 fp16 13 + 16 + 4 us one after the other, 19 together).
 struct AllArgs {
     ProductArgs hidden, weight;
     Gradient hidden_end, weight_end;

@@ -128,6 +128,16 @@ def test_largest_tiles_and_few_rows(lib, N, M, D):
     check(lib, make(11, N, M, D, "bf16"), "bf16", "silu")
 
 
+@pytest.mark.parametrize("N,M,D", [(4000, 4100, 8256), (4000, 8256, 4104), (8256, 4000, 4104)])
+def test_long_sums_of_the_largest_tiles(lib, N, M, D):
+    """Equal rows have equal results, whatever step their tiles begin with"""
+    print(f"case N={N} M={M} D={D}", flush=True)
+    s = make(20, N, M, D, "bf16", residual=False)
+    s["x"][N - 7] = s["x"][1]
+    out, _ = check(lib, s, "bf16", "gelu")
+    assert torch.equal(out[N - 7], out[1])
+
+
 def test_offsets_beyond_32_bits(lib):
     """Results that begin more than 2^31 elements behind the first one"""
     N, M, D = 140_000, 16_384, 64
