@@ -28,7 +28,8 @@ constexpr int64_t kFewWeights = 1 << 22;
 constexpr int32_t kTurned = 8192;
 constexpr int32_t kMaxRows = 1 << 21;  // (a launch goes over them in blocks of 64, fewer than 2^16)
 constexpr int64_t kComputeUnits = 256;
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLog2eD = 1.44269504088896340736;
+constexpr float kLog2e = (float)kLog2eD;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---------------------------------------------------------------- epilogues
@@ -69,6 +70,7 @@ __device__ __forceinline__ float normal(float z, float &bell) {
 struct Activation {
     int32_t kind;
     float a, b;  // of neither: what is not above a is 0 (-infinity: there is no activation)
+    float a_bits, b_bits;  // -log2(e) times those
 
     template <int KIND>
     __device__ __forceinline__ float of(float z, float &slope) const {
@@ -82,8 +84,8 @@ struct Activation {
             return z * q;
         } else {
             const float zz = __builtin_fminf(z * z, 1e30f);  // (an infinity is no factor of b = 0, and q is 0 or 1 from far less on)
-            const float u = z * __builtin_fmaf(b, zz, a);
-            const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -kLog2e));
+            const float u = z * __builtin_fmaf(b_bits, zz, a_bits);
+            const float q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
             slope = __builtin_fmaf(z * q * (1.0f - q), __builtin_fmaf(3.0f * b, zz, a), q);
             return z * q;
         }
@@ -146,22 +148,25 @@ struct Forward {
     __device__ __forceinline__ Row row(int32_t n, int32_t m) const {
         return residual ? read4(residual + n * residual_ld + m, M - m) : u32x2{0, 0};
     }
-    template <typename T, int KIND>
-    __device__ __forceinline__ f32x4 result(f32x4 z, Column b, Row r, u32x2 &codes) const {
+    template <typename T, int KIND, bool SLOPE>
+    __device__ __forceinline__ f32x4 result(f32x4 z, Column b, u32x2 &codes) const {
         f32x4 y;
         float s[4];
-        each<4>([&](auto i) CFGZIP_INLINE {
-            y[i.value] = act.of<KIND>(z[i.value] + value_at<T>(b, i.value), s[i.value]) + value_at<T>(r, i.value);
-        });
-        codes = u32x2{slope_codes(s[0], s[1]), slope_codes(s[2], s[3])};
+        each<4>([&](auto i) CFGZIP_INLINE { y[i.value] = act.of<KIND>(z[i.value] + value_at<T>(b, i.value), s[i.value]); });
+        if constexpr (SLOPE) codes = u32x2{slope_codes(s[0], s[1]), slope_codes(s[2], s[3])};
         return y;
+    }
+    template <typename T>
+    static __device__ __forceinline__ void add(f32x4 &y, Row r) {
+        each<4>([&](auto i) CFGZIP_INLINE { y[i.value] += value_at<T>(r, i.value); });
     }
     template <typename T>
     __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z, Column b, Row r) const {
         const int32_t left = M - m;
         f32x4 y;
         u32x2 codes;
-        act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value>(z, b, r, codes); });
+        act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value, true>(z, b, codes); });
+        add<T>(y, r);
         if (slope) write4(slope + n * slope_ld + m, codes, left);
         if (f32) write4(static_cast<float *>(out) + n * out_ld + m, y, left);
         else write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y), left);
@@ -169,10 +174,18 @@ struct Forward {
     // Those of P rows, STEP apart, that there are: nothing branches among the results.
     template <typename T, int P, int STEP>
     __device__ __forceinline__ void store_rows(int32_t n, int32_t N, int32_t m, f32x4 (&z)[P], Column b, const Row (&r)[P]) const {
+        // Slopes and residuals that nobody wants are left out where there are many rows (of the largest tiles; 4,096 x 16,384 x 4,096 464 us and 439 with
+        // gelu_tanh, 497 and 487 with slopes too).  Of few the branches cost more (256 x 4,096 x 4,096 21.7 and 24.7).
+        constexpr bool kBranches = P > 2;
         u32x2 codes[P];
         act.with([&](auto kind) CFGZIP_INLINE {
-            each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value>(z[p.value], b, r[p.value], codes[p.value]); });
+            auto all = [&](auto wanted) CFGZIP_INLINE {
+                each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value, wanted.value>(z[p.value], b, codes[p.value]); });
+            };
+            if (kBranches && !slope) all(std::false_type{});
+            else all(std::true_type{});
         });
+        if (!kBranches || residual) each<P>([&](auto p) CFGZIP_INLINE { add<T>(z[p.value], r[p.value]); });
         if (slope)
             each<P>([&](auto p) CFGZIP_INLINE {
                 if (n + p.value * STEP < N) write4(slope + (n + p.value * STEP) * slope_ld + m, codes[p.value], M - m);
@@ -957,12 +970,12 @@ extern "C" int cfgzip_head_layer(const void *hidden, int64_t hidden_stride, cons
     if (out == residual && (f32 || out_stride != residual_stride)) return CFGZIP_E_INVALID;
     const double a = 2.0 * 0.79788456080286535588;  // 2 sqrt(2 / pi)
     const bool tanh = activation == CFGZIP_ACT_GELU_TANH;
+    const double b = tanh ? 0.044715 * a : 0.0, of_z = tanh ? a : 1.0;
     const Activation act{activation,
                          activation == CFGZIP_ACT_NONE   ? -__builtin_inff()
                          : activation == CFGZIP_ACT_RELU ? 0.0f
-                         : tanh                          ? (float)a
-                                                         : 1.0f,
-                         tanh ? (float)(0.044715 * a) : 0.0f};
+                                                         : (float)of_z,
+                         (float)b, (float)(of_z * -kLog2eD), (float)(b * -kLog2eD)};
     const Forward end{static_cast<const uint16_t *>(bias), static_cast<const uint16_t *>(residual), residual_stride, act, out, out_stride, f32,
                       static_cast<uint16_t *>(slope), slope_stride, M};
     Carver carve(ws);
