@@ -148,25 +148,23 @@ struct Forward {
     __device__ __forceinline__ Row row(int32_t n, int32_t m) const {
         return residual ? read4(residual + n * residual_ld + m, M - m) : u32x2{0, 0};
     }
-    template <typename T, int KIND, bool SLOPE>
-    __device__ __forceinline__ f32x4 result(f32x4 z, Column b, u32x2 &codes) const {
+    template <typename T, int KIND, bool SLOPE, bool RESIDUAL>
+    __device__ __forceinline__ f32x4 result(f32x4 z, Column b, Row r, u32x2 &codes) const {
         f32x4 y;
         float s[4];
-        each<4>([&](auto i) CFGZIP_INLINE { y[i.value] = act.of<KIND>(z[i.value] + value_at<T>(b, i.value), s[i.value]); });
+        each<4>([&](auto i) CFGZIP_INLINE {
+            y[i.value] = act.of<KIND>(z[i.value] + value_at<T>(b, i.value), s[i.value]);
+            if constexpr (RESIDUAL) y[i.value] += value_at<T>(r, i.value);
+        });
         if constexpr (SLOPE) codes = u32x2{slope_codes(s[0], s[1]), slope_codes(s[2], s[3])};
         return y;
-    }
-    template <typename T>
-    static __device__ __forceinline__ void add(f32x4 &y, Row r) {
-        each<4>([&](auto i) CFGZIP_INLINE { y[i.value] += value_at<T>(r, i.value); });
     }
     template <typename T>
     __device__ __forceinline__ void store(int32_t n, int32_t m, f32x4 z, Column b, Row r) const {
         const int32_t left = M - m;
         f32x4 y;
         u32x2 codes;
-        act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value, true>(z, b, codes); });
-        add<T>(y, r);
+        act.with([&](auto kind) CFGZIP_INLINE { y = result<T, kind.value, true, true>(z, b, r, codes); });
         if (slope) write4(slope + n * slope_ld + m, codes, left);
         if (f32) write4(static_cast<float *>(out) + n * out_ld + m, y, left);
         else write4(static_cast<uint16_t *>(out) + n * out_ld + m, round4<T>(y), left);
@@ -180,12 +178,13 @@ struct Forward {
         u32x2 codes[P];
         act.with([&](auto kind) CFGZIP_INLINE {
             auto all = [&](auto wanted) CFGZIP_INLINE {
-                each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value, wanted.value>(z[p.value], b, codes[p.value]); });
+                each<P>([&](auto p) CFGZIP_INLINE { z[p.value] = result<T, kind.value, wanted.value, !kBranches>(z[p.value], b, r[p.value], codes[p.value]); });
             };
             if (kBranches && !slope) all(std::false_type{});
             else all(std::true_type{});
         });
-        if (!kBranches || residual) each<P>([&](auto p) CFGZIP_INLINE { add<T>(z[p.value], r[p.value]); });
+        if (kBranches && residual)
+            each<P>([&](auto p) CFGZIP_INLINE { each<4>([&](auto i) CFGZIP_INLINE { z[p.value][i.value] += value_at<T>(r[p.value], i.value); }); });
         if (slope)
             each<P>([&](auto p) CFGZIP_INLINE {
                 if (n + p.value * STEP < N) write4(slope + (n + p.value * STEP) * slope_ld + m, codes[p.value], M - m);
@@ -257,7 +256,7 @@ __device__ __forceinline__ f32x4 taken(const f32x4 &acc) {
 // A wave's sums on their way out: 16 rows of 16 FRAGMENTS columns at a time through the part of LDS that the operands' buffers leave, so that
 // a lane has four columns next to its neighbours', of rows that a loop goes through.  (With the epilogue's code written out for every
 // fragment's four results, 64 times in the largest tile, it came from memory for each tile: 40 us a tile whatever the activation, 590 us for
-// 4,096 x 16,384 x 4,096; now 428 to 445, with gelu_tanh and slope 500.)  What a chunk asks of memory is asked for ahead of the stores of the one before it: a load waits for all stores before it.
+// 4,096 x 16,384 x 4,096; now 428 to 445 without a slope, 490 with one.)  What a chunk asks of memory is asked for ahead of the stores of the one before it: a load waits for all stores before it.
 template <typename S>
 struct Way {
     static constexpr int FRAGMENTS = S::FM == 8 ? 8 : 2;
